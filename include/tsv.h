@@ -82,7 +82,9 @@ enum {                         /* per-sequence status bits, device-written */
   TSV_ST_LENGTH = 4,          /* L[b] < 0 or L[b] + D > max_L                              */
   TSV_ST_CSA_CAP = 8,         /* csa_cap[b] < (L + D) / m_csa                              */
   TSV_ST_HCA_CAP = 16,        /* hca_cap[b] < (L + D) / m_hca                              */
-  TSV_ST_INTERNAL = 32        /* a bounded wait inside a kernel gave up                    */
+  TSV_ST_INTERNAL = 32,       /* a bounded wait inside a kernel gave up                    */
+  TSV_ST_PAGE = 64,           /* a page-table entry, slot or reference count that the call needs is not valid */
+  TSV_ST_POOL = 128           /* the pool has too few free pages                           */
 };
 
 enum {                         /* tsv_shape.flags */
@@ -303,6 +305,154 @@ int accept_and_refresh(const tsv_shape *shape, int32_t n_layers, const tsv_cache
 int tree_verify_attn_static(const tsv_shape *shape, const tsv_cache *cache, const tsv_nodes *nodes,
                             const tsv_scratch *scratch, void *out, int32_t *topk_idx,
                             int32_t *status, void *stream);
+
+/* ======================================================================================================================
+ * Token-level layers: the operators of a layer that attends to tokens, not to compressed entries -- the sliding-window
+ * layers that draft (Section "Three-Stage Speculative Forward": draft extend, draft decode) and every layer's window.
+ *
+ *     qk_norm_rope(new tokens)  ->  window_sink_attn(new tokens over the token cache)  ->  token_commit
+ *
+ * Conventions of the calls above hold: device pointers, host structs, no allocation, no synchronisation, 16-byte aligned
+ * vectors, negative codes before any launch, `status[b]` or-ed into for what only the device can see.  Two calls on
+ * different streams may overlap if they share no buffer that one of them writes (the workspace is one).
+ *
+ * New tokens are PACKED: those of sequence b are rows row0[b] .. row0[b] + n[b] - 1 of every [rows][...] array, in order
+ * of their positions (a chain: token i is at position L[b] + i) or, with `parent`, as the nodes of a draft tree (node i is
+ * at L[b] + its depth; parent before child).  n[b] may be 0; the ranges of two sequences must not overlap.  Rows of no
+ * sequence are neither read nor written; with rows = 0 the arrays may be NULL.  A sequence with a problem that the device sees (n[b] outside 0..max_n or rows
+ * outside 0..rows: TSV_ST_NODES; a bad parent array, or a tree of more than TSV_MAX_D nodes: TSV_ST_PARENT; L[b] < 0 or
+ * L[b] + n[b] > max_L: TSV_ST_LENGTH) gets zeros in its output rows, where those are inside 0..rows, and commits nothing.
+ * ====================================================================================================================== */
+
+/* HOST memory.  Supported: B <= 2^20, H a multiple of Hk, H <= 256, d a multiple of 8, 8 <= d <= 512, window >= 1, n_sink >= 0. */
+typedef struct tsv_tok_shape {
+  int32_t dtype;              /* TSV_FP32 | TSV_BF16                                        */
+  int32_t B;                  /* sequences                                                  */
+  int32_t H, Hk, d;           /* query heads, key/value heads (query head h reads h / (H / Hk)), head dim */
+  int32_t window;             /* a query at position p sees p - window + 1 .. p ...         */
+  int32_t n_sink;             /* ... and the first positions 0 .. n_sink - 1 (up to p)      */
+  int32_t max_n;              /* bound on n[b], at most 2^22                                */
+  int64_t max_L;              /* bound on L[b] + n[b], at most 2^30                          */
+  float sm_scale;             /* softmax scale; <= 0 means 1/sqrt(d)                        */
+  int32_t reserved;
+} tsv_tok_shape;
+
+/* Token-level keys and values of ONE layer.  Rows of Hk * d elements, one per token; the row of position pos of sequence b is
+ *   ring (page_table NULL):  b * (n_sink + window) + (pos < n_sink ? pos : n_sink + (pos - n_sink) % window)
+ *   pages:                   page_table[b][pos / page_tokens] * page_tokens + pos % page_tokens
+ * With n_sink = 0 these are win_kv of tsv_cache, ring or token pool (v = NULL).  Pages that hold no visible position may be
+ * missing (-1): a window layer can give back what lies between its sinks and its window.  Rows that are not visible may
+ * hold anything, also infinities and NaN. */
+typedef struct tsv_tok_cache {
+  int32_t *L;                 /* [B] committed tokens                                       */
+  void *k;
+  void *v;                    /* NULL: the keys are the values                              */
+  int64_t rows;               /* HOST value: rows allocated in k (and v)                    */
+  const int32_t *page_table;  /* [B][max_pages] or NULL: ring                               */
+  int32_t page_tokens, max_pages;
+} tsv_tok_cache;
+
+typedef struct tsv_tok_batch {
+  const int64_t *row0;        /* [B]                                                        */
+  const int32_t *n;           /* [B]                                                        */
+  const int32_t *parent;      /* [rows] node of the same sequence, -1 for node 0; or NULL: chains */
+  int64_t rows;               /* HOST value: rows of the packed arrays                      */
+} tsv_tok_batch;
+
+/* Vectors of the new tokens: token row r starts at element r * ld, its heads follow each other.  ld >= heads * d, a multiple
+ * of 8 (bf16) or 4 (fp32) elements: so q, k and v may be column ranges of one fused projection. */
+typedef struct tsv_tok_rows {
+  const void *q, *k, *v;
+  int64_t q_ld, k_ld, v_ld;
+} tsv_tok_rows;
+
+/*
+ * qk_norm_rope -- for every head of q and k of every new token, x / sqrt(mean(x^2) + eps) * w (wq, wk: [d] fp32, NULL: 1),
+ * and then dims first .. first + rot - 1 turned by angle_i = position * inv_freq[i], i < rot / 2 (fp32 frequencies; the
+ * product and its reduction in 64 bits), (a, b) -> (a cos - b sin, a sin + b cos) over the pairs
+ *   pairs = 0:  a = x[first + i],     b = x[first + rot / 2 + i]
+ *   pairs = 1:  a = x[first + 2 i],   b = x[first + 2 i + 1].
+ * rot is 0 or a multiple of 16, first a multiple of 8, first + rot <= d.  in->q or in->k may be NULL (that part is left
+ * out; not both).  q_out, k_out: rows of ldq, ldk elements; each may be its input.  L [B] is read only.  in->v is not used.
+ */
+int qk_norm_rope(const tsv_tok_shape *shape, const int32_t *L, const tsv_tok_batch *batch, const tsv_tok_rows *in,
+                 const float *wq, const float *wk, float eps, const float *inv_freq, int32_t rot, int32_t first, int32_t pairs,
+                 void *q_out, int64_t ldq, void *k_out, int64_t ldk, int32_t *status, void *stream);
+
+/* Bytes of `workspace` window_sink_attn needs for this shape and number of packed rows.  0 on bad shape; never 0 else. */
+size_t tsv_tok_workspace_bytes(const tsv_tok_shape *shape, int64_t rows);
+
+/*
+ * window_sink_attn -- out [rows][H][d] (storage dtype, packed like the queries, no padding):
+ *   out = sum_j softmax_j(sm_scale q.k_j) v_j  over the positions j <= p with j > p - window or j < n_sink,
+ * where the committed positions j < L[b] come from the cache and the others from the rows `in` of the call (in->v NULL iff
+ * cache->v is: the keys are the values).  In a tree a node sees, of the new tokens, itself and its ancestors, under the same
+ * window.  The cache is not written.  What a query may not see has no influence on its result, also if it is not finite.
+ * A page that a query needs and that is not one of the pool's (-1, beyond `rows`, or a position beyond max_pages) is left
+ * out, and the sequence flagged TSV_ST_PAGE.
+ */
+int window_sink_attn(const tsv_tok_shape *shape, const tsv_tok_cache *cache, const tsv_tok_batch *batch, const tsv_tok_rows *in,
+                     void *out, void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+
+/*
+ * token_commit -- rows of new tokens become committed: count[b] of them (NULL: n[b]), the i-th being node path[b][i] (path:
+ * [B][path_ld] int32, e.g. accept_path of accept_and_refresh; NULL: node i), into the cache rows of positions L[b] + i; then
+ * L[b] += count.  A sequence with status[b] != 0, on entry or found here (count outside 0..n[b] or beyond path_ld, a node
+ * outside 0..n[b] - 1: TSV_ST_NODES; a missing page: TSV_ST_PAGE), commits nothing.
+ */
+int token_commit(const tsv_tok_shape *shape, const tsv_tok_cache *cache, const tsv_tok_batch *batch, const tsv_tok_rows *in,
+                 const int32_t *path, int32_t path_ld, const int32_t *count, int32_t *status, void *stream);
+
+/* ======================================================================================================================
+ * Pages of a paged pool: who holds them, and their contents.
+ * The pool has n_pages pages; `ref[p]` counts the sequences whose table row names page p (0: free).  A PLANE is an array with
+ * a fixed number of bytes per page (csa_kv, csa_ik, hca_kv, win_kv of every layer; k, v of a token cache): all planes are
+ * addressed by the same table.  A ROW array has a fixed number of bytes per sequence slot (L, capacities, the open-block
+ * states of every layer; a ring).  Fresh pages are always the free ones with the lowest numbers, in ascending order.
+ * The lists of a call (n entries, at most TSV_MAX_PAGE_LIST) are device arrays; `status[i]` belongs to entry i.
+ * Calls on one pool must be ordered (one stream).
+ * ====================================================================================================================== */
+#define TSV_MAX_PAGE_LIST 1024
+
+typedef struct tsv_page_array {
+  void *base;                 /* 16-byte aligned (planes), 4-byte aligned (rows)            */
+  int64_t bytes;              /* of a page (multiple of 16) or of a slot (multiple of 4)    */
+} tsv_page_array;
+
+typedef struct tsv_page_pool {
+  int32_t *page_table;        /* [slots][max_pages]; -1: no page                            */
+  int32_t *ref;               /* [n_pages]                                                  */
+  int32_t slots, max_pages, n_pages, page_tokens;
+  const tsv_page_array *planes;   /* HOST array, n_planes entries                           */
+  const tsv_page_array *rows;     /* HOST array, n_rows entries                             */
+  int32_t n_planes, n_rows;
+} tsv_page_pool;
+
+/* Bytes of `workspace` that pages_assign, pages_fork and pages_compact need for this pool.  0 on a bad pool. */
+size_t tsv_pages_workspace_bytes(const tsv_page_pool *pool);
+
+/* pages_assign -- logical pages first[i] .. last[i] - 1 of slot[i] that have no page get fresh ones: entries in order, logical
+ * pages ascending.  An entry for which too few pages are left gets none (TSV_ST_POOL; later entries still may). A slot may
+ * occur once. */
+int pages_assign(const tsv_page_pool *pool, int32_t n, const int32_t *slot, const int32_t *first, const int32_t *last, void *workspace,
+                 size_t workspace_bytes, int32_t *status, void *stream);
+
+/* pages_free -- slot[i] gives up its logical pages first[i] .. last[i] - 1 (those that it has); their contents stay until
+ * another sequence gets them.  A slot may occur more than once. */
+int pages_free(const tsv_page_pool *pool, int32_t n, const int32_t *slot, const int32_t *first, const int32_t *last, int32_t *status,
+               void *stream);
+
+/* pages_fork -- slot dst[i], which holds no pages, becomes a copy of slot src[i] with L[src[i]] committed tokens: its table row
+ * names the same pages where those are full (logical pages below L / page_tokens), and fresh ones elsewhere, the contents of
+ * the partly filled page copied in every plane; row dst[i] of every row array becomes row src[i].  All entries see the pool as
+ * it was before the call; a slot may be src of many, dst of one, and not both (TSV_ST_PAGE).  Where too few pages are left
+ * the entry changes nothing (TSV_ST_POOL; later entries still may).  L [slots] may be one of the row arrays. */
+int pages_fork(const tsv_page_pool *pool, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *L, void *workspace,
+               size_t workspace_bytes, int32_t *status, void *stream);
+
+/* pages_compact -- the used pages move to the numbers 0 .. n_used - 1: the page with the i-th lowest number >= n_used to the
+ * i-th lowest free number, in every plane, the table and the counts with it.  n_used: device, 1 value, written. */
+int pages_compact(const tsv_page_pool *pool, int32_t *n_used, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

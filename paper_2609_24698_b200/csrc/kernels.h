@@ -120,4 +120,20 @@ int prepare_tva_tc(const tsv_shape& s, const TvaPlan& p, const tsv_cache& c, con
 int launch_tva_tc(const tsv_shape& s, const TvaPlan& p, const TvaTcPrep& prep, const tsv_cache& c, const tsv_nodes& nd, const tsv_scratch& sc,
                   void* out, char* ws, int32_t* status, cudaStream_t st, bool with_plan = true);
 
+// Token-level operators and pages (tok_*.cu, pages.cu)
+int launch_rope(const tsv_tok_shape& s, const int32_t* L, const tsv_tok_batch& bt, const tsv_tok_rows& in, const float* wq, const float* wk, float eps,
+                const float* inv_freq, int rot, int first, int pairs, void* q_out, int64_t ldq, void* k_out, int64_t ldk, int32_t* status,
+                cudaStream_t st);
+size_t tok_attn_workspace(const tsv_tok_shape& s, int64_t rows);
+int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_tok_batch& bt, const tsv_tok_rows& in, void* out, char* ws, int32_t* status,
+                    cudaStream_t st);
+int launch_token_commit(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_tok_batch& bt, const tsv_tok_rows& in, const int32_t* path, int path_ld,
+                        const int32_t* count, int32_t* status, cudaStream_t st);
+size_t pages_workspace(const tsv_page_pool& p);
+int launch_pages_assign(const tsv_page_pool& p, int n, const int32_t* slot, const int32_t* first, const int32_t* last, char* ws, int32_t* status,
+                        cudaStream_t st);
+int launch_pages_free(const tsv_page_pool& p, int n, const int32_t* slot, const int32_t* first, const int32_t* last, int32_t* status, cudaStream_t st);
+int launch_pages_fork(const tsv_page_pool& p, int n, const int32_t* src, const int32_t* dst, const int32_t* L, char* ws, int32_t* status, cudaStream_t st);
+int launch_pages_compact(const tsv_page_pool& p, int32_t* n_used, char* ws, cudaStream_t st);
+
 }  // namespace tsv

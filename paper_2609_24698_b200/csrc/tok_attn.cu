@@ -1,0 +1,613 @@
+// window_sink_attn: attention of packed new tokens over their sinks, their window and each other.
+//
+//   out = sum_j softmax_j(scale q.k_j) v_j,   j <= p and (j > p - window or j < n_sink); in a tree new tokens see ancestors only
+//
+// Kernels here: attn_mma_kernel (bf16: 16 query rows, mma.sync), attn_fp32_kernel (fp32: 16 query rows, FMAs), and
+// attn_join_kernel, which joins the partial outputs of tiles whose keys were split over CTAs.
+#include "tok_attn.cuh"
+#include "tc_common.cuh"
+
+namespace tsv {
+
+namespace {
+
+using tc::cp16;
+using tc::cp_commit;
+using tc::cp_wait;
+using tc::ex2;
+using tc::smem_u32;
+
+constexpr int kRows = 16;             // query rows of a tile
+constexpr int kThreads = 128;
+
+// Keys of this split: whole blocks of KB keys, the same number for every split.
+__device__ __forceinline__ void split_range(const AttnArgs& a, const TileList& t, int KB, int& k0, int& k1) {
+  const int blocks = (t.nk + KB - 1) / KB, per = (blocks + a.nsplit - 1) / a.nsplit;
+  k0 = min(t.nk, (int)blockIdx.z * per * KB);
+  k1 = min(t.nk, k0 + per * KB);
+}
+__device__ __forceinline__ size_t part_index(const AttnArgs& a) {      // of this CTA's first partial row
+  return (((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.nsplit + blockIdx.z) * kRows;
+}
+template <typename T>
+__device__ __forceinline__ T* out_row(const AttnArgs& a, const TileList& t, int r) {
+  const int g = t.r0 + r;
+  return reinterpret_cast<T*>(a.out) + ((t.row0 + g / t.G) * a.s.H + (size_t)t.hk * t.G + g % t.G) * a.s.d;
+}
+template <typename T>
+__device__ __forceinline__ const T* query_row(const AttnArgs& a, const TileList& t, int r) {
+  const int g = t.r0 + r;
+  return reinterpret_cast<const T*>(a.in.q) + (t.row0 + g / t.G) * a.in.q_ld + ((size_t)t.hk * t.G + g % t.G) * a.s.d;
+}
+template <typename T>
+__device__ __forceinline__ void zero_rows(const AttnArgs& a, const TileList& t) {
+  float z[Vec<T>::N];
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; ++e) z[e] = 0.f;
+  const int nv = a.s.d / Vec<T>::N;
+  for (int i = threadIdx.x; i < t.nr * nv; i += blockDim.x) st16(out_row<T>(a, t, i / nv) + (i % nv) * Vec<T>::N, z);
+}
+// Position and ancestors of row r.
+__device__ __forceinline__ void row_facts(const AttnArgs& a, const TileList& t, const int* depth, const uint32_t* anc, int r, int& p, uint32_t& an) {
+  const int tok = (t.r0 + r) / t.G;
+  p = t.L + (a.bt.parent ? depth[tok] : tok);
+  an = a.bt.parent ? anc[tok] : 0;
+}
+// Those rows of `bad` (a bit per row) that see something not finite, by their definition, a warp each.
+template <typename T>
+__device__ __forceinline__ void exact_rows(const AttnArgs& a, const TileList& t, const int* depth, const uint32_t* anc, uint32_t bad, int k0, int k1) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int r = warp; r < t.nr; r += kThreads / 32) {
+    if (!(bad >> r & 1u)) continue;
+    int p;
+    uint32_t an;
+    row_facts(a, t, depth, anc, r, p, an);
+    float m, l, o[16];
+    if (!exact_row<T>(a, t, depth, query_row<T>(a, t, r), p, an, k0, k1, m, l, o)) continue;
+    if (a.nsplit > 1) {
+      const size_t at = part_index(a) + r;
+      for (int i = 0; i < 16; ++i) if (lane + 32 * i < a.s.d) a.po[at * a.s.d + lane + 32 * i] = o[i];
+      if (lane == 0) a.pml[at] = make_float2(m, l);
+    } else {
+      T* out = out_row<T>(a, t, r);
+      for (int i = 0; i < 16; ++i) if (lane + 32 * i < a.s.d) out[lane + 32 * i] = from_f<T>(o[i] / l);    // (every score -inf: 0 / 0, as the formula has it)
+    }
+  }
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm2(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4t(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, const uint32_t* b) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<uint32_t*>(&h);
+}
+
+// ---------------------------------------------------------------- bf16, 16 rows
+// Four warps: of a block of KB keys each computes the scores of a quarter (16 rows x KB / 4 keys over all of d), the row maxima go
+// through shared memory, then each adds the whole block's P V to its quarter of the output columns (d / 4: 16 rows x 128 columns are
+// 64 registers at d = 512).  P is rounded to bf16 for the product (half a step, 2^-9, of a weight; the sum of the weights is of the
+// unrounded ones); scores, maxima, sums and the output are fp32.  Rows of K and V come by 16-byte asynchronous copies, the next
+// block under the arithmetic of the current one, through the page table or from the new rows: 16-byte chunks of a row are stored at
+// chunk ^ (row & 7), which keeps every ldmatrix free of bank conflicts.  DP: d rounded up to 64, 128, 256 or 512, the rest zero.
+template <int DP, int KB, bool SHARED>
+struct MmaSmem {
+  alignas(16) bf16 q[kRows * DP];
+  bf16 k[2][KB * DP];
+  bf16 v[SHARED ? 1 : 2][SHARED ? 8 : KB * DP];
+  bf16 p[kRows * KB];
+  int64_t code[2][KB];
+  float red[4][kRows], sum[4][kRows];
+  int depth[TSV_MAX_D];
+  uint32_t anc[TSV_MAX_D];
+  int pos[kRows];
+  uint32_t row_anc[kRows];
+  TileList t;
+  uint32_t bad;
+  int missing[2];                     // a key of the block has no page
+};
+
+template <int DP, int KB, bool SHARED>
+__global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  typedef MmaSmem<DP, KB, SHARED> Sm;
+  Sm& sm = *reinterpret_cast<Sm*>(smem_raw);
+  constexpr int CH = DP / 8, KW = KB / 4, NT = KW / 8;    // 16-byte chunks of a row; keys of a warp, in tiles of 8
+  constexpr int CW = DP / 4, CT = CW / 8;                 // output columns of a warp, in tiles of 8
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (warp == 0) {
+    const TileList t = make_list(a, blockIdx.x, blockIdx.y, kRows, sm.depth, sm.anc);
+    if (lane == 0) { sm.t = t; sm.bad = 0; sm.missing[0] = sm.missing[1] = 0; }
+  }
+  __syncthreads();
+  const TileList& t = sm.t;
+  if (t.ok != 1) {
+    if (t.ok == 2 && a.nsplit == 1) zero_rows<bf16>(a, t);
+    return;
+  }
+  int k0, k1;
+  split_range(a, t, KB, k0, k1);
+  if (tid < kRows) {
+    int p = 0;
+    uint32_t an = 0;
+    if (tid < t.nr) row_facts(a, t, sm.depth, sm.anc, tid, p, an);
+    sm.pos[tid] = p; sm.row_anc[tid] = an;
+  }
+  auto codes = [&](int j) {                               // the rows behind block j
+    if (tid >= KB) return;
+    const int kk = k0 + j * KB + tid;
+    int64_t code = -1;
+    if (kk < k1) {
+      code = list_row(a, t, kk);
+      if (code == -1) { sm.missing[j & 1] = 1; atomicOr(a.status + t.b, TSV_ST_PAGE); }
+    }
+    sm.code[j & 1][tid] = code;
+  };
+  const int dch = a.s.d / 8;
+  auto load = [&](int j) {
+    const uint32_t ks = smem_u32(sm.k[j & 1]), vs = smem_u32(sm.v[SHARED ? 0 : j & 1]);
+    for (int i = tid; i < KB * CH; i += kThreads) {
+      const int r = i / CH, c = i % CH;
+      const int64_t code = sm.code[j & 1][r];
+      const bool live = code != -1 && c < dch;
+      const uint32_t at = (uint32_t)(r * CH + (c ^ (r & 7))) * 16;
+      cp16(ks + at, live ? (const void*)(row_ptr<bf16>(a, t.hk, code, false) + c * 8) : a.in.k, live);
+      if (!SHARED) cp16(vs + at, live ? (const void*)(row_ptr<bf16>(a, t.hk, code, true) + c * 8) : a.in.k, live);
+    }
+  };
+  const int nb = (k1 - k0 + KB - 1) / KB;
+  const uint32_t qs = smem_u32(sm.q);
+  for (int i = tid; i < kRows * CH; i += kThreads) {
+    const int r = i / CH, c = i % CH;
+    const bool live = r < t.nr && c < dch;
+    cp16(qs + (uint32_t)(r * CH + (c ^ (r & 7))) * 16, live ? (const void*)(query_row<bf16>(a, t, r) + c * 8) : a.in.q, live);
+  }
+  __syncthreads();
+  const int g = lane >> 2, tc = lane & 3;
+  int rp[2];
+  uint32_t ra[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) { rp[h] = sm.pos[g + 8 * h]; ra[h] = sm.row_anc[g + 8 * h]; }
+  for (int pass = 0; pass < 2; ++pass) {                  // (the second one only where a result is not finite)
+  codes(0);
+  __syncthreads();
+  if (nb) load(0);
+  cp_commit();
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float o[CT][4];
+#pragma unroll
+  for (int i = 0; i < CT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+  const uint32_t ps = smem_u32(sm.p);
+  for (int j = 0; j < nb; ++j) {
+    if (j + 1 < nb) codes(j + 1);
+    cp_wait<0>();
+    if (pass)                                             // (what this thread has copied)
+      for (int i = tid; i < KB * CH; i += kThreads) make_finite<bf16>((SHARED ? sm.k[j & 1] : sm.v[SHARED ? 0 : j & 1]) + (i / CH * CH + (i % CH ^ (i / CH & 7))) * 8);
+    __syncthreads();                                      // block j is here; everyone is done with block j - 1
+    if (j + 1 < nb) load(j + 1);
+    cp_commit();
+    const uint32_t ks = smem_u32(sm.k[j & 1]), vs = SHARED ? ks : smem_u32(sm.v[j & 1]);
+    // scores of this warp's keys
+    float s[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
+#pragma unroll 8
+    for (int kk = 0; kk < DP / 16; ++kk) {
+      uint32_t af[4];
+      { const int r = (lane & 7) + ((lane >> 3) & 1) * 8, c = 2 * kk + (lane >> 4);
+        ldsm4(af, qs + (uint32_t)(r * CH + (c ^ (r & 7))) * 16); }
+      if (NT == 2) {
+        uint32_t bf[4];
+        const int r = warp * KW + (lane & 7) + (lane >> 4) * 8, c = 2 * kk + ((lane >> 3) & 1);
+        ldsm4(bf, ks + (uint32_t)(r * CH + (c ^ (r & 7))) * 16);
+        mma16816(s[0], af, bf);
+        mma16816(s[NT - 1], af, bf + 2);
+      } else {
+        uint32_t bf[2];
+        const int r = warp * KW + (lane & 7), c = 2 * kk + ((lane >> 3) & 1);
+        ldsm2(bf, ks + (uint32_t)(r * CH + (c ^ (r & 7))) * 16);
+        mma16816(s[0], af, bf);
+      }
+    }
+    // masks, row maxima over the block
+    const bool missing = sm.missing[j & 1] != 0;
+    float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int h = e >> 1, key = warp * KW + i * 8 + 2 * tc + (e & 1), kk = k0 + j * KB + key;
+        bool see = kk < k1 && list_sees(a, t, sm.depth, rp[h], ra[h], kk);
+        if (missing && see) see = sm.code[j & 1][key] != -1;
+        s[i][e] = see ? s[i][e] * a.scale2 : -INFINITY;
+        mx[h] = fmaxf(mx[h], s[i][e]);
+      }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
+      mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
+      if (tc == 0) sm.red[warp][g + 8 * h] = mx[h];
+    }
+    __syncthreads();
+    float alpha[2], ref[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float mn = m[h];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) mn = fmaxf(mn, sm.red[w][g + 8 * h]);
+      ref[h] = mn == -INFINITY ? 0.f : mn;
+      alpha[h] = ex2(m[h] - ref[h]);
+      m[h] = mn;
+      l[h] *= alpha[h];
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { s[i][e] = ex2(s[i][e] - ref[e >> 1]); l[e >> 1] += s[i][e]; }
+      const int key = warp * KW + i * 8;                  // P: chunk of 8 keys, stored like the rows of K
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = g + 8 * h, c = key / 8;
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(sm.p) + (r * (KB / 8) + (c ^ (r & (KB / 8 - 1)))) * 16 + tc * 4) = pack2(s[i][2 * h], s[i][2 * h + 1]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] *= alpha[e >> 1];
+    if (tid == 0) sm.missing[j & 1] = 0;                  // (block j + 2's, set behind the next barrier)
+    __syncthreads();
+    // P V, this warp's columns
+#pragma unroll
+    for (int kk = 0; kk < KB / 16; ++kk) {
+      uint32_t af[4];
+      { const int r = (lane & 7) + ((lane >> 3) & 1) * 8, c = 2 * kk + (lane >> 4);
+        ldsm4(af, ps + (uint32_t)(r * (KB / 8) + (c ^ (r & (KB / 8 - 1)))) * 16); }
+#pragma unroll
+      for (int i = 0; i < CT; i += 2) {
+        uint32_t bf[4];
+        const int r = kk * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, c = (warp * CW) / 8 + i + (lane >> 4);
+        ldsm4t(bf, vs + (uint32_t)(r * CH + (c ^ (r & 7))) * 16);
+        mma16816(o[i], af, bf);
+        mma16816(o[i + 1], af, bf + 2);
+      }
+    }
+  }
+  // sums over the row's lanes and warps
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+    if (tc == 0) sm.sum[warp][g + 8 * h] = l[h];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = g + 8 * h;
+    l[h] = sm.sum[0][r] + sm.sum[1][r] + sm.sum[2][r] + sm.sum[3][r];
+    // (nothing of this split seen: {-inf, 0} and zeros; without splits every row sees its own key)
+    bool bad = !is_finite(l[h]) || (m[h] == -INFINITY && a.nsplit == 1);
+#pragma unroll
+    for (int i = 0; i < CT; ++i) bad |= !is_finite(o[i][2 * h]) || !is_finite(o[i][2 * h + 1]);
+    if (bad && pass == 0 && r < t.nr) atomicOr(&sm.bad, 1u << r);
+    const float inv = a.nsplit > 1 ? 1.f : 1.f / l[h];
+    if (r < t.nr) {
+      bf16* out = out_row<bf16>(a, t, r);
+      const size_t at = part_index(a) + r;
+#pragma unroll
+      for (int i = 0; i < CT; ++i) {
+        const int col = warp * CW + i * 8 + 2 * tc;
+        if (col >= a.s.d) continue;
+        if (a.nsplit > 1) *reinterpret_cast<float2*>(a.po + at * a.s.d + col) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
+        else *reinterpret_cast<uint32_t*>(out + col) = pack2(o[i][2 * h] * inv, o[i][2 * h + 1] * inv);
+      }
+      if (a.nsplit > 1 && warp == 0 && tc == 0) a.pml[at] = make_float2(m[h], l[h]);
+    }
+  }
+  __syncthreads();
+  if (!sm.bad) return;
+  }
+  exact_rows<bf16>(a, t, sm.depth, sm.anc, sm.bad, k0, k1);
+}
+
+// ---------------------------------------------------------------- fp32, 16 rows
+// The numerics type: FMAs in fp32.  Blocks of 32 keys in shared memory (rows padded by 16 bytes: a quarter-warp's loads of eight rows hit
+// eight different bank groups); a thread computes the scores of one key for four rows, then owns every 128th column of all 16 rows.
+constexpr int kKeys32 = 32;
+
+struct F32Ctl {
+  float p[kRows][kKeys32 + 4], alpha[kRows], m[kRows], l[kRows];
+  int64_t code[kKeys32];
+  int depth[TSV_MAX_D];
+  uint32_t anc[TSV_MAX_D];
+  int pos[kRows];
+  uint32_t row_anc[kRows];
+  TileList t;
+  uint32_t bad;
+};
+
+template <int NC>       // columns of a thread
+__global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  F32Ctl& sm = *reinterpret_cast<F32Ctl*>(smem_raw);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, d = a.s.d, ld = d + 4;
+  float* q = reinterpret_cast<float*>(smem_raw + ((sizeof(F32Ctl) + 15) & ~15));
+  float* ks = q + kRows * d;
+  float* vs = a.c.v ? ks + kKeys32 * ld : ks;
+  if (warp == 0) {
+    const TileList t = make_list(a, blockIdx.x, blockIdx.y, kRows, sm.depth, sm.anc);
+    if (lane == 0) { sm.t = t; sm.bad = 0; }
+  }
+  __syncthreads();
+  const TileList& t = sm.t;
+  if (t.ok != 1) {
+    if (t.ok == 2 && a.nsplit == 1) zero_rows<float>(a, t);
+    return;
+  }
+  int k0, k1;
+  split_range(a, t, kKeys32, k0, k1);
+  if (tid < kRows) {
+    int p = 0;
+    uint32_t an = 0;
+    if (tid < t.nr) row_facts(a, t, sm.depth, sm.anc, tid, p, an);
+    sm.pos[tid] = p; sm.row_anc[tid] = an;
+  }
+  const int nv = d / 4;
+  for (int i = tid; i < kRows * nv; i += kThreads) {
+    const int r = i / nv, c = i % nv;
+    cp16(smem_u32(q + r * d + c * 4), r < t.nr ? (const void*)(query_row<float>(a, t, r) + c * 4) : a.in.q, r < t.nr);
+  }
+  for (int pass = 0; pass < 2; ++pass) {                  // (the second one only where a result is not finite)
+  float o[NC][kRows];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) o[c][r] = 0.f;
+  if (tid < kRows) { sm.m[tid] = -INFINITY; sm.l[tid] = 0.f; }
+  for (int kb = k0; kb < k1; kb += kKeys32) {
+    __syncthreads();
+    if (tid < kKeys32) {
+      int64_t code = -1;
+      if (kb + tid < k1) {
+        code = list_row(a, t, kb + tid);
+        if (code == -1) atomicOr(a.status + t.b, TSV_ST_PAGE);
+      }
+      sm.code[tid] = code;
+    }
+    __syncthreads();
+    for (int i = tid; i < kKeys32 * nv; i += kThreads) {
+      const int r = i / nv, c = i % nv;
+      const int64_t code = sm.code[r];
+      cp16(smem_u32(ks + r * ld + c * 4), code != -1 ? (const void*)(row_ptr<float>(a, t.hk, code, false) + c * 4) : a.in.k, code != -1);
+      if (a.c.v) cp16(smem_u32(vs + r * ld + c * 4), code != -1 ? (const void*)(row_ptr<float>(a, t.hk, code, true) + c * 4) : a.in.k, code != -1);
+    }
+    cp_commit();
+    cp_wait<0>();
+    if (pass)                                             // (what this thread has copied)
+      for (int i = tid; i < kKeys32 * nv; i += kThreads) make_finite<float>(vs + i / nv * ld + i % nv * 4);
+    __syncthreads();
+    // scores: key `lane`, rows 4 warp ..
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < nv; ++c) {
+      const float4 kv = *reinterpret_cast<const float4*>(ks + lane * ld + c * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 qv = *reinterpret_cast<const float4*>(q + (4 * warp + i) * d + c * 4);
+        s[i] = fmaf(kv.x, qv.x, fmaf(kv.y, qv.y, fmaf(kv.z, qv.z, fmaf(kv.w, qv.w, s[i]))));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * warp + i;
+      const bool see = kb + lane < k1 && sm.code[lane] != -1 && list_sees(a, t, sm.depth, sm.pos[r], sm.row_anc[r], kb + lane);
+      s[i] = see ? s[i] * a.scale2 : -INFINITY;
+      float mx = s[i];
+#pragma unroll
+      for (int x = 16; x; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+      const float mo = sm.m[r], mn = fmaxf(mo, mx), ref = mn == -INFINITY ? 0.f : mn;
+      const float w = exp2f(s[i] - ref), al = exp2f(mo - ref);
+      const float sum = warp_sum(w);
+      sm.p[r][lane] = w;
+      __syncwarp();
+      if (lane == 0) { sm.alpha[r] = al; sm.m[r] = mn; sm.l[r] = sm.l[r] * al + sum; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const float al = sm.alpha[r];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) o[c][r] *= al;
+    }
+    for (int k = 0; k < kKeys32; k += 4) {
+      float v[NC][4];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[c][i] = tid + c * kThreads < d ? vs[(k + i) * ld + tid + c * kThreads] : 0.f;
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const float4 p = *reinterpret_cast<const float4*>(&sm.p[r][k]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c][r] = fmaf(p.x, v[c][0], fmaf(p.y, v[c][1], fmaf(p.z, v[c][2], fmaf(p.w, v[c][3], o[c][r]))));
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    if (r >= t.nr) break;
+    const float l = sm.l[r];
+    bool bad = !is_finite(l) || (sm.m[r] == -INFINITY && a.nsplit == 1);
+    const size_t at = part_index(a) + r;
+    float* out = a.nsplit > 1 ? a.po + at * d : out_row<float>(a, t, r);
+    const float inv = a.nsplit > 1 ? 1.f : 1.f / l;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      bad |= !is_finite(o[c][r]);
+      if (tid + c * kThreads < d) out[tid + c * kThreads] = o[c][r] * inv;
+    }
+    if (a.nsplit > 1 && tid == 0) a.pml[at] = make_float2(sm.m[r], l);
+    if (bad && pass == 0) atomicOr(&sm.bad, 1u << r);
+  }
+  __syncthreads();
+  if (!sm.bad) return;
+  }
+  exact_rows<float>(a, t, sm.depth, sm.anc, sm.bad, k0, k1);
+}
+
+// ---------------------------------------------------------------- partial outputs
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, splits in order.  A warp per row.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a, const int per) {
+  __shared__ TileList s_t;
+  __shared__ int depth[TSV_MAX_D];
+  __shared__ uint32_t anc[TSV_MAX_D];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.s.d;
+  if (warp == 0) {
+    const TileList t = make_list(a, blockIdx.x, blockIdx.y, per, depth, anc);
+    if (lane == 0) s_t = t;
+  }
+  __syncthreads();
+  const TileList& t = s_t;
+  if (t.ok == 2) zero_rows<T>(a, t);
+  if (t.ok != 1) return;
+  for (int r = warp + (kThreads / 32) * blockIdx.z; r < t.nr; r += (kThreads / 32) * gridDim.z) {
+    const size_t base = (((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.nsplit) * per + r;
+    float m = -INFINITY;
+    for (int i = 0; i < a.nsplit; ++i) m = fmaxf(m, a.pml[base + (size_t)i * per].x);
+    float l = 0.f, o[4][4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[c][e] = 0.f;
+    for (int i = 0; i < a.nsplit; ++i) {
+      const size_t at = base + (size_t)i * per;
+      const float2 ml = a.pml[at];
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;    // (nothing seen)
+      const float w = exp2f(ml.x - m);
+      l = fmaf(ml.y, w, l);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int col = (c * 32 + lane) * 4;
+        if (col < d) {
+          const float4 v = *reinterpret_cast<const float4*>(a.po + at * d + col);
+          o[c][0] = fmaf(v.x, w, o[c][0]); o[c][1] = fmaf(v.y, w, o[c][1]); o[c][2] = fmaf(v.z, w, o[c][2]); o[c][3] = fmaf(v.w, w, o[c][3]);
+        }
+      }
+    }
+    T* out = out_row<T>(a, t, r);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int col = (c * 32 + lane) * 4;
+      if (col < d) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[col + e] = from_f<T>(o[c][e] / l);
+      }
+    }
+  }
+}
+
+template <int DP, int KB, bool SHARED>
+int mma_launch(const AttnArgs& a, dim3 grid, cudaStream_t st) {
+  const int smem = (int)sizeof(MmaSmem<DP, KB, SHARED>);
+  if (!ensure_smem((const void*)attn_mma_kernel<DP, KB, SHARED>, smem)) return TSV_ERR_CUDA;
+  TSV_PREP((attn_mma_kernel<DP, KB, SHARED>));
+  attn_mma_kernel<DP, KB, SHARED><<<grid, kThreads, smem, st>>>(a);
+  count_launch();
+  return TSV_OK;
+}
+
+template <int NC>
+int fp32_launch(const AttnArgs& a, dim3 grid, cudaStream_t st) {
+  const int smem = (int)((sizeof(F32Ctl) + 15) & ~15) + 4 * (kRows * a.s.d + (a.c.v ? 2 : 1) * kKeys32 * (a.s.d + 4));
+  if (!ensure_smem((const void*)attn_fp32_kernel<NC>, smem)) return TSV_ERR_CUDA;
+  TSV_PREP(attn_fp32_kernel<NC>);
+  attn_fp32_kernel<NC><<<grid, kThreads, smem, st>>>(a);
+  count_launch();
+  return TSV_OK;
+}
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct AttnPlan {
+  int64_t tiles;          // row tiles over all sequences (bound)
+  int nsplit;
+  size_t off_po, off_pml;
+};
+
+// Keys are split where the tiles alone would leave SMs without work: into enough shares for two CTAs on each, of at least two blocks
+// of 64 keys.
+AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
+  AttnPlan p;
+  const int G = s.H / s.Hk;
+  p.tiles = tok_units_bound(s, rows, G, kRows);
+  const int64_t ctas = p.tiles * s.Hk;
+  int64_t reach = (int64_t)s.window + s.max_n;
+  if (reach > s.max_L) reach = s.max_L;
+  const int64_t keys = reach + (s.n_sink < s.max_L ? s.n_sink : s.max_L);
+  int64_t ns = (2 * 148 + ctas - 1) / ctas;
+  if (ns > (keys + 127) / 128) ns = (keys + 127) / 128;
+  if (ns > 64) ns = 64;
+  p.nsplit = (int)(ns < 1 ? 1 : ns);
+  p.off_po = 0;
+  p.off_pml = up256((size_t)4 * 148 * kRows * s.d * sizeof(float));
+  return p;
+}
+
+}  // namespace
+
+// The most that any number of rows up to `rows` takes: keys are split while the tiles are fewer than 2 * 148, into less than twice as
+// many CTAs as that.
+size_t tok_attn_workspace(const tsv_tok_shape& s, int64_t rows) {
+  (void)rows;
+  return up256((size_t)4 * 148 * kRows * s.d * sizeof(float)) + up256((size_t)4 * 148 * kRows * sizeof(float2));
+}
+
+int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_tok_batch& bt, const tsv_tok_rows& in, void* out, char* ws, int32_t* status,
+                    cudaStream_t st) {
+  const AttnPlan p = plan_of(s, bt.rows);
+  if (p.tiles > 0x7fffffff) return TSV_ERR_LIMIT;
+  AttnArgs a;
+  a.s = s; a.c = c; a.bt = bt; a.in = in; a.out = out;
+  a.po = reinterpret_cast<float*>(ws + p.off_po);
+  a.pml = reinterpret_cast<float2*>(ws + p.off_pml);
+  a.G = s.H / s.Hk;
+  a.nsplit = p.nsplit;
+  a.scale2 = s.sm_scale * 1.4426950408889634f;
+  a.status = status;
+  const dim3 grid((unsigned)p.tiles, s.Hk, p.nsplit);
+  int r;
+  if (s.dtype == TSV_FP32) {
+    r = s.d <= 128 ? fp32_launch<1>(a, grid, st) : s.d <= 256 ? fp32_launch<2>(a, grid, st) : fp32_launch<4>(a, grid, st);
+  } else if (!c.v) {
+    r = s.d <= 64 ? mma_launch<64, 64, true>(a, grid, st) : s.d <= 128 ? mma_launch<128, 64, true>(a, grid, st)
+      : s.d <= 256 ? mma_launch<256, 64, true>(a, grid, st) : mma_launch<512, 64, true>(a, grid, st);
+  } else {
+    r = s.d <= 64 ? mma_launch<64, 64, false>(a, grid, st) : s.d <= 128 ? mma_launch<128, 64, false>(a, grid, st)
+      : s.d <= 256 ? mma_launch<256, 64, false>(a, grid, st) : mma_launch<512, 32, false>(a, grid, st);
+  }
+  if (r) return r;
+  if (p.nsplit > 1) {
+    const dim3 jg((unsigned)p.tiles, s.Hk, 4);
+    if (s.dtype == TSV_FP32) attn_join_kernel<float><<<jg, kThreads, 0, st>>>(a, kRows);
+    else attn_join_kernel<bf16><<<jg, kThreads, 0, st>>>(a, kRows);
+    count_launch();
+  }
+  return cudaGetLastError() == cudaSuccess ? TSV_OK : TSV_ERR_CUDA;
+}
+
+}  // namespace tsv

@@ -1,0 +1,136 @@
+// token_commit: rows of new tokens (a chain, or the accepted path of a tree) into the token cache, then L += count.
+//
+// A copy: bound by HBM, by latency for the few rows of a tree.  Where a sequence has at most 64 rows to give, one CTA copies them
+// and moves L itself: one launch.  With more, CTAs share the rows and a second kernel moves L when all of them have read it.
+#include "tok_common.cuh"
+
+namespace tsv {
+
+namespace {
+
+constexpr int kCommitThreads = 256;
+constexpr int kCommitRows = 16;          // rows of a CTA where several share a sequence
+
+struct CommitArgs {
+  tsv_tok_shape s;
+  tsv_tok_cache c;
+  tsv_tok_batch bt;
+  const void *k, *v;
+  int64_t k_bytes, v_bytes;              // of a packed row's stride
+  const int32_t *path, *count;
+  int32_t path_ld, row_vecs;             // 16-byte vectors of a row
+  int32_t* status;
+};
+
+// What sequence b gives, by the whole CTA alike: its count, 0 if it is flagged.  All rows of the sequence are looked over by every
+// CTA that takes part of them, so that either all of them are written or none.
+__device__ __forceinline__ int commit_count(const CommitArgs& a, int b, int n, int L, int* s_bad) {
+  const int cnt = a.count ? __ldg(a.count + b) : n;
+  if (threadIdx.x == 0) {
+    int st = 0;
+    if (cnt < 0 || cnt > n || (a.path && cnt > a.path_ld)) st |= TSV_ST_NODES;
+    if (L < 0 || (int64_t)L + n > a.s.max_L) st |= TSV_ST_LENGTH;
+    *s_bad = st;
+  }
+  __syncthreads();
+  if (!*s_bad) {
+    int st = 0;
+    if (a.path)
+      for (int i = threadIdx.x; i < cnt; i += kCommitThreads) {
+        const int node = __ldg(a.path + (size_t)b * a.path_ld + i);
+        if (node < 0 || node >= n) st |= TSV_ST_NODES;
+      }
+    if (a.c.page_table && cnt > 0)
+      for (int lp = L / a.c.page_tokens + threadIdx.x; lp <= (L + cnt - 1) / a.c.page_tokens; lp += kCommitThreads)
+        if (tok_cache_row(a.c, a.s.window, a.s.n_sink, b, min(lp * a.c.page_tokens + a.c.page_tokens - 1, L + cnt - 1)) < 0) st |= TSV_ST_PAGE;
+    if (st) atomicOr(s_bad, st);
+    __syncthreads();
+  }
+  const int st = *s_bad;
+  __syncthreads();
+  if (st) {
+    if (threadIdx.x == 0) atomicOr(a.status + b, st);
+    return 0;
+  }
+  return cnt;
+}
+
+__device__ __forceinline__ void commit_rows(const CommitArgs& a, const TokUnit& u, int L, int cnt, int i0, int i1) {
+  const int rv = a.row_vecs, planes = a.v ? 2 : 1;
+  const int64_t total = (int64_t)(i1 - i0) * rv * planes;
+  for (int64_t t = threadIdx.x; t < total; t += kCommitThreads) {
+    const int plane = (int)(t / ((int64_t)(i1 - i0) * rv));
+    const int rest = (int)(t - (int64_t)plane * (i1 - i0) * rv), i = i0 + rest / rv, vec = rest % rv;
+    // a ring's slot keeps its last writer's row: earlier ones are not written
+    if (!a.c.page_table && L + i >= a.s.n_sink && i < cnt - a.s.window) continue;
+    const int node = a.path ? __ldg(a.path + (size_t)u.b * a.path_ld + i) : i;
+    const int64_t row = tok_cache_row(a.c, a.s.window, a.s.n_sink, u.b, L + i);
+    const char* src = reinterpret_cast<const char*>(plane ? a.v : a.k) + (u.row0 + node) * (plane ? a.v_bytes : a.k_bytes);
+    char* dst = reinterpret_cast<char*>(plane ? a.c.v : a.c.k) + row * rv * 16;
+    reinterpret_cast<uint4*>(dst)[vec] = __ldg(reinterpret_cast<const uint4*>(src) + vec);
+  }
+}
+
+__global__ void __launch_bounds__(kCommitThreads) commit_seq_kernel(const CommitArgs a) {
+  __shared__ int s_bad;
+  TokUnit u;
+  u.b = blockIdx.x; u.unit = 0;
+  const int flags = a.status[u.b];                        // (read by every thread ahead of the first barrier, written behind it)
+  u.n = tok_count(a.s, a.bt, u.b, nullptr, u.row0);
+  if (u.n < 0 && threadIdx.x == 0) atomicOr(a.status + u.b, TSV_ST_NODES);
+  if (u.n < 0) return;
+  const int L = a.c.L[u.b];
+  if (__syncthreads_or(flags)) return;
+  const int cnt = commit_count(a, u.b, u.n, L, &s_bad);
+  commit_rows(a, u, L, cnt, 0, cnt);
+  if (threadIdx.x == 0 && cnt) a.c.L[u.b] = L + cnt;      // (every thread has read L before a barrier of commit_count)
+}
+
+__global__ void __launch_bounds__(kCommitThreads) commit_rows_kernel(const CommitArgs a) {
+  __shared__ int s_bad, s_found;
+  __shared__ TokUnit s_u;
+  if (threadIdx.x < 32) {
+    TokUnit u;
+    const bool f = find_unit(a.s, a.bt, 1, kCommitRows, blockIdx.x, a.status, u);
+    if (threadIdx.x == 0) { s_found = f && a.status[u.b] == 0; s_u = u; }
+  }
+  __syncthreads();
+  if (!s_found) return;
+  const TokUnit u = s_u;
+  const int L = a.c.L[u.b];
+  const int cnt = commit_count(a, u.b, u.n, L, &s_bad);
+  const int i0 = u.unit * kCommitRows, i1 = min(cnt, i0 + kCommitRows);
+  if (i0 < i1) commit_rows(a, u, L, cnt, i0, i1);
+}
+
+__global__ void commit_lengths_kernel(const CommitArgs a) {
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b >= a.s.B || a.status[b]) return;
+  const int n = __ldg(a.bt.n + b), cnt = a.count ? __ldg(a.count + b) : n;
+  if (n == 0 && cnt != 0) atomicOr(a.status + b, TSV_ST_NODES);       // (no CTA has looked at a sequence without tokens)
+  else a.c.L[b] += cnt;
+}
+
+}  // namespace
+
+int launch_token_commit(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_tok_batch& bt, const tsv_tok_rows& in, const int32_t* path, int path_ld,
+                        const int32_t* count, int32_t* status, cudaStream_t st) {
+  const int es = s.dtype == TSV_BF16 ? 2 : 4;
+  CommitArgs a = {s, c, bt, in.k, in.v, in.k_ld * es, in.v_ld * es, path, count, path_ld, s.Hk * s.d * es / 16, status};
+  if (s.max_n <= 64) {
+    TSV_PREP(commit_seq_kernel);
+    commit_seq_kernel<<<s.B, kCommitThreads, 0, st>>>(a);
+    count_launch();
+  } else {
+    const int64_t units = tok_units_bound(s, bt.rows, 1, kCommitRows);
+    if (units > 0x7fffffff) return TSV_ERR_LIMIT;
+    TSV_PREP(commit_rows_kernel);
+    TSV_PREP(commit_lengths_kernel);
+    commit_rows_kernel<<<(unsigned)units, kCommitThreads, 0, st>>>(a);
+    commit_lengths_kernel<<<(s.B + 127) / 128, 128, 0, st>>>(a);
+    count_launch(2);
+  }
+  return cudaGetLastError() == cudaSuccess ? TSV_OK : TSV_ERR_CUDA;
+}
+
+}  // namespace tsv

@@ -1,0 +1,117 @@
+"""Pages of a paged pool over the C-ABI library: handing out, giving back, forking sequences, compacting (include/tsv.h, "Pages
+of a paged pool").  Argument marshalling and checks only.
+
+A pool is a page table, a count of holders per page, the PLANES that hold the pages' contents (csa_kv, csa_ik, hca_kv, win_kv of
+every layer; k and v of token caches) and the ROWS with what a sequence has besides (lengths, capacities, open-block states).
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding as tsv
+from .binding import TsvError, _aligned, _lib, _p, _stream
+from .tokens import ST_PAGE, ST_POOL, _check  # noqa: F401
+
+MAX_LIST = 1024
+
+
+class CPageArray(C.Structure):
+    _fields_ = [("base", _p), ("bytes", C.c_int64)]
+
+
+class CPagePool(C.Structure):
+    _fields_ = [("page_table", _p), ("ref", _p), ("slots", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page_tokens", C.c_int32),
+                ("planes", _p), ("rows", _p), ("n_planes", C.c_int32), ("n_rows", C.c_int32)]
+
+
+_lib.tsv_pages_workspace_bytes.restype = C.c_size_t
+_lib.tsv_pages_workspace_bytes.argtypes = [_p]
+_lib.pages_assign.restype = C.c_int
+_lib.pages_assign.argtypes = [_p, C.c_int32, _p, _p, _p, _p, C.c_size_t, _p, _p]
+_lib.pages_free.restype = C.c_int
+_lib.pages_free.argtypes = [_p, C.c_int32, _p, _p, _p, _p, _p]
+_lib.pages_fork.restype = C.c_int
+_lib.pages_fork.argtypes = [_p, C.c_int32, _p, _p, _p, _p, C.c_size_t, _p, _p]
+_lib.pages_compact.restype = C.c_int
+_lib.pages_compact.argtypes = [_p, _p, _p, C.c_size_t, _p]
+
+_at = C.addressof
+
+
+class PagePool:
+    """Description of a pool over the caller's tensors, which it keeps: page_table [slots, max_pages] and ref [n_pages] (int32), planes
+    (contiguous, the same share of each belongs to a page) and rows (contiguous, [slots, ...])."""
+
+    def __init__(self, page_table: torch.Tensor, ref: torch.Tensor, page_tokens: int, planes: Sequence[torch.Tensor], rows: Sequence[torch.Tensor] = ()):
+        slots, max_pages = page_table.shape
+        n = ref.numel()
+        self.page_table, self.ref, self.planes, self.rows = page_table, ref, list(planes), list(rows)
+        for t, parts, what in [(t, n, "plane") for t in self.planes] + [(t, slots, "row array") for t in self.rows]:
+            if not t.is_cuda or t.device != page_table.device or not t.is_contiguous() or t.numel() % parts:
+                raise TsvError(tsv.ERR_SHAPE, f"PagePool: a {what} must be contiguous on {page_table.device} and divide into {parts}, got {tuple(t.shape)}")
+        arrays = lambda ts, parts: (CPageArray * max(1, len(ts)))(*[CPageArray(t.data_ptr(), t.numel() // parts * t.element_size()) for t in ts])
+        self._planes, self._rows = arrays(self.planes, n), arrays(self.rows, slots)
+        self.c = CPagePool(_check("page_table", page_table, torch.int32, slots * max_pages), _check("ref", ref, torch.int32, n), slots, max_pages, n,
+                           page_tokens, _at(self._planes), _at(self._rows), len(self.planes), len(self.rows))
+
+    @staticmethod
+    def of_layers(caches: Sequence[tsv.LayerCache], ref: Optional[torch.Tensor] = None) -> "PagePool":
+        """The pool behind the paged caches of layers that share one page table tensor; ref: the counts, by default those that the table
+        shows."""
+        c0 = caches[0]
+        if c0.page_table is None or any(c.page_table is None or c.page_table.data_ptr() != c0.page_table.data_ptr() for c in caches):
+            raise TsvError(tsv.ERR_SHAPE, "PagePool.of_layers: the layers must share one page table")
+        n = c0.win_kv.shape[0] // c0.page_tokens
+        if ref is None:
+            held = c0.page_table.flatten().long()
+            ref = torch.zeros(n, dtype=torch.int32, device=held.device).index_add_(0, held.clamp(min=0), (held >= 0).int())
+        planes = [t for c in caches for t in (c.csa_kv, c.csa_ik, c.hca_kv, c.win_kv)]
+        rows = [t for c in caches for t in (c.L, c.csa_cap, c.hca_cap, c.csa_mx, c.csa_s, c.csa_acc_kv, c.csa_acc_ik, c.hca_mx, c.hca_s, c.hca_acc_kv)]
+        return PagePool(c0.page_table, ref, c0.page_tokens, planes, rows)
+
+
+def alloc_workspace(pool: PagePool) -> torch.Tensor:
+    n = int(_lib.tsv_pages_workspace_bytes(_at(pool.c)))
+    if n == 0:
+        raise TsvError(tsv.ERR_SHAPE, "tsv_pages_workspace_bytes")
+    return torch.empty(n + 256, dtype=torch.uint8, device=pool.page_table.device)
+
+
+def _list(n: int, *lists: torch.Tensor):
+    return [_check("list", t, torch.int32, n) for t in lists]
+
+
+def _raise(r: int, where: str) -> None:
+    if r:
+        raise TsvError(r, where)
+
+
+def pages_assign(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor,
+                 stream=None) -> None:
+    """Logical pages first[i] .. last[i] - 1 of slots[i] that have no page get the free ones with the lowest numbers."""
+    n = slots.numel()
+    wp, wn = _aligned(workspace)
+    _raise(_lib.pages_assign(_at(pool.c), n, *_list(n, slots, first, last), wp, wn, *_list(n, status), _stream(stream)), "pages_assign")
+
+
+def pages_free(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    """slots[i] gives up its logical pages first[i] .. last[i] - 1."""
+    n = slots.numel()
+    _raise(_lib.pages_free(_at(pool.c), n, *_list(n, slots, first, last, status), _stream(stream)), "pages_free")
+
+
+def pages_fork(pool: PagePool, src: torch.Tensor, dst: torch.Tensor, L: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    """dst[i], a slot without pages, becomes a copy of src[i] with L[src[i]] tokens: full pages shared, the last one and the rows copied."""
+    n = src.numel()
+    wp, wn = _aligned(workspace)
+    _raise(_lib.pages_fork(_at(pool.c), n, *_list(n, src, dst), _check("L", L, torch.int32, pool.c.slots), wp, wn, *_list(n, status), _stream(stream)),
+           "pages_fork")
+
+
+def pages_compact(pool: PagePool, n_used: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """The used pages move to the lowest numbers, contents, table and counts; n_used (int32, 1 value) becomes their number."""
+    wp, wn = _aligned(workspace)
+    _raise(_lib.pages_compact(_at(pool.c), _check("n_used", n_used, torch.int32, 1), wp, wn, _stream(stream)), "pages_compact")
