@@ -2,8 +2,8 @@
 //
 //   out = sum_j softmax_j(scale q.k_j) v_j,   j <= p and (j > p - window or j < n_sink); in a tree new tokens see ancestors only
 //
-// Kernels here: attn_mma_kernel (bf16: 16 query rows, mma.sync), attn_fp32_kernel (fp32: 16 query rows, FMAs), and
-// attn_join_kernel, which joins the partial outputs of tiles whose keys were split over CTAs.
+// Kernels here: attn_mma_kernel (bf16, few rows per sequence: 16 query rows, mma.sync), attn_fp32_kernel (fp32: 16 query rows, FMAs), and
+// attn_join_kernel, which joins the partial outputs of tiles whose keys were split over CTAs.  Calls with more rows: tok_attn_tc.cu.
 #include "tok_attn.cuh"
 #include "tc_common.cuh"
 
@@ -544,37 +544,43 @@ int fp32_launch(const AttnArgs& a, dim3 grid, cudaStream_t st) {
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct AttnPlan {
-  int64_t tiles;          // row tiles over all sequences (bound)
+  bool tc;                // 128-row tiles on the tensor cores
+  int per;                // query rows of a tile
+  int64_t tiles;          // tiles over all sequences (bound)
   int nsplit;
-  size_t off_po, off_pml;
+  size_t off_pml;
 };
 
-// Keys are split where the tiles alone would leave SMs without work: into enough shares for two CTAs on each, of at least two blocks
-// of 64 keys.
+// bf16 tiles of 128 rows where a sequence may have enough rows for a key head to fill a good part of one.
+bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s.max_n * (s.H / s.Hk) >= 48; }
+
+// Tiles and CTAs that splitting the keys aims at: those that run at a time.
+int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? tc_slots(s.d) / tc_halves(s.d) : 2 * 148; }
+
+// Keys are split where the tiles alone would leave SMs without work, into shares of some blocks of keys each.
 AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   AttnPlan p;
-  const int G = s.H / s.Hk;
-  p.tiles = tok_units_bound(s, rows, G, kRows);
+  p.tc = takes_tc(s);
+  p.per = p.tc ? kTcTile : kRows;
+  p.tiles = tok_units_bound(s, rows, s.H / s.Hk, p.per);
   const int64_t ctas = p.tiles * s.Hk;
   int64_t reach = (int64_t)s.window + s.max_n;
   if (reach > s.max_L) reach = s.max_L;
-  const int64_t keys = reach + (s.n_sink < s.max_L ? s.n_sink : s.max_L);
-  int64_t ns = (2 * 148 + ctas - 1) / ctas;
-  if (ns > (keys + 127) / 128) ns = (keys + 127) / 128;
+  const int64_t keys = reach + (s.n_sink < s.max_L ? s.n_sink : s.max_L), least = p.tc ? 512 : 128;
+  int64_t ns = (slots_of(s) + ctas - 1) / ctas;
+  if (ns > (keys + least - 1) / least) ns = (keys + least - 1) / least;
   if (ns > 64) ns = 64;
   p.nsplit = (int)(ns < 1 ? 1 : ns);
-  p.off_po = 0;
-  p.off_pml = up256((size_t)4 * 148 * kRows * s.d * sizeof(float));
+  p.off_pml = up256((size_t)2 * slots_of(s) * p.per * s.d * sizeof(float));
   return p;
 }
 
 }  // namespace
 
-// The most that any number of rows up to `rows` takes: keys are split while the tiles are fewer than 2 * 148, into less than twice as
-// many CTAs as that.
+// The most that any number of rows takes: keys are split while there are fewer tiles than slots_of, into less than twice as many.
 size_t tok_attn_workspace(const tsv_tok_shape& s, int64_t rows) {
-  (void)rows;
-  return up256((size_t)4 * 148 * kRows * s.d * sizeof(float)) + up256((size_t)4 * 148 * kRows * sizeof(float2));
+  const AttnPlan p = plan_of(s, rows);
+  return p.off_pml + up256((size_t)2 * slots_of(s) * p.per * sizeof(float2));
 }
 
 int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_tok_batch& bt, const tsv_tok_rows& in, void* out, char* ws, int32_t* status,
@@ -583,7 +589,7 @@ int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_to
   if (p.tiles > 0x7fffffff) return TSV_ERR_LIMIT;
   AttnArgs a;
   a.s = s; a.c = c; a.bt = bt; a.in = in; a.out = out;
-  a.po = reinterpret_cast<float*>(ws + p.off_po);
+  a.po = reinterpret_cast<float*>(ws);
   a.pml = reinterpret_cast<float2*>(ws + p.off_pml);
   a.G = s.H / s.Hk;
   a.nsplit = p.nsplit;
@@ -591,7 +597,9 @@ int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_to
   a.status = status;
   const dim3 grid((unsigned)p.tiles, s.Hk, p.nsplit);
   int r;
-  if (s.dtype == TSV_FP32) {
+  if (p.tc) {
+    r = launch_attn_tc(a, p.tiles, st);
+  } else if (s.dtype == TSV_FP32) {
     r = s.d <= 128 ? fp32_launch<1>(a, grid, st) : s.d <= 256 ? fp32_launch<2>(a, grid, st) : fp32_launch<4>(a, grid, st);
   } else if (!c.v) {
     r = s.d <= 64 ? mma_launch<64, 64, true>(a, grid, st) : s.d <= 128 ? mma_launch<128, 64, true>(a, grid, st)
@@ -602,9 +610,9 @@ int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_to
   }
   if (r) return r;
   if (p.nsplit > 1) {
-    const dim3 jg((unsigned)p.tiles, s.Hk, 4);
-    if (s.dtype == TSV_FP32) attn_join_kernel<float><<<jg, kThreads, 0, st>>>(a, kRows);
-    else attn_join_kernel<bf16><<<jg, kThreads, 0, st>>>(a, kRows);
+    const dim3 jg((unsigned)p.tiles, s.Hk, p.per / 4);
+    if (s.dtype == TSV_FP32) attn_join_kernel<float><<<jg, kThreads, 0, st>>>(a, p.per);
+    else attn_join_kernel<bf16><<<jg, kThreads, 0, st>>>(a, p.per);
     count_launch();
   }
   return cudaGetLastError() == cudaSuccess ? TSV_OK : TSV_ERR_CUDA;

@@ -24,6 +24,12 @@ struct AttnArgs {
   int32_t* status;
 };
 
+// The tensor-core path (tok_attn_tc.cu): tiles of 128 rows.  `units`: tiles over all sequences (a bound); columns of a CTA.
+int launch_attn_tc(const AttnArgs& a, int64_t units, cudaStream_t st);
+constexpr int kTcTile = 128;
+inline int tc_halves(int d) { return d > 256 ? 2 : 1; }
+inline int tc_slots(int d) { return d > 128 ? 148 : 2 * 148; }      // CTAs that run at a time
+
 struct TileList {
   int b, n, L, G;
   int64_t row0;

@@ -1,0 +1,591 @@
+// window_sink_attn on the tensor cores (tcgen05), bf16: tiles of 128 query rows of one sequence and key head.
+//
+// A persistent CTA walks over work items (tile, key head, columns, share of the keys), warps by role:
+//   warps 0-3   softmax and epilogue, a row per thread
+//   warp 4      issues the products: S = Q K^T, then O += P V with P as the A operand straight from tensor memory
+//   warps 5-8   copy Q, K and V rows into shared memory (16-byte asynchronous copies: rows come from pages, a ring or the call's own
+//               tensors, any of them with strides of their own, which no tensor map describes)
+// K and V live in panels of 128 rows x 64 columns (16 KiB, 128-byte swizzle): K row-major is the K-major operand of S, and the same
+// layout read MN-major the operand of P V, so that where the keys are the values one copy serves both products.
+//
+// Tensor memory: S (128 columns, two buffers where a CTA has the SM to itself) and O.  P (bf16) overlays the S it came from.  d = 512 has
+// no room for S beside all of O (512 columns): two CTAs take 256 output columns each and compute S and the softmax alike.  Up to
+// d = 128, 256 columns and at most 96 KiB let two CTAs share an SM: one's softmax runs under the other's products.
+//
+// Softmax: a block of 128 keys at a time.  Its row maximum becomes the row's reference only where it exceeds the old one by more than 2^8
+// (bf16 and fp32 have the range for weights above one): then O and the sum are rescaled, nearly never after the first block.
+// P is rounded to bf16 for the product (2^-9 of a weight); scores, sums and O are fp32.
+#include "tc_common.cuh"
+#include "tok_attn.cuh"
+
+namespace tsv {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = kTcTile;        // query rows of a tile, keys of a block
+constexpr int kMmaWarp = 4, kProducers = 128;      // (warps 0-3 before it)
+constexpr int kTcThreads = 288;
+constexpr int kPanel = 16384;
+constexpr int kLag = 3;               // panels whose copies may be under way behind the one being requested
+constexpr float kGap = 8.f;           // log2 units by which a maximum may exceed the row's reference
+constexpr int kCtl = 3072;
+
+template <int DP, bool SHARED>
+struct Cfg {
+  static constexpr int OC = DP < 256 ? DP : 256;             // output columns of an item
+  static constexpr int HALVES = DP / OC;
+  static constexpr int NP = DP / 64, VP = OC / 64;           // panels of all of d, of the output columns
+  static constexpr int KP = SHARED ? NP - VP : NP;           // panels that only S reads
+  static constexpr int NKS = KP == 0 ? 0 : DP == 256 ? 4 : 2;          // ring of those
+  static constexpr int NVB = DP == 64 ? (SHARED ? 4 : 2) : SHARED && DP <= 256 ? 2 : 1;   // buffers of the others, VP panels each
+  static constexpr int SB = DP >= 256 ? 2 : 1;               // S buffers
+  static constexpr int TM = DP >= 256 ? 512 : 256;           // tensor memory columns
+  static constexpr int OCC = DP >= 256 ? 1 : 2;              // CTAs per SM
+  static constexpr int SMEM = kCtl + (NP + NKS + NVB * VP) * kPanel;
+};
+
+struct TcCtl {
+  uint64_t fullQ[8], emptyQ;
+  uint64_t fullK[4], emptyK[4];
+  uint64_t fullV[8], emptyV[4];
+  uint64_t s_full[2], p_ready[2], pv_done, o_free;
+  uint32_t tmem_base;
+  uint32_t redo[32];                  // items with a result that is not finite, a bit each
+  int depth[9][TSV_MAX_D];            // of the item's tree, a copy per warp
+  uint32_t anc[9][TSV_MAX_D];
+};
+static_assert(sizeof(TcCtl) + kTile * 2 <= kCtl, "control block overflow");
+
+__device__ __forceinline__ void bar_init(uint64_t* b, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// Bits [lo, hi) of a word, any lo and hi.
+__device__ __forceinline__ uint32_t bits(int lo, int hi) {
+  lo = max(lo, 0); hi = min(hi, 32);
+  return lo >= hi ? 0u : (0xffffffffu << lo) & (0xffffffffu >> (32 - hi));
+}
+
+struct TcArgs {
+  AttnArgs a;
+  int64_t items;
+};
+
+template <int DP, bool SHARED>
+__global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_kernel(const __grid_constant__ TcArgs g) {
+  typedef Cfg<DP, SHARED> C;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  const AttnArgs& a = g.a;
+  TcCtl& sm = *reinterpret_cast<TcCtl*>(smem_raw);
+  const uint32_t base = smem_u32(smem_raw) + kCtl;
+  const uint32_t q_at = base, k_at = q_at + C::NP * kPanel, v_at = k_at + C::NKS * kPanel;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
+  if (tid == 0) {
+    for (int i = 0; i < 8; ++i) { bar_init(&sm.fullQ[i], kProducers); bar_init(&sm.fullV[i], kProducers); }
+    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullK[i], kProducers); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
+    for (int i = 0; i < 2; ++i) { bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); }
+    bar_init(&sm.emptyQ, 1); bar_init(&sm.pv_done, 1); bar_init(&sm.o_free, kTile);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid < 32) sm.redo[tid] = 0;
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem_base)), "n"(C::TM) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + C::SB * kTile;
+
+  // An item's tile, columns and keys
+  struct Item { TileList t; int half, k0, k1, nb, split; int64_t unit; };
+  auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !mbar_wait(b, parity)) fail = 1; };
+  // Calls body(item, mode) for this CTA's items (mode 0), then, for those that left a mark, twice more: computed as before, for which
+  // rows are not finite (1), then with values that are not finite taken as zero (2).
+  auto walk = [&](auto&& body, auto&& finish) {
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {
+      int li = 0;
+#pragma unroll 1
+      for (int64_t idx = blockIdx.x; idx < g.items; idx += gridDim.x, ++li) {
+        if (round && !(sm.redo[(li >> 5) & 31] >> (li & 31) & 1u)) continue;
+        Item w;
+        w.half = (int)(idx % C::HALVES);
+        int64_t r = idx / C::HALVES;
+        const int hk = (int)(r % a.s.Hk);
+        r /= a.s.Hk;
+        w.split = (int)(r % a.nsplit);
+        w.unit = r / a.nsplit;
+        w.t = make_list(a, w.unit, hk, kTile, sm.depth[warp], sm.anc[warp]);
+        __syncwarp();
+        if (!w.t.ok) break;
+        w.k0 = w.k1 = w.nb = 0;
+        if (w.t.ok == 1) {
+          const int blocks = (w.t.nk + kTile - 1) / kTile, per = (blocks + a.nsplit - 1) / a.nsplit;
+          w.k0 = min(w.t.nk, w.split * per * kTile);
+          w.k1 = min(w.t.nk, w.k0 + per * kTile);
+          w.nb = (w.k1 - w.k0 + kTile - 1) / kTile;
+        }
+        for (int mode = round; mode <= 2 * round; ++mode) body(w, mode, li);
+      }
+      finish();                                                 // (before this role waits for the others)
+      if (round == 0) {
+        __syncthreads();
+        uint32_t any = 0;
+        for (int i = 0; i < 32; ++i) any |= sm.redo[i];
+        if (!any) break;                                        // (alike in all threads)
+      }
+    }
+  };
+  auto rows_of_block = [&](const Item& w, int j) { return min(kTile, w.k1 - w.k0 - j * kTile); };
+
+  if (warp > kMmaWarp) {
+    // ------------------------------------------------------------------ producers
+    const int pt = tid - 32 * (kMmaWarp + 1), prow = pt >> 3, chunk = pt & 7;    // rows prow + 16 i, one 16-byte chunk of a panel
+    uint64_t* pend[kLag];
+    int np = 0;                                            // panels requested and not announced
+    auto announce = [&](int keep) {                        // those before the last `keep`
+      if (keep == 0) cp_wait<0>(); else cp_wait<kLag - 1>();
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      if (keep == 0) {
+#pragma unroll
+        for (int i = 0; i < kLag; ++i) if (i < np) bar_arrive(pend[i]);
+        np = 0;
+      } else {
+        bar_arrive(pend[0]);
+#pragma unroll
+        for (int i = 0; i + 1 < kLag; ++i) pend[i] = pend[i + 1];
+        --np;
+      }
+    };
+    auto push = [&](uint64_t* b) {
+      cp_commit();
+#pragma unroll
+      for (int i = 0; i < kLag; ++i) if (i == np) pend[i] = b;
+      if (++np == kLag) announce(kLag - 1);
+    };
+    auto acquire = [&](uint64_t* b, uint32_t parity) {     // (nothing may stay unannounced while this waits: its release may depend on it)
+      if (np && !bar_test(b, parity)) announce(0);
+      wait(b, parity);
+    };
+    const int dch = a.s.d / 8;
+    uint32_t cQ = 0, cK = 0, cV = 0;
+    const uint32_t off = (uint32_t)prow * 128 + ((chunk ^ (prow & 7)) << 4);     // (rows 16 apart: the same swizzle)
+    walk([&](const Item& w, int mode, int) {
+      if (w.nb == 0) return;
+      const bf16* ptr[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = prow + 16 * i, gr = w.t.r0 + r;
+        ptr[i] = r < w.t.nr ? reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)w.t.hk * a.G + gr % a.G) * a.s.d : nullptr;
+      }
+      acquire(&sm.emptyQ, (cQ & 1) ^ 1);
+#pragma unroll 1
+      for (int p = 0; p < C::NP; ++p) {
+        // (in the order in which S takes them: the item's own output columns last where K is V)
+        const int pan = SHARED && C::KP ? (p + (w.half + 1) * C::VP) % C::NP : p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bool live = ptr[i] && pan * 8 + chunk < dch;
+          cp16(q_at + p * kPanel + off + i * 2048, live ? (const void*)(ptr[i] + pan * 64 + chunk * 8) : a.in.q, live);
+        }
+        push(&sm.fullQ[p]);
+      }
+      ++cQ;
+#pragma unroll 1
+      for (int j = 0; j < w.nb; ++j) {
+        const int rows = rows_of_block(w, j), rows16 = (rows + 15) & ~15;
+        int64_t code[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = prow + 16 * i;
+          code[i] = -1;
+          if (r < rows) {
+            code[i] = list_row(a, w.t, w.k0 + j * kTile + r);
+            if (code[i] == -1) atomicOr(a.status + w.t.b, TSV_ST_PAGE);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ptr[i] = code[i] == -1 ? nullptr : row_ptr<bf16>(a, w.t.hk, code[i], false);
+        auto panel = [&](uint32_t at, int pan) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (16 * i >= rows16) break;
+            const bool live = ptr[i] && pan * 8 + chunk < dch;
+            cp16(at + off + i * 2048, live ? (const void*)(ptr[i] + pan * 64 + chunk * 8) : a.in.q, live);
+          }
+        };
+#pragma unroll 1
+        for (int p = 0; p < C::KP; ++p) {
+          const int slot = cK % (C::NKS ? C::NKS : 1);
+          acquire(&sm.emptyK[slot], (cK / (C::NKS ? C::NKS : 1) & 1) ^ 1);
+          panel(k_at + slot * kPanel, SHARED ? (p + (w.half + 1) * C::VP) % C::NP : p);
+          push(&sm.fullK[slot]);
+          ++cK;
+        }
+        const int buf = cV % C::NVB;
+        if (!SHARED) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) ptr[i] = code[i] == -1 ? nullptr : row_ptr<bf16>(a, w.t.hk, code[i], true);
+        }
+        acquire(&sm.emptyV[buf], (cV / C::NVB & 1) ^ 1);
+#pragma unroll 1
+        for (int p = 0; p < C::VP; ++p) {
+          const uint32_t at = v_at + (buf * C::VP + p) * kPanel;
+          panel(at, w.half * C::VP + p);
+          if (mode == 2) {
+            cp_commit();
+            cp_wait<0>();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (16 * i < rows16) make_finite<bf16>(smem_raw + (at + off + i * 2048 - smem_u32(smem_raw)));
+          }
+          push(&sm.fullV[buf * C::VP + p]);
+        }
+        ++cV;
+      }
+    }, [&]() { if (np) announce(0); });
+  } else if (warp == kMmaWarp) {
+    // ------------------------------------------------------------------ products
+    const uint32_t idesc_v = make_idesc(C::OC, 1);
+    uint32_t cQ = 0, cK = 0, cVs = 0, cVo = 0, cS = 0, cP = 0;     // uses so far: Q, K panels, V buffers by S and by O, S and P
+    const bool one = lane == 0;
+    walk([&](const Item& w, int, int) {
+      if (w.nb == 0) return;
+      auto scores = [&](int j, int p0, int p1) {           // panels p0 .. p1 - 1 of block j
+        const uint32_t idesc = make_idesc((rows_of_block(w, j) + 15) & ~15, 0);
+        const uint32_t dst = s_col + (cS % C::SB) * kTile;
+        for (int p = p0; p < p1; ++p) {
+          if (j == 0) wait(&sm.fullQ[p], cQ & 1);
+          uint32_t at;
+          const bool ring = p < C::KP;
+          const int slot = cK % (C::NKS ? C::NKS : 1);
+          if (ring) {
+            wait(&sm.fullK[slot], cK / (C::NKS ? C::NKS : 1) & 1);
+            at = k_at + slot * kPanel;
+          } else {
+            const int buf = cVs % C::NVB;
+            wait(&sm.fullV[buf * C::VP + p - C::KP], cVs / C::NVB & 1);
+            at = v_at + (buf * C::VP + p - C::KP) * kPanel;
+          }
+          fence_after();
+          if (one) {
+            const uint64_t qd = make_desc(q_at + p * kPanel, 16, 1024), kd = make_desc(at, 16, 1024);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) mma_ss(dst, qd + 2 * ks, kd + 2 * ks, idesc, (p | ks) != 0);
+            if (ring) mma_commit(&sm.emptyK[slot]);
+          }
+          __syncwarp();
+          if (ring) ++cK;
+        }
+        if (p1 < C::NP) return;
+        if (one) {
+          mma_commit(&sm.s_full[cS % C::SB]);
+          if (j == w.nb - 1) mma_commit(&sm.emptyQ);
+        }
+        __syncwarp();
+        ++cS;
+        if (SHARED) ++cVs;
+      };
+      auto output = [&](int j) {
+        const int buf = cVo % C::NVB, sb = cP % C::SB;
+        if (!SHARED)
+          for (int p = 0; p < C::VP; ++p) wait(&sm.fullV[buf * C::VP + p], cVo / C::NVB & 1);
+        if (j == 0) wait(&sm.o_free, (cQ & 1) ^ 1);
+        wait(&sm.p_ready[sb], cP / C::SB & 1);
+        fence_after();
+        const int steps = (rows_of_block(w, j) + 15) / 16;
+        if (one) {
+          const uint64_t vd = make_desc(v_at + buf * C::VP * kPanel, kPanel, 1024);
+          for (int ks = 0; ks < steps; ++ks) mma_ts(o_col, s_col + sb * kTile + ks * 8, vd + ks * (2048 >> 4), idesc_v, (j | ks) != 0);
+          mma_commit(&sm.emptyV[buf]);
+          mma_commit(&sm.pv_done);
+        }
+        __syncwarp();
+        ++cVo; ++cP;
+      };
+      // The scores of the next block under the softmax of this one, where there is a second buffer for them: all of them, or, where the
+      // panels that both products read have one buffer, those of the other panels.
+      constexpr int AHEAD = C::SB == 1 ? 0 : SHARED && C::NVB == 1 ? C::KP : C::NP;
+      scores(0, 0, C::NP);
+      for (int j = 0; j < w.nb; ++j) {
+        if (AHEAD && j + 1 < w.nb) scores(j + 1, 0, AHEAD);
+        output(j);
+        if (AHEAD < C::NP && j + 1 < w.nb) scores(j + 1, AHEAD, C::NP);
+      }
+      ++cQ;
+    }, []() {});
+  } else {
+    // ------------------------------------------------------------------ softmax and epilogue
+    const uint32_t lane_at = (uint32_t)(warp * 32) << 16;
+    const int row = tid;
+    uint32_t cS = 0, cW = 0;                               // blocks so far; those whose P V is known to be complete
+    // (one by one, each before the P of the block after the next is announced: a parity says no more than the last phase)
+    auto wait_pv = [&](uint32_t blocks) { for (; cW != blocks; ++cW) wait(&sm.pv_done, cW & 1); fence_after(); };
+    bool bad = false;                                      // of mode 1, for mode 2
+    walk([&](const Item& w, int mode, int li) {
+      const TileList& t = w.t;
+      const size_t part = ((size_t)(w.unit * a.s.Hk + t.hk) * a.nsplit + w.split) * kTile + row;
+      const bool live = row < t.nr, lead = w.half == 0;
+      if (t.ok == 2) {                                     // (with the keys split: the join's)
+        if (mode == 0 && a.nsplit == 1 && live) {
+          const int gr = t.r0 + row;
+          uint4* o = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + (size_t)t.hk * a.G + gr % a.G) * a.s.d);
+          for (int c = w.half * (C::OC / 8); c < min(a.s.d / 8, (w.half + 1) * (C::OC / 8)); ++c) o[c] = make_uint4(0, 0, 0, 0);
+        }
+        return;
+      }
+      if (w.nb == 0) {                                     // (a share without keys: only where they are split)
+        if (mode == 0 && live && lead) a.pml[part] = make_float2(-INFINITY, 0.f);
+        return;
+      }
+      // what this row sees of the list: positions kmin .. kmax and those below ksink, nodes
+      const int tok = (t.r0 + (live ? row : 0)) / a.G;
+      const bool tree = a.bt.parent != nullptr;
+      const int* depth = sm.depth[warp];
+      const int p = t.L + (tree ? depth[tok] : tok);
+      const uint32_t an = tree ? sm.anc[warp][tok] : 0;
+      const int shift = t.ns - t.lo;                       // index of a position of the window part, less the position
+      const int kmin = p - a.s.window + 1 + shift, kmax = tree ? t.nc - 1 : p + shift;
+      const int ksink = max(t.ns, min(a.s.n_sink, t.nk) + shift);
+      uint32_t nodes = 0;
+      if (tree)
+        for (int j = 0; j < t.n; ++j)
+          if ((an >> j & 1u) && (t.L + depth[j] > p - a.s.window || t.L + depth[j] < a.s.n_sink)) nodes |= 1u << j;
+      // pages that are not there
+      bool missing = false;
+      if (a.c.page_table) {
+        const int P = a.c.page_tokens, hi = min(t.L, t.lo + (t.nc - t.ns)) - 1;
+        for (int lp = lane; lp <= (t.ns - 1) / P && lp * P < min(t.ns, t.L); lp += 32) missing |= tok_cache_row(a.c, a.s.window, a.s.n_sink, t.b, min(min(t.ns, t.L) - 1, lp * P + P - 1)) < 0;
+        for (int lp = t.lo / P + lane; lp <= hi / P && t.lo <= hi; lp += 32) missing |= tok_cache_row(a.c, a.s.window, a.s.n_sink, t.b, min(hi, lp * P + P - 1)) < 0;
+        missing = __any_sync(0xffffffffu, missing);
+      }
+      auto visible = [&](int c0) {                         // keys c0 .. c0 + 31 of the list, a bit each
+        uint32_t m = bits(max(kmin, 0) - c0, min(kmax + 1, t.nc) - c0) | bits(-c0, min(min(ksink, kmax + 1), t.nc) - c0);
+        if (tree) {
+          const int s = t.nc - c0;
+          if (s < 32 && s > -32) m |= s >= 0 ? nodes << s : nodes >> -s;
+        }
+        m &= bits(0, w.k1 - c0);
+        if (missing)
+          for (uint32_t x = m; x; x &= x - 1) { const int i = __ffs(x) - 1; if (list_row(a, t, c0 + i) == -1) m &= ~(1u << i); }
+        return m;
+      };
+      float ref = -INFINITY, l[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int j = 0; j < w.nb; ++j) {
+        const int sb = cS % C::SB, c0 = w.k0 + j * kTile, slabs = (rows_of_block(w, j) + 31) / 32;
+        const uint32_t scol = s_col + sb * kTile + lane_at;
+        wait(&sm.s_full[sb], cS / C::SB & 1);
+        fence_after();
+        uint32_t vis[4];
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i >= slabs) break;
+          vis[i] = visible(c0 + 32 * i);
+          uint32_t sv[32];
+          tmem_ld32(scol + 32 * i, sv);
+          if (__all_sync(0xffffffffu, vis[i] == 0xffffffffu)) {
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < 32; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(sv[e]));
+            mx = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) mx = fmaxf(mx, (vis[i] >> e & 1u) ? __uint_as_float(sv[e]) : -INFINITY);
+          }
+        }
+        mx *= a.scale2;
+        const bool up = mx > ref + kGap || (ref == -INFINITY && mx > ref);
+        if (__any_sync(0xffffffffu, up)) {
+          const float to = up ? mx : ref, f = up && ref != -INFINITY ? ex2(ref - to) : 1.f;
+          ref = to;
+          if (__any_sync(0xffffffffu, f != 1.f)) {         // (never in the first block)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l[i] *= f;
+            if (j) {
+              wait_pv(cS);
+#pragma unroll 1
+              for (int c = 0; c < C::OC; c += 32) {
+                uint32_t r[32];
+                tmem_ld32(o_col + lane_at + c, r);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+                tmem_st16(o_col + lane_at + c, r);
+                tmem_st16(o_col + lane_at + c + 16, r + 16);
+              }
+            }
+          }
+        }
+        const float neg = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i >= slabs) break;
+          uint32_t sv[32], pk[16];
+          tmem_ld32(scol + 32 * i, sv);
+          if (!__all_sync(0xffffffffu, vis[i] == 0xffffffffu)) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) if (!(vis[i] >> e & 1u)) sv[e] = 0xff800000u;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float p0 = ex2(fmaf(__uint_as_float(sv[e]), a.scale2, neg)), p1 = ex2(fmaf(__uint_as_float(sv[e + 1]), a.scale2, neg));
+            l[(e >> 1) & 3] += p0 + p1;
+            const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
+            pk[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          tmem_st16(scol + 16 * i, pk);
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        fence_before();
+        wait_pv(cS);
+        bar_arrive(&sm.p_ready[sb]);
+        ++cS;
+      }
+      // the output
+      const float sum = (l[0] + l[1]) + (l[2] + l[3]);
+      wait_pv(cS);
+      bool odd = !is_finite(sum) || (ref == -INFINITY && a.nsplit == 1);
+      fail = __any_sync(0xffffffffu, fail);
+      const uint32_t ocol = o_col + lane_at;
+      if (a.nsplit > 1) {
+        float* po = a.po + part * a.s.d + w.half * C::OC;
+#pragma unroll 1
+        for (int c = 0; c < C::OC; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(ocol + c, r);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            odd |= !(is_finite(__uint_as_float(r[e])) && is_finite(__uint_as_float(r[e + 1])) && is_finite(__uint_as_float(r[e + 2])) && is_finite(__uint_as_float(r[e + 3])));
+            if (live && mode != 1 && w.half * C::OC + c + e < a.s.d) *reinterpret_cast<uint4*>(po + c + e) = make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]);
+          }
+        }
+        if (live && lead && mode != 1) a.pml[part] = make_float2(ref, sum);
+      } else {
+        // read out so that four lanes share a row: they transpose their words, and a warp stores whole 128-byte lines of eight rows
+        const float inv = 1.f / sum;
+        const int quad = lane >> 2, qi = lane & 3;
+#pragma unroll 1
+        for (int hh = 0; hh < 2; ++hh) {
+          float iv[2];
+          bf16* o[2];
+          bool okr[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = 16 * hh + 8 * h + quad, gr = t.r0 + warp * 32 + r;
+            iv[h] = __shfl_sync(0xffffffffu, inv, r);
+            okr[h] = warp * 32 + r < t.nr && mode != 1;
+            o[h] = reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + (size_t)t.hk * a.G + gr % a.G) * a.s.d + w.half * C::OC;
+          }
+          bool bad_h[2] = {false, false};
+#pragma unroll 1
+          for (int c = 0; c < C::OC; c += 64) {
+            uint32_t r[32];
+            tmem_ld16x256b_x8_nowait(ocol + ((uint32_t)(16 * hh) << 16) + c, r);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            tmem_regs_ready(r);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t wd[8];                             // words of 8-column groups g = 0 .. 7: columns 8 g + 2 qi, + 1
+#pragma unroll
+              for (int gq = 0; gq < 8; ++gq) {
+                const float x = __uint_as_float(r[4 * gq + 2 * h]), y = __uint_as_float(r[4 * gq + 2 * h + 1]);
+                bad_h[h] |= !(is_finite(x) && is_finite(y));
+                const __nv_bfloat162 v = __floats2bfloat162_rn(x * iv[h], y * iv[h]);
+                wd[gq] = *reinterpret_cast<const uint32_t*>(&v);
+              }
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {               // groups 4 k .. 4 k + 3: lane qi gets all words of group 4 k + qi
+                uint32_t x[4] = {wd[4 * k], wd[4 * k + 1], wd[4 * k + 2], wd[4 * k + 3]};
+#pragma unroll
+                for (int m = 1; m <= 2; m <<= 1) {
+                  const bool upper = (qi & m) != 0;
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    if (!(i & m)) {
+                      const uint32_t send = upper ? x[i] : x[i | m], got = __shfl_xor_sync(0xffffffffu, send, m);
+                      if (upper) x[i] = got; else x[i | m] = got;
+                    }
+                }
+                const int col = c + (4 * k + qi) * 8;
+                if (okr[h] && w.half * C::OC + col < a.s.d) *reinterpret_cast<uint4*>(o[h] + col) = make_uint4(x[0], x[1], x[2], x[3]);
+              }
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {                   // a row's four lanes to the row's thread
+            uint32_t b = __ballot_sync(0xffffffffu, bad_h[h]);
+            if (lane >= 16 * hh + 8 * h && lane < 16 * hh + 8 * h + 8) odd |= (b >> (4 * (lane & 7)) & 15u) != 0;
+          }
+        }
+      }
+      fence_before();
+      bar_arrive(&sm.o_free);
+      odd = odd && live;
+      if (mode == 0 && odd) atomicOr(&sm.redo[(li >> 5) & 31], 1u << (li & 31));
+      if (mode == 1) bad = odd;
+      if (mode == 2) {
+        for (uint32_t todo = __ballot_sync(0xffffffffu, bad); todo; todo &= todo - 1) {
+          const int r = __ffs(todo) - 1, gr = t.r0 + warp * 32 + r, pr = __shfl_sync(0xffffffffu, p, r);
+          const uint32_t ar = __shfl_sync(0xffffffffu, an, r);
+          const size_t at = (size_t)t.hk * a.G + gr % a.G;
+          float m, ls, ov[16];
+          if (!exact_row<bf16>(a, t, depth, reinterpret_cast<const bf16*>(a.in.q) + (t.row0 + gr / a.G) * a.in.q_ld + at * a.s.d, pr, ar, w.k0, w.k1, m, ls, ov)) continue;
+          const size_t pa = part - row + warp * 32 + r;
+          bf16* o = reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + at) * a.s.d;
+          for (int i = w.half * (C::OC / 32); i < 16 && i < (w.half + 1) * (C::OC / 32); ++i) {
+            const int col = lane + 32 * i;
+            if (col >= a.s.d) continue;
+            if (a.nsplit > 1) a.po[pa * a.s.d + col] = ov[i]; else o[col] = from_f<bf16>(ov[i] / ls);
+          }
+          if (a.nsplit > 1 && lead && lane == 0) a.pml[pa] = make_float2(m, ls);
+        }
+      }
+    }, []() {});
+  }
+  if (__any_sync(0xffffffffu, fail)) for (int b = lane; b < a.s.B; b += 32) atomicOr(a.status + b, TSV_ST_INTERNAL);   // (an internal error: every sequence is flagged)
+  fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(C::TM) : "memory");
+}
+
+template <int DP, bool SHARED>
+int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
+  typedef Cfg<DP, SHARED> C;
+  TcArgs g;
+  g.a = a;
+  g.items = units * a.s.Hk * a.nsplit * C::HALVES;
+  if (!ensure_smem((const void*)attn_tc_kernel<DP, SHARED>, C::SMEM)) return TSV_ERR_CUDA;
+  TSV_PREP((attn_tc_kernel<DP, SHARED>));
+  const int64_t grid = g.items < 148 * C::OCC ? g.items : 148 * C::OCC;
+  attn_tc_kernel<DP, SHARED><<<(unsigned)grid, kTcThreads, C::SMEM, st>>>(g);
+  count_launch();
+  return TSV_OK;
+}
+
+}  // namespace
+
+int launch_attn_tc(const AttnArgs& a, int64_t units, cudaStream_t st) {
+  const int d = a.s.d;
+  if (!a.c.v)
+    return d <= 64 ? tc_launch<64, true>(a, units, st) : d <= 128 ? tc_launch<128, true>(a, units, st)
+         : d <= 256 ? tc_launch<256, true>(a, units, st) : tc_launch<512, true>(a, units, st);
+  return d <= 64 ? tc_launch<64, false>(a, units, st) : d <= 128 ? tc_launch<128, false>(a, units, st)
+       : d <= 256 ? tc_launch<256, false>(a, units, st) : tc_launch<512, false>(a, units, st);
+}
+
+}  // namespace tsv
