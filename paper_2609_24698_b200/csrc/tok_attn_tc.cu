@@ -3,8 +3,10 @@
 // A persistent CTA walks over work items (tile, key head, columns, share of the keys), warps by role:
 //   warps 0-3   softmax and epilogue, a row per thread
 //   warp 4      issues the products: S = Q K^T, then O += P V with P as the A operand straight from tensor memory
-//   warps 5-8   copy Q, K and V rows into shared memory (16-byte asynchronous copies: rows come from pages, a ring or the call's own
-//               tensors, any of them with strides of their own, which no tensor map describes)
+//   warp 5      finds the items ahead of the others: tile, keys, tree
+//   the others  copy Q, K and V rows into shared memory (16-byte asynchronous copies: rows come from pages, a ring or the call's own
+//               tensors, any of them with strides of their own, which no tensor map describes); a barrier counts a panel's copies as
+//               they land, and the thread that issues the products orders them before its reads (fence.proxy.async)
 // K and V live in panels of 128 rows x 64 columns (16 KiB, 128-byte swizzle): K row-major is the K-major operand of S, and the same
 // layout read MN-major the operand of P V, so that where the keys are the values one copy serves both products.
 //
@@ -25,10 +27,9 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = kTcTile;        // query rows of a tile, keys of a block
-constexpr int kMmaWarp = 4, kProducers = 128;      // (warps 0-3 before it)
-constexpr int kTcThreads = 288;
+constexpr int kMmaWarp = 4, kListWarp = 5;      // (softmax before them, producers behind)
 constexpr int kPanel = 16384;
-constexpr int kLag = 3;               // panels whose copies may be under way behind the one being requested
+constexpr int kItems = 3;             // items found ahead
 constexpr float kGap = 8.f;           // log2 units by which a maximum may exceed the row's reference
 constexpr int kCtl = 3072;
 
@@ -43,7 +44,20 @@ struct Cfg {
   static constexpr int SB = DP >= 256 ? 2 : 1;               // S buffers
   static constexpr int TM = DP >= 256 ? 512 : 256;           // tensor memory columns
   static constexpr int OCC = DP >= 256 ? 1 : 2;              // CTAs per SM
+  static constexpr int PW = DP >= 256 ? 4 : 2;               // producer warps (two of two CTAs: 16 warps per SM, 128 registers each)
+  static constexpr int THREADS = 32 * (6 + PW);
   static constexpr int SMEM = kCtl + (NP + NKS + NVB * VP) * kPanel;
+};
+
+// An item: tile, output columns, keys.  mode: 0 the first time; of those that left a mark then, 1 as before (which rows are not finite?)
+// and 2 with values that are not finite taken as zero.
+struct Item {
+  TileList t;
+  int64_t unit;
+  int half, split, k0, k1, nb, mode, li;
+  int missing;                        // a page of the list is not there
+  int depth[TSV_MAX_D];
+  uint32_t anc[TSV_MAX_D];
 };
 
 struct TcCtl {
@@ -51,12 +65,12 @@ struct TcCtl {
   uint64_t fullK[4], emptyK[4];
   uint64_t fullV[8], emptyV[4];
   uint64_t s_full[2], p_ready[2], pv_done, o_free;
+  uint64_t item_full[kItems], item_free[kItems];
   uint32_t tmem_base;
   uint32_t redo[32];                  // items with a result that is not finite, a bit each
-  int depth[9][TSV_MAX_D];            // of the item's tree, a copy per warp
-  uint32_t anc[9][TSV_MAX_D];
+  Item item[kItems];
 };
-static_assert(sizeof(TcCtl) + kTile * 2 <= kCtl, "control block overflow");
+static_assert(sizeof(TcCtl) <= kCtl, "control block overflow");
 
 __device__ __forceinline__ void bar_init(uint64_t* b, int count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
@@ -64,11 +78,11 @@ __device__ __forceinline__ void bar_init(uint64_t* b, int count) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
 }
-__device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
-  return ok != 0;
+// An arrival of this thread when its copies so far have landed.
+__device__ __forceinline__ void bar_arrive_copied(uint64_t* b) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
 }
+__device__ __forceinline__ void fence_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc) : "memory");
@@ -85,7 +99,7 @@ struct TcArgs {
 };
 
 template <int DP, bool SHARED>
-__global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_kernel(const __grid_constant__ TcArgs g) {
+__global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::OCC)) attn_tc_kernel(const __grid_constant__ TcArgs g) {
   typedef Cfg<DP, SHARED> C;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const AttnArgs& a = g.a;
@@ -95,8 +109,9 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
   if (tid == 0) {
-    for (int i = 0; i < 8; ++i) { bar_init(&sm.fullQ[i], kProducers); bar_init(&sm.fullV[i], kProducers); }
-    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullK[i], kProducers); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
+    for (int i = 0; i < 8; ++i) { bar_init(&sm.fullQ[i], 32 * C::PW); bar_init(&sm.fullV[i], 32 * C::PW); }
+    for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], 5 + C::PW); }
+    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullK[i], 32 * C::PW); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
     for (int i = 0; i < 2; ++i) { bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); }
     bar_init(&sm.emptyQ, 1); bar_init(&sm.pv_done, 1); bar_init(&sm.o_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -111,38 +126,23 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
   fence_after();
   const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + C::SB * kTile;
 
-  // An item's tile, columns and keys
-  struct Item { TileList t; int half, k0, k1, nb, split; int64_t unit; };
   auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !mbar_wait(b, parity)) fail = 1; };
-  // Calls body(item, mode) for this CTA's items (mode 0), then, for those that left a mark, twice more: computed as before, for which
-  // rows are not finite (1), then with values that are not finite taken as zero (2).
-  auto walk = [&](auto&& body, auto&& finish) {
+  // Calls body(item) for this CTA's items, as the list warp finds them, until it marks the end; then, where one has left a mark, for those.
+  auto walk = [&](auto&& body) {
+    uint32_t c = 0;
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {
-      int li = 0;
 #pragma unroll 1
-      for (int64_t idx = blockIdx.x; idx < g.items; idx += gridDim.x, ++li) {
-        if (round && !(sm.redo[(li >> 5) & 31] >> (li & 31) & 1u)) continue;
-        Item w;
-        w.half = (int)(idx % C::HALVES);
-        int64_t r = idx / C::HALVES;
-        const int hk = (int)(r % a.s.Hk);
-        r /= a.s.Hk;
-        w.split = (int)(r % a.nsplit);
-        w.unit = r / a.nsplit;
-        w.t = make_list(a, w.unit, hk, kTile, sm.depth[warp], sm.anc[warp]);
+      for (;; ++c) {
+        wait(&sm.item_full[c % kItems], c / kItems & 1);
+        if (__any_sync(0xffffffffu, fail)) { fail = 1; break; }     // (without its item a warp has nothing to go by)
+        const Item& w = sm.item[c % kItems];
+        const bool end = w.t.ok == 0;
+        if (!end) body(w);
         __syncwarp();
-        if (!w.t.ok) break;
-        w.k0 = w.k1 = w.nb = 0;
-        if (w.t.ok == 1) {
-          const int blocks = (w.t.nk + kTile - 1) / kTile, per = (blocks + a.nsplit - 1) / a.nsplit;
-          w.k0 = min(w.t.nk, w.split * per * kTile);
-          w.k1 = min(w.t.nk, w.k0 + per * kTile);
-          w.nb = (w.k1 - w.k0 + kTile - 1) / kTile;
-        }
-        for (int mode = round; mode <= 2 * round; ++mode) body(w, mode, li);
+        if (lane == 0) bar_arrive(&sm.item_free[c % kItems]);
+        if (end) { ++c; break; }
       }
-      finish();                                                 // (before this role waits for the others)
       if (round == 0) {
         __syncthreads();
         uint32_t any = 0;
@@ -153,117 +153,167 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
   };
   auto rows_of_block = [&](const Item& w, int j) { return min(kTile, w.k1 - w.k0 - j * kTile); };
 
-  if (warp > kMmaWarp) {
-    // ------------------------------------------------------------------ producers
-    const int pt = tid - 32 * (kMmaWarp + 1), prow = pt >> 3, chunk = pt & 7;    // rows prow + 16 i, one 16-byte chunk of a panel
-    uint64_t* pend[kLag];
-    int np = 0;                                            // panels requested and not announced
-    auto announce = [&](int keep) {                        // those before the last `keep`
-      if (keep == 0) cp_wait<0>(); else cp_wait<kLag - 1>();
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      if (keep == 0) {
-#pragma unroll
-        for (int i = 0; i < kLag; ++i) if (i < np) bar_arrive(pend[i]);
-        np = 0;
-      } else {
-        bar_arrive(pend[0]);
-#pragma unroll
-        for (int i = 0; i + 1 < kLag; ++i) pend[i] = pend[i + 1];
-        --np;
+  if (warp == kListWarp) {
+    // ------------------------------------------------------------------ items
+    uint32_t c = 0;
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {
+      int li = 0;
+      int64_t idx = blockIdx.x;
+#pragma unroll 1
+      for (bool more = true; more; idx += gridDim.x, ++li) {
+        if (idx < g.items && round && !(sm.redo[(li >> 5) & 31] >> (li & 31) & 1u)) continue;
+        const int half = (int)(idx % C::HALVES);
+        int64_t r = idx / C::HALVES;
+        const int hk = (int)(r % a.s.Hk);
+        r /= a.s.Hk;
+        const int split = (int)(r % a.nsplit);
+        const int64_t unit = r / a.nsplit;
+#pragma unroll 1
+        for (int mode = round; more && mode <= 2 * round; ++mode, ++c) {
+          wait(&sm.item_free[c % kItems], (c / kItems & 1) ^ 1);
+          fail = __any_sync(0xffffffffu, fail);
+          Item& w = sm.item[c % kItems];
+          TileList t;
+          t.ok = 0;
+          if (idx < g.items && !fail) t = make_list(a, unit, hk, kTile, w.depth, w.anc);
+          more = t.ok != 0;
+          int k0 = 0, k1 = 0, nb = 0;
+          bool missing = false;
+          if (t.ok == 1) {
+            const int blocks = (t.nk + kTile - 1) / kTile, per = (blocks + a.nsplit - 1) / a.nsplit;
+            k0 = min(t.nk, split * per * kTile);
+            k1 = min(t.nk, k0 + per * kTile);
+            nb = (k1 - k0 + kTile - 1) / kTile;
+            if (a.c.page_table) {                          // the last position of the list in each of its pages
+              const int P = a.c.page_tokens, s1 = min(t.ns, t.L) - 1, w1 = min(t.L, t.lo + (t.nc - t.ns)) - 1;
+              for (int lp = lane; s1 >= 0 && lp <= s1 / P; lp += 32) missing |= tok_cache_row(a.c, a.s.window, a.s.n_sink, t.b, min(s1, lp * P + P - 1)) < 0;
+              for (int lp = t.lo / P + lane; w1 >= t.lo && lp <= w1 / P; lp += 32) missing |= tok_cache_row(a.c, a.s.window, a.s.n_sink, t.b, min(w1, lp * P + P - 1)) < 0;
+            }
+          }
+          missing = __any_sync(0xffffffffu, missing);
+          if (lane == 0) {
+            w.t = t; w.unit = unit; w.half = half; w.split = split; w.k0 = k0; w.k1 = k1; w.nb = nb; w.mode = mode; w.li = li; w.missing = missing;
+            if (missing) atomicOr(a.status + t.b, TSV_ST_PAGE);
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sm.item_full[c % kItems]);
+        }
       }
-    };
-    auto push = [&](uint64_t* b) {
-      cp_commit();
-#pragma unroll
-      for (int i = 0; i < kLag; ++i) if (i == np) pend[i] = b;
-      if (++np == kLag) announce(kLag - 1);
-    };
-    auto acquire = [&](uint64_t* b, uint32_t parity) {     // (nothing may stay unannounced while this waits: its release may depend on it)
-      if (np && !bar_test(b, parity)) announce(0);
-      wait(b, parity);
-    };
+      if (round == 0) {
+        __syncthreads();
+        uint32_t any = 0;
+        for (int i = 0; i < 32; ++i) any |= sm.redo[i];
+        if (!any || fail) break;
+      }
+    }
+  } else if (warp > kListWarp) {
+    // ------------------------------------------------------------------ producers
+    // A thread copies one 16-byte chunk of the rows prow + ROWS i of a panel; where these rows are is worked out by the eight threads of
+    // a row together, a block ahead.
+    constexpr int ROWS = 4 * C::PW, PER = kTile / ROWS, EACH = PER / 8;
+    const int pt = tid - 32 * (kListWarp + 1), prow = pt >> 3, chunk = pt & 7;
     const int dch = a.s.d / 8;
     uint32_t cQ = 0, cK = 0, cV = 0;
-    const uint32_t off = (uint32_t)prow * 128 + ((chunk ^ (prow & 7)) << 4);     // (rows 16 apart: the same swizzle)
-    walk([&](const Item& w, int mode, int) {
-      if (w.nb == 0) return;
-      const bf16* ptr[8];
+    const uint32_t off = (uint32_t)prow * 128 + ((chunk ^ (prow & 7)) << 4);     // (the rows are multiples of 8 apart: the same swizzle)
+    walk([&](const Item& w) {
+      const int nb = w.nb;
+      if (nb == 0) return;
+      const int mode = w.mode, half = w.half, hk = w.t.hk;
+      // ptr: this thread's chunk in panel 0 of its rows (nullptr: nothing there)
+      auto panel = [&](uint32_t at, int rows, int pan, const bf16* const (&ptr)[PER]) {     // rows: a multiple of 16
+        const bool in = pan * 8 + chunk < dch;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = prow + 16 * i, gr = w.t.r0 + r;
-        ptr[i] = r < w.t.nr ? reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)w.t.hk * a.G + gr % a.G) * a.s.d : nullptr;
-      }
-      acquire(&sm.emptyQ, (cQ & 1) ^ 1);
-#pragma unroll 1
-      for (int p = 0; p < C::NP; ++p) {
-        // (in the order in which S takes them: the item's own output columns last where K is V)
-        const int pan = SHARED && C::KP ? (p + (w.half + 1) * C::VP) % C::NP : p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const bool live = ptr[i] && pan * 8 + chunk < dch;
-          cp16(q_at + p * kPanel + off + i * 2048, live ? (const void*)(ptr[i] + pan * 64 + chunk * 8) : a.in.q, live);
+        for (int i = 0; i < PER; ++i) {
+          if (ROWS * i >= rows) break;
+          const bool live = in && ptr[i];
+          cp16(at + off + i * ROWS * 128, live ? ptr[i] + pan * 64 : reinterpret_cast<const bf16*>(a.in.q), live);
         }
-        push(&sm.fullQ[p]);
-      }
-      ++cQ;
-#pragma unroll 1
-      for (int j = 0; j < w.nb; ++j) {
-        const int rows = rows_of_block(w, j), rows16 = (rows + 15) & ~15;
-        int64_t code[8];
+      };
+      // Rows of a block: a thread finds those of i = chunk, chunk + 8 and tells the others of its group, which have the same rows.
+      int64_t code[EACH];
+      auto find = [&](int j) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = prow + 16 * i;
-          code[i] = -1;
-          if (r < rows) {
-            code[i] = list_row(a, w.t, w.k0 + j * kTile + r);
-            if (code[i] == -1) atomicOr(a.status + w.t.b, TSV_ST_PAGE);
-          }
+        for (int e = 0; e < EACH; ++e) {
+          const int kk = w.k0 + j * kTile + prow + ROWS * (chunk + 8 * e);
+          code[e] = kk < w.k1 ? list_row(a, w.t, kk) : -1;
+        }
+      };
+      auto point = [&](bool value, const bf16* (&ptr)[PER]) {
+        unsigned long long mine[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) mine[e] = code[e] == -1 ? 0ull : reinterpret_cast<unsigned long long>(row_ptr<bf16>(a, hk, code[e], value));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const unsigned long long x = __shfl_sync(0xffffffffu, mine[i / 8], (lane & ~7) | (i & 7));
+          ptr[i] = x ? reinterpret_cast<const bf16*>(x) + chunk * 8 : nullptr;
+        }
+      };
+      const bf16* ptr[PER];
+      const bf16* vptr[PER];
+      {
+        unsigned long long mine[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+          const int r = prow + ROWS * (chunk + 8 * e), gr = w.t.r0 + r;
+          mine[e] = r < w.t.nr ? reinterpret_cast<unsigned long long>(reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)hk * a.G + gr % a.G) * a.s.d) : 0ull;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ptr[i] = code[i] == -1 ? nullptr : row_ptr<bf16>(a, w.t.hk, code[i], false);
-        auto panel = [&](uint32_t at, int pan) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (16 * i >= rows16) break;
-            const bool live = ptr[i] && pan * 8 + chunk < dch;
-            cp16(at + off + i * 2048, live ? (const void*)(ptr[i] + pan * 64 + chunk * 8) : a.in.q, live);
-          }
-        };
+        for (int i = 0; i < PER; ++i) {
+          const unsigned long long x = __shfl_sync(0xffffffffu, mine[i / 8], (lane & ~7) | (i & 7));
+          ptr[i] = x ? reinterpret_cast<const bf16*>(x) + chunk * 8 : nullptr;
+        }
+        wait(&sm.emptyQ, (cQ & 1) ^ 1);
+#pragma unroll 1
+        for (int p = 0; p < C::NP; ++p) {
+          // (in the order in which S takes them: the item's own output columns last where K is V)
+          panel(q_at + p * kPanel, kTile, SHARED && C::KP ? (p + (half + 1) * C::VP) % C::NP : p, ptr);
+          bar_arrive_copied(&sm.fullQ[p]);
+        }
+        ++cQ;
+      }
+      find(0);
+#pragma unroll 1
+      for (int j = 0; j < nb; ++j) {
+        const int rows16 = (rows_of_block(w, j) + 15) & ~15;
+        point(false, ptr);
+        if (!SHARED) point(true, vptr);
+        if (j + 1 < nb) find(j + 1);
 #pragma unroll 1
         for (int p = 0; p < C::KP; ++p) {
           const int slot = cK % (C::NKS ? C::NKS : 1);
-          acquire(&sm.emptyK[slot], (cK / (C::NKS ? C::NKS : 1) & 1) ^ 1);
-          panel(k_at + slot * kPanel, SHARED ? (p + (w.half + 1) * C::VP) % C::NP : p);
-          push(&sm.fullK[slot]);
+          wait(&sm.emptyK[slot], (cK / (C::NKS ? C::NKS : 1) & 1) ^ 1);
+          panel(k_at + slot * kPanel, rows16, SHARED ? (p + (half + 1) * C::VP) % C::NP : p, ptr);
+          bar_arrive_copied(&sm.fullK[slot]);
           ++cK;
         }
         const int buf = cV % C::NVB;
-        if (!SHARED) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) ptr[i] = code[i] == -1 ? nullptr : row_ptr<bf16>(a, w.t.hk, code[i], true);
-        }
-        acquire(&sm.emptyV[buf], (cV / C::NVB & 1) ^ 1);
+        wait(&sm.emptyV[buf], (cV / C::NVB & 1) ^ 1);
 #pragma unroll 1
         for (int p = 0; p < C::VP; ++p) {
           const uint32_t at = v_at + (buf * C::VP + p) * kPanel;
-          panel(at, w.half * C::VP + p);
+          panel(at, rows16, half * C::VP + p, SHARED ? ptr : vptr);
           if (mode == 2) {
             cp_commit();
             cp_wait<0>();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (16 * i < rows16) make_finite<bf16>(smem_raw + (at + off + i * 2048 - smem_u32(smem_raw)));
+            for (int i = 0; i < PER; ++i) if (ROWS * i < rows16) make_finite<bf16>(smem_raw + (at + off + i * ROWS * 128 - smem_u32(smem_raw)));
+            bar_arrive(&sm.fullV[buf * C::VP + p]);
+          } else {
+            bar_arrive_copied(&sm.fullV[buf * C::VP + p]);
           }
-          push(&sm.fullV[buf * C::VP + p]);
         }
         ++cV;
       }
-    }, [&]() { if (np) announce(0); });
+    });
+    cp_commit();
+    cp_wait<0>();
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------------ products
     const uint32_t idesc_v = make_idesc(C::OC, 1);
     uint32_t cQ = 0, cK = 0, cVs = 0, cVo = 0, cS = 0, cP = 0;     // uses so far: Q, K panels, V buffers by S and by O, S and P
     const bool one = lane == 0;
-    walk([&](const Item& w, int, int) {
+    walk([&](const Item& w) {
       if (w.nb == 0) return;
       auto scores = [&](int j, int p0, int p1) {           // panels p0 .. p1 - 1 of block j
         const uint32_t idesc = make_idesc((rows_of_block(w, j) + 15) & ~15, 0);
@@ -281,6 +331,7 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
             wait(&sm.fullV[buf * C::VP + p - C::KP], cVs / C::NVB & 1);
             at = v_at + (buf * C::VP + p - C::KP) * kPanel;
           }
+          fence_proxy();
           fence_after();
           if (one) {
             const uint64_t qd = make_desc(q_at + p * kPanel, 16, 1024), kd = make_desc(at, 16, 1024);
@@ -306,6 +357,7 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
           for (int p = 0; p < C::VP; ++p) wait(&sm.fullV[buf * C::VP + p], cVo / C::NVB & 1);
         if (j == 0) wait(&sm.o_free, (cQ & 1) ^ 1);
         wait(&sm.p_ready[sb], cP / C::SB & 1);
+        fence_proxy();
         fence_after();
         const int steps = (rows_of_block(w, j) + 15) / 16;
         if (one) {
@@ -327,7 +379,7 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
         if (AHEAD < C::NP && j + 1 < w.nb) scores(j + 1, AHEAD, C::NP);
       }
       ++cQ;
-    }, []() {});
+    });
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
     const uint32_t lane_at = (uint32_t)(warp * 32) << 16;
@@ -336,7 +388,8 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
     // (one by one, each before the P of the block after the next is announced: a parity says no more than the last phase)
     auto wait_pv = [&](uint32_t blocks) { for (; cW != blocks; ++cW) wait(&sm.pv_done, cW & 1); fence_after(); };
     bool bad = false;                                      // of mode 1, for mode 2
-    walk([&](const Item& w, int mode, int li) {
+    walk([&](const Item& w) {
+      const int mode = w.mode, li = w.li;
       const TileList& t = w.t;
       const size_t part = ((size_t)(w.unit * a.s.Hk + t.hk) * a.nsplit + w.split) * kTile + row;
       const bool live = row < t.nr, lead = w.half == 0;
@@ -355,9 +408,9 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
       // what this row sees of the list: positions kmin .. kmax and those below ksink, nodes
       const int tok = (t.r0 + (live ? row : 0)) / a.G;
       const bool tree = a.bt.parent != nullptr;
-      const int* depth = sm.depth[warp];
+      const int* depth = w.depth;
       const int p = t.L + (tree ? depth[tok] : tok);
-      const uint32_t an = tree ? sm.anc[warp][tok] : 0;
+      const uint32_t an = tree ? w.anc[tok] : 0;
       const int shift = t.ns - t.lo;                       // index of a position of the window part, less the position
       const int kmin = p - a.s.window + 1 + shift, kmax = tree ? t.nc - 1 : p + shift;
       const int ksink = max(t.ns, min(a.s.n_sink, t.nk) + shift);
@@ -365,14 +418,7 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
       if (tree)
         for (int j = 0; j < t.n; ++j)
           if ((an >> j & 1u) && (t.L + depth[j] > p - a.s.window || t.L + depth[j] < a.s.n_sink)) nodes |= 1u << j;
-      // pages that are not there
-      bool missing = false;
-      if (a.c.page_table) {
-        const int P = a.c.page_tokens, hi = min(t.L, t.lo + (t.nc - t.ns)) - 1;
-        for (int lp = lane; lp <= (t.ns - 1) / P && lp * P < min(t.ns, t.L); lp += 32) missing |= tok_cache_row(a.c, a.s.window, a.s.n_sink, t.b, min(min(t.ns, t.L) - 1, lp * P + P - 1)) < 0;
-        for (int lp = t.lo / P + lane; lp <= hi / P && t.lo <= hi; lp += 32) missing |= tok_cache_row(a.c, a.s.window, a.s.n_sink, t.b, min(hi, lp * P + P - 1)) < 0;
-        missing = __any_sync(0xffffffffu, missing);
-      }
+      const bool missing = w.missing != 0;
       auto visible = [&](int c0) {                         // keys c0 .. c0 + 31 of the list, a bit each
         uint32_t m = bits(max(kmin, 0) - c0, min(kmax + 1, t.nc) - c0) | bits(-c0, min(min(ksink, kmax + 1), t.nc) - c0);
         if (tree) {
@@ -555,7 +601,7 @@ __global__ void __launch_bounds__(kTcThreads, (Cfg<DP, SHARED>::OCC)) attn_tc_ke
           if (a.nsplit > 1 && lead && lane == 0) a.pml[pa] = make_float2(m, ls);
         }
       }
-    }, []() {});
+    });
   }
   if (__any_sync(0xffffffffu, fail)) for (int b = lane; b < a.s.B; b += 32) atomicOr(a.status + b, TSV_ST_INTERNAL);   // (an internal error: every sequence is flagged)
   fence_before();
@@ -572,7 +618,7 @@ int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
   if (!ensure_smem((const void*)attn_tc_kernel<DP, SHARED>, C::SMEM)) return TSV_ERR_CUDA;
   TSV_PREP((attn_tc_kernel<DP, SHARED>));
   const int64_t grid = g.items < 148 * C::OCC ? g.items : 148 * C::OCC;
-  attn_tc_kernel<DP, SHARED><<<(unsigned)grid, kTcThreads, C::SMEM, st>>>(g);
+  attn_tc_kernel<DP, SHARED><<<(unsigned)grid, C::THREADS, C::SMEM, st>>>(g);
   count_launch();
   return TSV_OK;
 }
