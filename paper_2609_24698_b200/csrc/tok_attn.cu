@@ -555,13 +555,13 @@ struct AttnPlan {
 bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s.max_n * (s.H / s.Hk) >= 48; }
 
 // Tiles and CTAs that splitting the keys aims at: those that run at a time.
-int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? tc_slots(s.d) / tc_halves(s.d) : 2 * 148; }
+int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? 148 / tc_halves(s.d) : 2 * 148; }
 
 // Keys are split where the tiles alone would leave SMs without work, into shares of some blocks of keys each.
 AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   AttnPlan p;
   p.tc = takes_tc(s);
-  p.per = p.tc ? kTcTile : kRows;
+  p.per = p.tc ? tc_tile(s.d) : kRows;
   p.tiles = tok_units_bound(s, rows, s.H / s.Hk, p.per);
   const int64_t ctas = p.tiles * s.Hk;
   int64_t reach = (int64_t)s.window + s.max_n;

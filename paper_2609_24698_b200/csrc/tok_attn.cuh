@@ -24,11 +24,10 @@ struct AttnArgs {
   int32_t* status;
 };
 
-// The tensor-core path (tok_attn_tc.cu): tiles of 128 rows.  `units`: tiles over all sequences (a bound); columns of a CTA.
+// The tensor-core path (tok_attn_tc.cu).  `units`: tiles over all sequences (a bound), of tc_tile rows; tc_halves CTAs share one's columns.
 int launch_attn_tc(const AttnArgs& a, int64_t units, cudaStream_t st);
-constexpr int kTcTile = 128;
+inline int tc_tile(int d) { return d > 128 ? 128 : 256; }
 inline int tc_halves(int d) { return d > 256 ? 2 : 1; }
-inline int tc_slots(int d) { return d > 128 ? 148 : 2 * 148; }      // CTAs that run at a time
 
 struct TileList {
   int b, n, L, G;

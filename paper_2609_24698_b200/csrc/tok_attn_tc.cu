@@ -1,21 +1,25 @@
-// window_sink_attn on the tensor cores (tcgen05), bf16: tiles of 128 query rows of one sequence and key head.
+// window_sink_attn on the tensor cores (tcgen05), bf16: tiles of 128 query rows of one sequence and key head, two at a time up to d = 128.
 //
-// A persistent CTA walks over work items (tile, key head, columns, share of the keys), warps by role:
-//   warps 0-3   softmax and epilogue, a row per thread
-//   warp 4      issues the products: S = Q K^T, then O += P V with P as the A operand straight from tensor memory
-//   warp 5      finds the items ahead of the others: tile, keys, tree
-//   the others  copy Q, K and V rows into shared memory (16-byte asynchronous copies: rows come from pages, a ring or the call's own
-//               tensors, any of them with strides of their own, which no tensor map describes); a barrier counts a panel's copies as
-//               they land, and the thread that issues the products orders them before its reads (fence.proxy.async)
+// A persistent CTA per SM walks over work items (one or two tiles, key head, columns, share of the keys), warps by role:
+//   warps 0-3    softmax of the first tile, a row per thread
+//   warps 4-7    softmax of the second tile; where there is one tile, its epilogue, under the next item's scores and softmax
+//   warp 8       issues the products: S = Q K^T, then O += P V with P as the A operand straight from tensor memory
+//   warp 9       finds the items ahead of the others: tile, keys, tree
+//   warps 10-13  copy Q, K and V rows into shared memory (16-byte asynchronous copies: rows come from pages, a ring or the call's own
+//                tensors, any of them with strides of their own, which no tensor map describes); a barrier counts a panel's copies as
+//                they land, and the thread that issues the products orders them before its reads (fence.proxy.async)
 // K and V live in panels of 128 rows x 64 columns (16 KiB, 128-byte swizzle): K row-major is the K-major operand of S, and the same
-// layout read MN-major the operand of P V, so that where the keys are the values one copy serves both products.
+// layout read MN-major the operand of P V, so that where the keys are the values one copy serves both products.  Two tiles share a
+// block of K and V: copies (half of the shared-memory traffic of a tile) and their instructions per product halve, and one tile's
+// softmax runs under the other's products.
 //
-// Tensor memory: S (128 columns, two buffers where a CTA has the SM to itself) and O.  P (bf16) overlays the S it came from.  d = 512 has
-// no room for S beside all of O (512 columns): two CTAs take 256 output columns each and compute S and the softmax alike.  Up to
-// d = 128, 256 columns and at most 96 KiB let two CTAs share an SM: one's softmax runs under the other's products.
+// Tensor memory: two buffers of S (128 columns; of the two tiles, or of two blocks of the one) and O.  P (bf16) overlays the S it came
+// from.  d = 512 has no room for S beside all of O (512 columns): two CTAs take 256 output columns each and compute S and the softmax
+// alike.
 //
-// Softmax: a block of 128 keys at a time.  Its row maximum becomes the row's reference only where it exceeds the old one by more than 2^8
-// (bf16 and fp32 have the range for weights above one): then O and the sum are rescaled, nearly never after the first block.
+// Softmax: S is read once, in slabs of 32 keys.  The row's reference is its first maximum, rounded up to a whole power of two; it moves
+// where a later slab exceeds it by more than 2^10 (bf16 and fp32 have the range for weights above one), and then what is there of
+// P, the sum and O are multiplied by a power of two, exactly.  Nearly never after the first slab.
 // P is rounded to bf16 for the product (2^-9 of a weight); scores, sums and O are fp32.
 #include "tc_common.cuh"
 #include "tok_attn.cuh"
@@ -26,27 +30,23 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = kTcTile;        // query rows of a tile, keys of a block
-constexpr int kMmaWarp = 4, kListWarp = 5;      // (softmax before them, producers behind)
+constexpr int kTile = 128;            // query rows of a tile, keys of a block
+constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 4, kTcThreads = 32 * (10 + kCopyWarps);
 constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
-constexpr float kGap = 8.f;           // log2 units by which a maximum may exceed the row's reference
+constexpr float kGap = 10.f;          // log2 units by which a maximum may exceed the row's reference
 constexpr int kCtl = 3072;
 
 template <int DP, bool SHARED>
 struct Cfg {
+  static constexpr int NT = DP <= 128 ? 2 : 1;               // tiles of an item
   static constexpr int OC = DP < 256 ? DP : 256;             // output columns of an item
   static constexpr int HALVES = DP / OC;
   static constexpr int NP = DP / 64, VP = OC / 64;           // panels of all of d, of the output columns
   static constexpr int KP = SHARED ? NP - VP : NP;           // panels that only S reads
-  static constexpr int NKS = KP == 0 ? 0 : DP == 256 ? 4 : 2;          // ring of those
-  static constexpr int NVB = DP == 64 ? (SHARED ? 4 : 2) : SHARED && DP <= 256 ? 2 : 1;   // buffers of the others, VP panels each
-  static constexpr int SB = DP >= 256 ? 2 : 1;               // S buffers
-  static constexpr int TM = DP >= 256 ? 512 : 256;           // tensor memory columns
-  static constexpr int OCC = DP >= 256 ? 1 : 2;              // CTAs per SM
-  static constexpr int PW = DP >= 256 ? 4 : 2;               // producer warps (two of two CTAs: 16 warps per SM, 128 registers each)
-  static constexpr int THREADS = 32 * (6 + PW);
-  static constexpr int SMEM = kCtl + (NP + NKS + NVB * VP) * kPanel;
+  static constexpr int NKS = KP == 0 ? 0 : DP == 512 ? 2 : 4;          // ring of those
+  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : SHARED && DP == 256 ? 2 : 1;   // buffers of the others, VP panels each
+  static constexpr int SMEM = kCtl + (NT * NP + NKS + NVB * VP) * kPanel;
 };
 
 // An item: tile, output columns, keys.  mode: 0 the first time; of those that left a mark then, 1 as before (which rows are not finite?)
@@ -54,7 +54,7 @@ struct Cfg {
 struct Item {
   TileList t;
   int64_t unit;
-  int half, split, k0, k1, nb, mode, li;
+  int half, split, k0, k1, nb, nt, mode, li;
   int missing;                        // a page of the list is not there
   int depth[TSV_MAX_D];
   uint32_t anc[TSV_MAX_D];
@@ -64,10 +64,12 @@ struct TcCtl {
   uint64_t fullQ[8], emptyQ;
   uint64_t fullK[4], emptyK[4];
   uint64_t fullV[8], emptyV[4];
-  uint64_t s_full[2], p_ready[2], pv_done, o_free;
+  uint64_t s_full[2], p_ready[2], pv_done[2], o_free[2];
+  uint64_t o_full, stat_full, stat_free;      // one tile: O is complete; reference and sum of its rows, for the epilogue
   uint64_t item_full[kItems], item_free[kItems];
   uint32_t tmem_base;
   uint32_t redo[32];                  // items with a result that is not finite, a bit each
+  float2 stat[kTile];
   Item item[kItems];
 };
 static_assert(sizeof(TcCtl) <= kCtl, "control block overflow");
@@ -93,38 +95,67 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
   return lo >= hi ? 0u : (0xffffffffu << lo) & (0xffffffffu >> (32 - hi));
 }
 
+// Two fp32 at a time.
+__device__ __forceinline__ uint64_t pair2(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// 2^x for a whole x <= 0, exactly (below the smallest normal number: 0).
+__device__ __forceinline__ float power_of_two(float x) {
+  const int e = (int)fmaxf(x, -127.f) + 127;
+  return __int_as_float(max(e, 0) << 23);
+}
+
 struct TcArgs {
   AttnArgs a;
   int64_t items;
 };
 
 template <int DP, bool SHARED>
-__global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::OCC)) attn_tc_kernel(const __grid_constant__ TcArgs g) {
+__global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_constant__ TcArgs g) {
   typedef Cfg<DP, SHARED> C;
+  constexpr int NT = C::NT;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const AttnArgs& a = g.a;
   TcCtl& sm = *reinterpret_cast<TcCtl*>(smem_raw);
   const uint32_t base = smem_u32(smem_raw) + kCtl;
-  const uint32_t q_at = base, k_at = q_at + C::NP * kPanel, v_at = k_at + C::NKS * kPanel;
+  const uint32_t q_at = base, k_at = q_at + NT * C::NP * kPanel, v_at = k_at + C::NKS * kPanel;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
   if (tid == 0) {
-    for (int i = 0; i < 8; ++i) { bar_init(&sm.fullQ[i], 32 * C::PW); bar_init(&sm.fullV[i], 32 * C::PW); }
-    for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], 5 + C::PW); }
-    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullK[i], 32 * C::PW); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
-    for (int i = 0; i < 2; ++i) { bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); }
-    bar_init(&sm.emptyQ, 1); bar_init(&sm.pv_done, 1); bar_init(&sm.o_free, kTile);
+    for (int i = 0; i < 8; ++i) { bar_init(&sm.fullQ[i], 32 * kCopyWarps); bar_init(&sm.fullV[i], 32 * kCopyWarps); }
+    for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], 9 + kCopyWarps); }
+    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullK[i], 32 * kCopyWarps); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
+    for (int i = 0; i < 2; ++i) { bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.pv_done[i], 1); bar_init(&sm.o_free[i], kTile); }
+    bar_init(&sm.emptyQ, 1); bar_init(&sm.o_full, 1); bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid < 32) sm.redo[tid] = 0;
   if (warp == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem_base)), "n"(C::TM) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + C::SB * kTile;
+  const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + 2 * kTile;
 
   auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !mbar_wait(b, parity)) fail = 1; };
   // Calls body(item) for this CTA's items, as the list warp finds them, until it marks the end; then, where one has left a mark, for those.
@@ -176,7 +207,7 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
           Item& w = sm.item[c % kItems];
           TileList t;
           t.ok = 0;
-          if (idx < g.items && !fail) t = make_list(a, unit, hk, kTile, w.depth, w.anc);
+          if (idx < g.items && !fail) t = make_list(a, unit, hk, NT * kTile, w.depth, w.anc);
           more = t.ok != 0;
           int k0 = 0, k1 = 0, nb = 0;
           bool missing = false;
@@ -193,7 +224,7 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
           }
           missing = __any_sync(0xffffffffu, missing);
           if (lane == 0) {
-            w.t = t; w.unit = unit; w.half = half; w.split = split; w.k0 = k0; w.k1 = k1; w.nb = nb; w.mode = mode; w.li = li; w.missing = missing;
+            w.t = t; w.unit = unit; w.half = half; w.split = split; w.k0 = k0; w.k1 = k1; w.nb = nb; w.nt = t.ok && t.nr > kTile ? 2 : 1; w.mode = mode; w.li = li; w.missing = missing;
             if (missing) atomicOr(a.status + t.b, TSV_ST_PAGE);
           }
           __syncwarp();
@@ -211,7 +242,7 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
     // ------------------------------------------------------------------ producers
     // A thread copies one 16-byte chunk of the rows prow + ROWS i of a panel; where these rows are is worked out by the eight threads of
     // a row together, a block ahead.
-    constexpr int ROWS = 4 * C::PW, PER = kTile / ROWS, EACH = PER / 8;
+    constexpr int ROWS = 4 * kCopyWarps, PER = kTile / ROWS, EACH = PER / 8;
     const int pt = tid - 32 * (kListWarp + 1), prow = pt >> 3, chunk = pt & 7;
     const int dch = a.s.d / 8;
     uint32_t cQ = 0, cK = 0, cV = 0;
@@ -251,11 +282,13 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
       };
       const bf16* ptr[PER];
       const bf16* vptr[PER];
-      {
+      wait(&sm.emptyQ, (cQ & 1) ^ 1);
+#pragma unroll 1
+      for (int tile = 0; tile < w.nt; ++tile) {
         unsigned long long mine[EACH];
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-          const int r = prow + ROWS * (chunk + 8 * e), gr = w.t.r0 + r;
+          const int r = tile * kTile + prow + ROWS * (chunk + 8 * e), gr = w.t.r0 + r;
           mine[e] = r < w.t.nr ? reinterpret_cast<unsigned long long>(reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)hk * a.G + gr % a.G) * a.s.d) : 0ull;
         }
 #pragma unroll
@@ -263,15 +296,14 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
           const unsigned long long x = __shfl_sync(0xffffffffu, mine[i / 8], (lane & ~7) | (i & 7));
           ptr[i] = x ? reinterpret_cast<const bf16*>(x) + chunk * 8 : nullptr;
         }
-        wait(&sm.emptyQ, (cQ & 1) ^ 1);
 #pragma unroll 1
         for (int p = 0; p < C::NP; ++p) {
           // (in the order in which S takes them: the item's own output columns last where K is V)
-          panel(q_at + p * kPanel, kTile, SHARED && C::KP ? (p + (half + 1) * C::VP) % C::NP : p, ptr);
-          bar_arrive_copied(&sm.fullQ[p]);
+          panel(q_at + (tile * C::NP + p) * kPanel, kTile, SHARED && C::KP ? (p + (half + 1) * C::VP) % C::NP : p, ptr);
+          bar_arrive_copied(&sm.fullQ[tile * C::NP + p]);
         }
-        ++cQ;
       }
+      ++cQ;
       find(0);
 #pragma unroll 1
       for (int j = 0; j < nb; ++j) {
@@ -311,20 +343,24 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------------ products
     const uint32_t idesc_v = make_idesc(C::OC, 1);
-    uint32_t cQ = 0, cK = 0, cVs = 0, cVo = 0, cS = 0, cP = 0;     // uses so far: Q, K panels, V buffers by S and by O, S and P
+    uint32_t cK = 0, cVs = 0, cVo = 0;                     // uses so far: K panels, V buffers by S and by O
+    uint32_t cS = 0, par_q = 0, par_p = 0, par_o = 3;      // blocks' scores; parities of a tile's fullQ and o_free, of p_ready
     const bool one = lane == 0;
     walk([&](const Item& w) {
-      if (w.nb == 0) return;
-      auto scores = [&](int j, int p0, int p1) {           // panels p0 .. p1 - 1 of block j
-        const uint32_t idesc = make_idesc((rows_of_block(w, j) + 15) & ~15, 0);
-        const uint32_t dst = s_col + (cS % C::SB) * kTile;
+      const int nb = w.nb, nt = NT == 2 ? w.nt : 1;
+      if (nb == 0) return;
+      const int k_all = w.k1 - w.k0;
+      // scores of panels p0 .. p1 - 1 of block j and tile t, into S buffer x
+      auto scores = [&](int j, int t, int x, int p0, int p1) {
+        const uint32_t idesc = make_idesc((min(kTile, k_all - j * kTile) + 15) & ~15, 0), dst = s_col + x * kTile;
+        const bool last = t == nt - 1;
         for (int p = p0; p < p1; ++p) {
-          if (j == 0) wait(&sm.fullQ[p], cQ & 1);
-          uint32_t at;
+          if (j == 0) wait(&sm.fullQ[t * C::NP + p], par_q >> t & 1);
           const bool ring = p < C::KP;
-          const int slot = cK % (C::NKS ? C::NKS : 1);
+          const uint32_t kp = cK + p, slot = kp % (C::NKS ? C::NKS : 1);
+          uint32_t at;
           if (ring) {
-            wait(&sm.fullK[slot], cK / (C::NKS ? C::NKS : 1) & 1);
+            wait(&sm.fullK[slot], kp / (C::NKS ? C::NKS : 1) & 1);
             at = k_at + slot * kPanel;
           } else {
             const int buf = cVs % C::NVB;
@@ -334,210 +370,134 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
           fence_proxy();
           fence_after();
           if (one) {
-            const uint64_t qd = make_desc(q_at + p * kPanel, 16, 1024), kd = make_desc(at, 16, 1024);
+            const uint64_t qd = make_desc(q_at + (t * C::NP + p) * kPanel, 16, 1024), kd = make_desc(at, 16, 1024);
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) mma_ss(dst, qd + 2 * ks, kd + 2 * ks, idesc, (p | ks) != 0);
-            if (ring) mma_commit(&sm.emptyK[slot]);
+            if (ring && last) mma_commit(&sm.emptyK[slot]);
           }
           __syncwarp();
-          if (ring) ++cK;
         }
         if (p1 < C::NP) return;
         if (one) {
-          mma_commit(&sm.s_full[cS % C::SB]);
-          if (j == w.nb - 1) mma_commit(&sm.emptyQ);
+          mma_commit(&sm.s_full[x]);
+          if (last && j == nb - 1) mma_commit(&sm.emptyQ);
         }
         __syncwarp();
-        ++cS;
-        if (SHARED) ++cVs;
+        if (last) { cK += C::KP; ++cVs; ++cS; }
       };
-      auto output = [&](int j) {
-        const int buf = cVo % C::NVB, sb = cP % C::SB;
+      auto output = [&](int j, int t, int x) {
+        const int buf = cVo % C::NVB;
+        const bool last = t == nt - 1;
         if (!SHARED)
           for (int p = 0; p < C::VP; ++p) wait(&sm.fullV[buf * C::VP + p], cVo / C::NVB & 1);
-        if (j == 0) wait(&sm.o_free, (cQ & 1) ^ 1);
-        wait(&sm.p_ready[sb], cP / C::SB & 1);
+        if (j == 0) { wait(&sm.o_free[t], par_o >> t & 1); par_o ^= 1u << t; }
+        wait(&sm.p_ready[x], par_p >> x & 1);
+        par_p ^= 1u << x;
         fence_proxy();
         fence_after();
-        const int steps = (rows_of_block(w, j) + 15) / 16;
+        const int steps = (min(kTile, k_all - j * kTile) + 15) / 16;
         if (one) {
           const uint64_t vd = make_desc(v_at + buf * C::VP * kPanel, kPanel, 1024);
-          for (int ks = 0; ks < steps; ++ks) mma_ts(o_col, s_col + sb * kTile + ks * 8, vd + ks * (2048 >> 4), idesc_v, (j | ks) != 0);
-          mma_commit(&sm.emptyV[buf]);
-          mma_commit(&sm.pv_done);
+          for (int ks = 0; ks < steps; ++ks) mma_ts(o_col + t * C::OC, s_col + x * kTile + ks * 8, vd + ks * (2048 >> 4), idesc_v, (j | ks) != 0);
+          if (last) mma_commit(&sm.emptyV[buf]);
+          mma_commit(&sm.pv_done[t]);
+          if (NT == 1 && j == nb - 1) mma_commit(&sm.o_full);
         }
         __syncwarp();
-        ++cVo; ++cP;
+        if (last) ++cVo;
       };
-      // The scores of the next block under the softmax of this one, where there is a second buffer for them: all of them, or, where the
-      // panels that both products read have one buffer, those of the other panels.
-      constexpr int AHEAD = C::SB == 1 ? 0 : SHARED && C::NVB == 1 ? C::KP : C::NP;
-      scores(0, 0, C::NP);
-      for (int j = 0; j < w.nb; ++j) {
-        if (AHEAD && j + 1 < w.nb) scores(j + 1, 0, AHEAD);
-        output(j);
-        if (AHEAD < C::NP && j + 1 < w.nb) scores(j + 1, AHEAD, C::NP);
+      if (NT == 2) {
+        for (int t = 0; t < nt; ++t) scores(0, t, t, 0, C::NP);
+        for (int j = 0; j < nb; ++j)
+          for (int t = 0; t < nt; ++t) {
+            output(j, t, t);
+            if (j + 1 < nb) scores(j + 1, t, t, 0, C::NP);
+          }
+      } else {
+        // The scores of the next block under the softmax of this one: all of them, or, where the panels that both products read have one
+        // buffer, those of the other panels.
+        constexpr int AHEAD = SHARED && C::NVB == 1 ? C::KP : C::NP;
+        scores(0, 0, cS & 1, 0, C::NP);
+        for (int j = 0; j < nb; ++j) {
+          const int x = (cS - 1) & 1;                      // (of block j)
+          if (AHEAD && j + 1 < nb) scores(j + 1, 0, x ^ 1, 0, AHEAD);
+          output(j, 0, x);
+          if (AHEAD < C::NP && j + 1 < nb) scores(j + 1, 0, x ^ 1, AHEAD, C::NP);
+        }
       }
-      ++cQ;
+      par_q ^= nt == 2 ? 3u : 1u;                          // (an item of one tile does not use the other's)
     });
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
-    const uint32_t lane_at = (uint32_t)(warp * 32) << 16;
-    const int row = tid;
-    uint32_t cS = 0, cW = 0;                               // blocks so far; those whose P V is known to be complete
-    // (one by one, each before the P of the block after the next is announced: a parity says no more than the last phase)
-    auto wait_pv = [&](uint32_t blocks) { for (; cW != blocks; ++cW) wait(&sm.pv_done, cW & 1); fence_after(); };
-    bool bad = false;                                      // of mode 1, for mode 2
-    walk([&](const Item& w) {
-      const int mode = w.mode, li = w.li;
-      const TileList& t = w.t;
-      const size_t part = ((size_t)(w.unit * a.s.Hk + t.hk) * a.nsplit + w.split) * kTile + row;
-      const bool live = row < t.nr, lead = w.half == 0;
-      if (t.ok == 2) {                                     // (with the keys split: the join's)
-        if (mode == 0 && a.nsplit == 1 && live) {
-          const int gr = t.r0 + row;
-          uint4* o = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + (size_t)t.hk * a.G + gr % a.G) * a.s.d);
+    const int grp = warp >> 2, q4 = warp & 3;              // (a warp reaches the 32 lanes of tensor memory of its number modulo 4)
+    const uint32_t lane_at = (uint32_t)(q4 * 32) << 16;
+    const int tile = NT == 2 ? grp : 0, row = q4 * 32 + lane;
+    constexpr uint32_t FULL = 0xffffffffu;
+    auto out_at = [&](const TileList& t, int r) {          // (r: within the item)
+      const int gr = t.r0 + r;
+      return reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + (size_t)t.hk * a.G + gr % a.G) * a.s.d;
+    };
+    auto part_at = [&](const Item& w, int r) { return ((size_t)(w.unit * a.s.Hk + w.t.hk) * a.nsplit + w.split) * (NT * kTile) + r; };
+    auto position = [&](const Item& w, int r, uint32_t& an) {      // of row r; its ancestors
+      const int tok = (w.t.r0 + min(r, w.t.nr - 1)) / a.G;
+      an = a.bt.parent ? w.anc[tok] : 0;
+      return w.t.L + (a.bt.parent ? w.depth[tok] : tok);
+    };
+    // Rows without keys: zeros of a flagged sequence, or an empty share of split keys.
+    auto no_keys = [&](const Item& w) {
+      const int r = tile * kTile + row;
+      if (w.mode || r >= w.t.nr) return;
+      if (w.t.ok == 2) {                                   // (with the keys split: the join's)
+        uint4* o = reinterpret_cast<uint4*>(out_at(w.t, r));
+        if (a.nsplit == 1)
           for (int c = w.half * (C::OC / 8); c < min(a.s.d / 8, (w.half + 1) * (C::OC / 8)); ++c) o[c] = make_uint4(0, 0, 0, 0);
-        }
-        return;
+      } else if (w.half == 0) {
+        a.pml[part_at(w, r)] = make_float2(-INFINITY, 0.f);
       }
-      if (w.nb == 0) {                                     // (a share without keys: only where they are split)
-        if (mode == 0 && live && lead) a.pml[part] = make_float2(-INFINITY, 0.f);
-        return;
-      }
-      // what this row sees of the list: positions kmin .. kmax and those below ksink, nodes
-      const int tok = (t.r0 + (live ? row : 0)) / a.G;
-      const bool tree = a.bt.parent != nullptr;
-      const int* depth = w.depth;
-      const int p = t.L + (tree ? depth[tok] : tok);
-      const uint32_t an = tree ? w.anc[tok] : 0;
-      const int shift = t.ns - t.lo;                       // index of a position of the window part, less the position
-      const int kmin = p - a.s.window + 1 + shift, kmax = tree ? t.nc - 1 : p + shift;
-      const int ksink = max(t.ns, min(a.s.n_sink, t.nk) + shift);
-      uint32_t nodes = 0;
-      if (tree)
-        for (int j = 0; j < t.n; ++j)
-          if ((an >> j & 1u) && (t.L + depth[j] > p - a.s.window || t.L + depth[j] < a.s.n_sink)) nodes |= 1u << j;
-      const bool missing = w.missing != 0;
-      auto visible = [&](int c0) {                         // keys c0 .. c0 + 31 of the list, a bit each
-        uint32_t m = bits(max(kmin, 0) - c0, min(kmax + 1, t.nc) - c0) | bits(-c0, min(min(ksink, kmax + 1), t.nc) - c0);
-        if (tree) {
-          const int s = t.nc - c0;
-          if (s < 32 && s > -32) m |= s >= 0 ? nodes << s : nodes >> -s;
-        }
-        m &= bits(0, w.k1 - c0);
-        if (missing)
-          for (uint32_t x = m; x; x &= x - 1) { const int i = __ffs(x) - 1; if (list_row(a, t, c0 + i) == -1) m &= ~(1u << i); }
-        return m;
-      };
-      float ref = -INFINITY, l[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-      for (int j = 0; j < w.nb; ++j) {
-        const int sb = cS % C::SB, c0 = w.k0 + j * kTile, slabs = (rows_of_block(w, j) + 31) / 32;
-        const uint32_t scol = s_col + sb * kTile + lane_at;
-        wait(&sm.s_full[sb], cS / C::SB & 1);
-        fence_after();
-        uint32_t vis[4];
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i >= slabs) break;
-          vis[i] = visible(c0 + 32 * i);
-          uint32_t sv[32];
-          tmem_ld32(scol + 32 * i, sv);
-          if (__all_sync(0xffffffffu, vis[i] == 0xffffffffu)) {
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int e = 0; e < 32; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(sv[e]));
-            mx = fmaxf(mx, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) mx = fmaxf(mx, (vis[i] >> e & 1u) ? __uint_as_float(sv[e]) : -INFINITY);
-          }
-        }
-        mx *= a.scale2;
-        const bool up = mx > ref + kGap || (ref == -INFINITY && mx > ref);
-        if (__any_sync(0xffffffffu, up)) {
-          const float to = up ? mx : ref, f = up && ref != -INFINITY ? ex2(ref - to) : 1.f;
-          ref = to;
-          if (__any_sync(0xffffffffu, f != 1.f)) {         // (never in the first block)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) l[i] *= f;
-            if (j) {
-              wait_pv(cS);
-#pragma unroll 1
-              for (int c = 0; c < C::OC; c += 32) {
-                uint32_t r[32];
-                tmem_ld32(o_col + lane_at + c, r);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
-                tmem_st16(o_col + lane_at + c, r);
-                tmem_st16(o_col + lane_at + c + 16, r + 16);
-              }
-            }
-          }
-        }
-        const float neg = ref == -INFINITY ? 0.f : -ref;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i >= slabs) break;
-          uint32_t sv[32], pk[16];
-          tmem_ld32(scol + 32 * i, sv);
-          if (!__all_sync(0xffffffffu, vis[i] == 0xffffffffu)) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) if (!(vis[i] >> e & 1u)) sv[e] = 0xff800000u;
-          }
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const float p0 = ex2(fmaf(__uint_as_float(sv[e]), a.scale2, neg)), p1 = ex2(fmaf(__uint_as_float(sv[e + 1]), a.scale2, neg));
-            l[(e >> 1) & 3] += p0 + p1;
-            const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-            pk[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-          tmem_st16(scol + 16 * i, pk);
-        }
-        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        fence_before();
-        wait_pv(cS);
-        bar_arrive(&sm.p_ready[sb]);
-        ++cS;
-      }
-      // the output
-      const float sum = (l[0] + l[1]) + (l[2] + l[3]);
-      wait_pv(cS);
+    };
+    // O out of tensor memory; its rows' reference and sum are ref and sum.  bad: of mode 1, for mode 2.
+    bool bad = false;
+    auto epilogue = [&](const Item& w, float ref, float sum) {
+      const TileList& t = w.t;
+      const int mode = w.mode, rt = tile * kTile, r0 = rt + q4 * 32;
+      const bool live = rt + row < t.nr, lead = w.half == 0;
+      const uint32_t ocol = o_col + tile * C::OC + lane_at;
       bool odd = !is_finite(sum) || (ref == -INFINITY && a.nsplit == 1);
-      fail = __any_sync(0xffffffffu, fail);
-      const uint32_t ocol = o_col + lane_at;
       if (a.nsplit > 1) {
+        const size_t part = part_at(w, rt + row);
         float* po = a.po + part * a.s.d + w.half * C::OC;
+        float nz = 0.f;                                    // 0 x each value: NaN where one is not finite
 #pragma unroll 1
         for (int c = 0; c < C::OC; c += 32) {
           uint32_t r[32];
           tmem_ld32(ocol + c, r);
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
-            odd |= !(is_finite(__uint_as_float(r[e])) && is_finite(__uint_as_float(r[e + 1])) && is_finite(__uint_as_float(r[e + 2])) && is_finite(__uint_as_float(r[e + 3])));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) nz = fmaf(__uint_as_float(r[e + i]), 0.f, nz);
             if (live && mode != 1 && w.half * C::OC + c + e < a.s.d) *reinterpret_cast<uint4*>(po + c + e) = make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]);
           }
         }
+        odd |= !(nz == 0.f);
         if (live && lead && mode != 1) a.pml[part] = make_float2(ref, sum);
       } else {
         // read out so that four lanes share a row: they transpose their words, and a warp stores whole 128-byte lines of eight rows
         const float inv = 1.f / sum;
         const int quad = lane >> 2, qi = lane & 3;
+        const __nv_bfloat162 zero2 = __floats2bfloat162_rn(0.f, 0.f);
 #pragma unroll 1
         for (int hh = 0; hh < 2; ++hh) {
           float iv[2];
           bf16* o[2];
           bool okr[2];
+          __nv_bfloat162 nz[2] = {zero2, zero2};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int r = 16 * hh + 8 * h + quad, gr = t.r0 + warp * 32 + r;
-            iv[h] = __shfl_sync(0xffffffffu, inv, r);
-            okr[h] = warp * 32 + r < t.nr && mode != 1;
-            o[h] = reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + (size_t)t.hk * a.G + gr % a.G) * a.s.d + w.half * C::OC;
+            const int r = 16 * hh + 8 * h + quad;
+            iv[h] = __shfl_sync(FULL, inv, r);
+            okr[h] = r0 + r < t.nr && mode != 1;
+            o[h] = out_at(t, min(r0 + r, t.nr - 1)) + w.half * C::OC;
           }
-          bool bad_h[2] = {false, false};
 #pragma unroll 1
           for (int c = 0; c < C::OC; c += 64) {
             uint32_t r[32];
@@ -549,9 +509,8 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
               uint32_t wd[8];                             // words of 8-column groups g = 0 .. 7: columns 8 g + 2 qi, + 1
 #pragma unroll
               for (int gq = 0; gq < 8; ++gq) {
-                const float x = __uint_as_float(r[4 * gq + 2 * h]), y = __uint_as_float(r[4 * gq + 2 * h + 1]);
-                bad_h[h] |= !(is_finite(x) && is_finite(y));
-                const __nv_bfloat162 v = __floats2bfloat162_rn(x * iv[h], y * iv[h]);
+                const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[4 * gq + 2 * h]) * iv[h], __uint_as_float(r[4 * gq + 2 * h + 1]) * iv[h]);
+                nz[h] = __hfma2(v, zero2, nz[h]);
                 wd[gq] = *reinterpret_cast<const uint32_t*>(&v);
               }
 #pragma unroll
@@ -563,7 +522,7 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
 #pragma unroll
                   for (int i = 0; i < 4; ++i)
                     if (!(i & m)) {
-                      const uint32_t send = upper ? x[i] : x[i | m], got = __shfl_xor_sync(0xffffffffu, send, m);
+                      const uint32_t send = upper ? x[i] : x[i | m], got = __shfl_xor_sync(FULL, send, m);
                       if (upper) x[i] = got; else x[i | m] = got;
                     }
                 }
@@ -574,39 +533,190 @@ __global__ void __launch_bounds__((Cfg<DP, SHARED>::THREADS), (Cfg<DP, SHARED>::
           }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {                   // a row's four lanes to the row's thread
-            uint32_t b = __ballot_sync(0xffffffffu, bad_h[h]);
+            const float2 z = __bfloat1622float2(nz[h]);
+            const uint32_t b = __ballot_sync(FULL, !(z.x == 0.f && z.y == 0.f));
             if (lane >= 16 * hh + 8 * h && lane < 16 * hh + 8 * h + 8) odd |= (b >> (4 * (lane & 7)) & 15u) != 0;
           }
         }
       }
       fence_before();
-      bar_arrive(&sm.o_free);
+      bar_arrive(&sm.o_free[tile]);
       odd = odd && live;
-      if (mode == 0 && odd) atomicOr(&sm.redo[(li >> 5) & 31], 1u << (li & 31));
+      if (mode == 0 && odd) atomicOr(&sm.redo[(w.li >> 5) & 31], 1u << (w.li & 31));
       if (mode == 1) bad = odd;
       if (mode == 2) {
-        for (uint32_t todo = __ballot_sync(0xffffffffu, bad); todo; todo &= todo - 1) {
-          const int r = __ffs(todo) - 1, gr = t.r0 + warp * 32 + r, pr = __shfl_sync(0xffffffffu, p, r);
-          const uint32_t ar = __shfl_sync(0xffffffffu, an, r);
-          const size_t at = (size_t)t.hk * a.G + gr % a.G;
+        uint32_t an;
+        const int p = position(w, rt + row, an);
+        for (uint32_t todo = __ballot_sync(FULL, bad); todo; todo &= todo - 1) {
+          const int x = __ffs(todo) - 1, gr = t.r0 + r0 + x, pr = __shfl_sync(FULL, p, x);
+          const uint32_t ar = __shfl_sync(FULL, an, x);
+          const bf16* q = reinterpret_cast<const bf16*>(a.in.q) + (t.row0 + gr / a.G) * a.in.q_ld + ((size_t)t.hk * a.G + gr % a.G) * a.s.d;
           float m, ls, ov[16];
-          if (!exact_row<bf16>(a, t, depth, reinterpret_cast<const bf16*>(a.in.q) + (t.row0 + gr / a.G) * a.in.q_ld + at * a.s.d, pr, ar, w.k0, w.k1, m, ls, ov)) continue;
-          const size_t pa = part - row + warp * 32 + r;
-          bf16* o = reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + at) * a.s.d;
-          for (int i = w.half * (C::OC / 32); i < 16 && i < (w.half + 1) * (C::OC / 32); ++i) {
+          if (!exact_row<bf16>(a, t, w.depth, q, pr, ar, w.k0, w.k1, m, ls, ov)) continue;
+          const size_t pa = part_at(w, r0 + x);
+          bf16* o = out_at(t, r0 + x);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
             const int col = lane + 32 * i;
-            if (col >= a.s.d) continue;
+            if (col >= a.s.d || col < w.half * C::OC || col >= (w.half + 1) * C::OC) continue;
             if (a.nsplit > 1) a.po[pa * a.s.d + col] = ov[i]; else o[col] = from_f<bf16>(ov[i] / ls);
           }
           if (a.nsplit > 1 && lead && lane == 0) a.pml[pa] = make_float2(m, ls);
         }
       }
-    });
+    };
+    if (NT == 1 && grp == 1) {
+      // ---------------------------------------------------------------- epilogue of the one tile
+      uint32_t n = 0;
+      walk([&](const Item& w) {
+        if (w.nb == 0) { no_keys(w); return; }
+        wait(&sm.stat_full, n & 1);
+        const float2 st = sm.stat[row];
+        bar_arrive(&sm.stat_free);
+        wait(&sm.o_full, n & 1);
+        ++n;
+        fence_after();
+        epilogue(w, st.x, st.y);
+      });
+    } else {
+      // ---------------------------------------------------------------- softmax
+      uint32_t cS = 0, par_s = 0, cW = 0, n = 0;           // blocks so far, parity of s_full; blocks whose P V is known to be complete; items
+      // (one by one, each before the P of the block after the next is announced: a parity says no more than the last phase)
+      auto wait_pv = [&](uint32_t blocks) { for (; cW != blocks; ++cW) wait(&sm.pv_done[tile], cW & 1); fence_after(); };
+      walk([&](const Item& w) {
+        const TileList& t = w.t;
+        if (w.nb == 0) { if (NT == 2) no_keys(w); return; }
+        if (tile * kTile >= t.nr) return;
+        // what this row sees of the list: positions kmin .. kmax and those below ksink, nodes
+        const bool tree = a.bt.parent != nullptr, missing = w.missing != 0;
+        uint32_t an;
+        const int p = position(w, tile * kTile + row, an), nb = w.nb, k0 = w.k0, k1 = w.k1, nc = t.nc;
+        const int shift = t.ns - t.lo;                     // index of a position of the window part, less the position
+        const int kmin = max(0, p - a.s.window + 1 + shift), kmax = tree ? nc - 1 : p + shift;
+        const int ksink = min(max(t.ns, min(a.s.n_sink, t.nk) + shift), kmax + 1);
+        uint32_t nodes = 0;
+        if (tree)
+          for (int j = 0; j < t.n; ++j)
+            if ((an >> j & 1u) && (t.L + w.depth[j] > p - a.s.window || t.L + w.depth[j] < a.s.n_sink)) nodes |= 1u << j;
+        // keys that every row of the warp sees
+        const int all0 = __reduce_max_sync(FULL, kmin), all1 = min(min(__reduce_min_sync(FULL, kmax) + 1, nc), k1);
+        auto visible = [&](int c0) {                       // keys c0 .. c0 + 31 of the list, a bit each
+          uint32_t m = bits(kmin - c0, min(kmax + 1, nc) - c0) | bits(-c0, min(ksink, nc) - c0);
+          if (tree) {
+            const int s = nc - c0;
+            if (s < 32 && s > -32) m |= s >= 0 ? nodes << s : nodes >> -s;
+          }
+          m &= bits(0, k1 - c0);
+          if (missing)
+            for (uint32_t x = m; x; x &= x - 1) { const int i = __ffs(x) - 1; if (list_row(a, t, c0 + i) == -1) m &= ~(1u << i); }
+          return m;
+        };
+        float ref = -INFINITY;
+        uint64_t l2[2] = {0, 0};                           // (two sums of two)
+        const uint64_t scale2 = pair2(a.scale2, a.scale2);
+#pragma unroll 1
+        for (int j = 0; j < nb; ++j) {
+          const int x = NT == 2 ? tile : (int)(cS & 1), c0 = k0 + j * kTile, slabs = (min(kTile, k1 - c0) + 31) / 32;
+          const uint32_t scol = s_col + x * kTile + lane_at;
+          wait(&sm.s_full[x], par_s >> x & 1);
+          par_s ^= 1u << x;
+          fence_after();
+          uint32_t sv[2][32];
+          tmem_ld32_nowait(scol, sv[0]);
+          auto slab = [&](int i, uint32_t (&s)[32], uint32_t (&ahead)[32]) {
+            const int c = c0 + 32 * i;
+            const bool whole = !missing && c >= all0 && c + 32 <= all1;
+            const uint32_t vis = whole ? FULL : visible(c);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            tmem_regs_ready(s);
+            if (i + 1 < slabs) tmem_ld32_nowait(scol + 32 * (i + 1), ahead);
+            if (!whole) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) if (!(vis >> e & 1u)) s[e] = 0xff800000u;
+            }
+            float m4[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m4[e] = fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 4]));
+#pragma unroll
+            for (int e = 8; e < 32; e += 2) m4[(e >> 1) & 3] = fmaxf(fmaxf(m4[(e >> 1) & 3], __uint_as_float(s[e])), __uint_as_float(s[e + 1]));
+            const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale2;
+            const bool up = mx > ref + kGap || (ref == -INFINITY && mx > ref);
+            if (__any_sync(FULL, up)) {                    // (alike in the warp: accesses to tensor memory are the whole warp's)
+              const float to = up ? ceilf(mx) : ref, f = up && ref != -INFINITY ? power_of_two(ref - to) : 1.f;
+              ref = to;
+              if (__any_sync(FULL, f != 1.f)) {
+                const uint64_t f2 = pair2(f, f);
+                l2[0] = fma2(l2[0], f2, 0); l2[1] = fma2(l2[1], f2, 0);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                if (i + 1 < slabs) tmem_regs_ready(ahead);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+#pragma unroll 1
+                for (int v = 0; v < i; ++v) {              // P of this block so far
+                  uint32_t r[16];
+                  tmem_ld16(scol + 16 * v, r);
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) {
+                    const float2 pv = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r[e]));
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(pv.x * f, pv.y * f);
+                    r[e] = *reinterpret_cast<const uint32_t*>(&h);
+                  }
+                  tmem_st16(scol + 16 * v, r);
+                }
+                if (j) {
+                  wait_pv(cS);
+#pragma unroll 1
+                  for (int v = 0; v < C::OC; v += 16) {
+                    uint32_t r[16];
+                    tmem_ld16(o_col + tile * C::OC + lane_at + v, r);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+                    tmem_st16(o_col + tile * C::OC + lane_at + v, r);
+                  }
+                }
+              }
+            }
+            const float neg = ref == -INFINITY ? 0.f : -ref;
+            const uint64_t neg2 = pair2(neg, neg);
+            uint32_t pk[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float2 y = unpair(fma2(pair2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, neg2));
+              const float p0 = ex2(y.x), p1 = ex2(y.y);
+              l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], pair2(p0, p1));
+              const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
+              pk[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            tmem_st16(scol + 16 * i, pk);
+          };
+#pragma unroll 1
+          for (int i = 0; i < slabs; i += 2) {
+            slab(i, sv[0], sv[1]);
+            if (i + 1 < slabs) slab(i + 1, sv[1], sv[0]);
+          }
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          fence_before();
+          wait_pv(cS);
+          bar_arrive(&sm.p_ready[x]);
+          ++cS;
+        }
+        const float2 la = unpair(l2[0]), lb = unpair(l2[1]);
+        const float sum = (la.x + la.y) + (lb.x + lb.y);
+        if (NT == 1) {
+          wait(&sm.stat_free, (n & 1) ^ 1);
+          sm.stat[row] = make_float2(ref, sum);
+          bar_arrive(&sm.stat_full);
+          ++n;
+        } else {
+          wait_pv(cS);
+          epilogue(w, ref, sum);
+        }
+      });
+    }
   }
   if (__any_sync(0xffffffffu, fail)) for (int b = lane; b < a.s.B; b += 32) atomicOr(a.status + b, TSV_ST_INTERNAL);   // (an internal error: every sequence is flagged)
   fence_before();
   __syncthreads();
-  if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(C::TM) : "memory");
+  if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
 }
 
 template <int DP, bool SHARED>
@@ -617,8 +727,8 @@ int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
   g.items = units * a.s.Hk * a.nsplit * C::HALVES;
   if (!ensure_smem((const void*)attn_tc_kernel<DP, SHARED>, C::SMEM)) return TSV_ERR_CUDA;
   TSV_PREP((attn_tc_kernel<DP, SHARED>));
-  const int64_t grid = g.items < 148 * C::OCC ? g.items : 148 * C::OCC;
-  attn_tc_kernel<DP, SHARED><<<(unsigned)grid, C::THREADS, C::SMEM, st>>>(g);
+  const int64_t grid = g.items < 148 ? g.items : 148;
+  attn_tc_kernel<DP, SHARED><<<(unsigned)grid, kTcThreads, C::SMEM, st>>>(g);
   count_launch();
   return TSV_OK;
 }

@@ -322,6 +322,29 @@ def test_many_sequences(api):
     lay.check(lay.run(tk))
 
 
+# more tiles than SMs, of one and of two halves, with a block of keys or several, in any order
+@pytest.mark.parametrize("heads,window", [(("bf16", 32, 1, 64, True), 20), (("bf16", 64, 2, 128, False), 150), (("bf16", 64, 1, 128, True), 200),
+                                          (("bf16", 40, 1, 72, False), 140), (("bf16", 32, 2, 256, False), 150), (("bf16", 64, 1, 512, True), 160)], ids=str)
+@pytest.mark.parametrize("tree", [False, True])
+def test_many_tiles(api, heads, window, tree):
+    _, tk, _ = api
+    rng = np.random.default_rng(window)
+    B = 260 if heads[3] <= 128 else 170
+    n = [int(x) for x in rng.integers(0, 12, B)]
+    lay = Layer(tk, *heads, window=window, sinks=2, L=[int(x) for x in rng.integers(0, 300, B)], n=n, tree=tree, page=32 if tree else 0, seed=9)
+    out = lay.run(tk)
+    pick = sorted(int(b) for b in rng.permutation(B)[:40])           # (the restatement takes its time)
+    es = STEP["bf16"]
+    got = f64(out)
+    assert not lay.status.any() and np.isfinite(got[~np.isnan(f64(lay.q)).any((1, 2))]).all()
+    for b in pick:
+        if n[b]:
+            r = slice(lay.row0[b], lay.row0[b] + n[b])
+            ref, mag, reach = lay.ref(b)
+            tol = es * np.abs(ref) + mag * 2.0 ** -8 + mag * 2 * ((heads[3] + 4) * 2.0 ** -24 * reach)[..., None] + 1e-30
+            assert (np.abs(got[r] - ref) <= tol).all(), b
+
+
 @pytest.mark.parametrize("heads", [HEADS[0], HEADS[1], HEADS[2]], ids=lambda h: "_".join(map(str, h)))
 def test_repeated_overlapping_and_replayed_calls(api, heads):
     """Bits do not depend on the run, on what is in the workspace, on the stream, on another call at the same time, or on a graph."""
