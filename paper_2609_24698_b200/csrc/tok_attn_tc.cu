@@ -8,16 +8,17 @@
 //   warps 10-13  copy Q, K and V rows into shared memory (16-byte asynchronous copies: rows come from pages, a ring or the call's own
 //                tensors, any of them with strides of their own, which no tensor map describes); a barrier counts a panel's copies as
 //                they land, and the thread that issues the products orders them before its reads (fence.proxy.async)
-// K and V live in panels of 128 rows x 64 columns (16 KiB, 128-byte swizzle): K row-major is the K-major operand of S, and the same
+// K and V live in panels of 128 rows (64 at d = 512) x 64 columns (128-byte swizzle): K row-major is the K-major operand of S, and the same
 // layout read MN-major the operand of P V, so that where the keys are the values one copy serves both products.  Two tiles share a
 // block of K and V: copies (half of the shared-memory traffic of a tile) and their instructions per product halve, and one tile's
 // softmax runs under the other's products.
 //
 // Tensor memory: two buffers of S (128 columns; of the two tiles, or of two blocks of the one) and O.  P (bf16) overlays the S it came
 // from.  d = 512 has no room for S beside all of O (512 columns): two CTAs take 256 output columns each and compute S and the softmax
-// alike.
+// alike.  There, where Q takes 128 KiB, blocks of 64 keys leave room for two of them: with one of 128 keys the next block's copies waited
+// for this one's P V, and lists of a few more than 128 keys paid for a second block 6.6 of 20 thousand cycles.
 //
-// Softmax: S is read once, in slabs of 32 keys.  The row's reference is its first maximum, rounded up to a whole power of two; it moves
+// Softmax: S is read once, in slabs of 64 keys.  The row's reference is its first maximum, rounded up to a whole power of two; it moves
 // where a later slab exceeds it by more than 2^10 (bf16 and fp32 have the range for weights above one), and then what is there of
 // P, the sum and O are multiplied by a power of two, exactly.  Nearly never after the first slab.
 // P is rounded to bf16 for the product (2^-9 of a weight); scores, sums and O are fp32.
@@ -30,7 +31,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = 128;            // query rows of a tile, keys of a block
+constexpr int kTile = 128;            // query rows of a tile; columns of an S buffer
 constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 4, kTcThreads = 32 * (10 + kCopyWarps);
 constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
@@ -44,26 +45,29 @@ struct Cfg {
   static constexpr int HALVES = DP / OC;
   static constexpr int NP = DP / 64, VP = OC / 64;           // panels of all of d, of the output columns
   static constexpr int KP = SHARED ? NP - VP : NP;           // panels that only S reads
-  static constexpr int NKS = KP == 0 ? 0 : DP == 512 ? 2 : 4;          // ring of those
-  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : SHARED && DP == 256 ? 2 : 1;   // buffers of the others, VP panels each
-  static constexpr int SMEM = kCtl + (NT * NP + NKS + NVB * VP) * kPanel;
+  static constexpr int GP = VP;                              // panels of a group: copied, announced and multiplied together
+  static constexpr int NG = NP / GP, KG = KP / GP;           // groups of all of d, of those that only S reads
+  static constexpr int BN = DP == 512 ? 64 : 128;            // keys of a block
+  static constexpr int PB = BN * 128;                        // bytes of a panel of keys
+  static constexpr int NKB = KP == 0 ? 0 : DP == 64 ? 4 : DP == 128 ? 2 : 1;          // buffers of a block's K groups
+  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : SHARED ? 2 : 1;   // of its V group
+  static constexpr int SMEM = kCtl + NT * NP * kPanel + (NKB * KP + NVB * VP) * PB;
 };
 
 // An item: tile, output columns, keys.  mode: 0 the first time; of those that left a mark then, 1 as before (which rows are not finite?)
 // and 2 with values that are not finite taken as zero.
 struct Item {
   TileList t;
-  int64_t unit;
-  int half, split, k0, k1, nb, nt, mode, li;
+  int unit, half, split, k0, k1, nb, nt, mode, li;
   int missing;                        // a page of the list is not there
   int depth[TSV_MAX_D];
   uint32_t anc[TSV_MAX_D];
 };
 
 struct TcCtl {
-  uint64_t fullQ[8], emptyQ;
+  uint64_t fullQ[4], emptyQ;                  // groups of panels: Q (tile, group), K (buffer, group), V (buffer)
   uint64_t fullK[4], emptyK[4];
-  uint64_t fullV[8], emptyV[4];
+  uint64_t fullV[4], emptyV[4];
   uint64_t s_full[2], p_ready[2], pv_done[2], o_free[2];
   uint64_t o_full, stat_full, stat_free;      // one tile: O is complete; reference and sum of its rows, for the epilogue
   uint64_t item_full[kItems], item_free[kItems];
@@ -79,6 +83,30 @@ __device__ __forceinline__ void bar_init(uint64_t* b, int count) {
 }
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+// One bounded try in line, the others (to the limit) in a function: a wait is in the code of some thirty places.
+__device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
+#pragma unroll 1
+  for (uint32_t it = 0; it < WAIT_LIMIT; ++it) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
+  const uint32_t addr = smem_u32(bar);
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
+  return ok || bar_wait_on(addr, parity);
+}
+// Whether the phase is complete.
+__device__ __forceinline__ bool bar_ready(uint64_t* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  return ok != 0;
 }
 // An arrival of this thread when its copies so far have landed.
 __device__ __forceinline__ void bar_arrive_copied(uint64_t* b) {
@@ -125,8 +153,63 @@ __device__ __forceinline__ float power_of_two(float x) {
 
 struct TcArgs {
   AttnArgs a;
-  int64_t items;
+  int32_t items;
 };
+
+// What is rare stays out of the loops' code: at some 150 KB of it, the warp that issues the products took a thousand cycles for the forty
+// instructions of a panel.
+
+// Of keys c0 .. (bits of m) those that have a page.
+__device__ __noinline__ uint32_t have_pages(const AttnArgs& a, const TileList& t, int c0, uint32_t m) {
+  for (uint32_t x = m; x; x &= x - 1) {
+    const int i = __ffs(x) - 1;
+    if (list_row(a, t, c0 + i) == -1) m &= ~(1u << i);
+  }
+  return m;
+}
+// Multiplies the first `slabs` slabs of P at p_col, and `cols` columns of O, by f (a power of two).
+__device__ __noinline__ void rescale(uint32_t p_col, int slabs, uint32_t o_col, int cols, float f) {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+#pragma unroll 1
+  for (int v = 0; v < slabs; ++v) {
+    uint32_t r[16];
+    tmem_ld16(p_col + 16 * v, r);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float2 pv = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r[e]));
+      const __nv_bfloat162 h = __floats2bfloat162_rn(pv.x * f, pv.y * f);
+      r[e] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    tmem_st16(p_col + 16 * v, r);
+  }
+#pragma unroll 1
+  for (int v = 0; v < cols; v += 16) {
+    uint32_t r[16];
+    tmem_ld16(o_col + v, r);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+    tmem_st16(o_col + v, r);
+  }
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// Columns c0 .. c1 - 1 of row r of an item (r0: in its sequence and key head) by definition, if the row sees something not finite; part:
+// the row's place among partial outputs.  By a warp.
+__device__ __noinline__ void exact_output(const AttnArgs& a, const TileList& t, const int* depth, int gr, int p, uint32_t an, int k0, int k1, int c0, int c1,
+                                          size_t part) {
+  const int lane = threadIdx.x & 31;
+  const int64_t tok = t.row0 + gr / a.G;
+  const size_t head = (size_t)t.hk * a.G + gr % a.G;
+  float m, l, o[16];
+  if (!exact_row<bf16>(a, t, depth, reinterpret_cast<const bf16*>(a.in.q) + tok * a.in.q_ld + head * a.s.d, p, an, k0, k1, m, l, o)) return;
+  bf16* out = reinterpret_cast<bf16*>(a.out) + (tok * a.s.H + head) * a.s.d;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int col = lane + 32 * i;
+    if (col < c0 || col >= c1) continue;
+    if (a.nsplit > 1) a.po[part * a.s.d + col] = o[i]; else out[col] = from_f<bf16>(o[i] / l);
+  }
+  if (a.nsplit > 1 && c0 == 0 && lane == 0) a.pml[part] = make_float2(m, l);
+}
 
 template <int DP, bool SHARED>
 __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_constant__ TcArgs g) {
@@ -136,13 +219,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   const AttnArgs& a = g.a;
   TcCtl& sm = *reinterpret_cast<TcCtl*>(smem_raw);
   const uint32_t base = smem_u32(smem_raw) + kCtl;
-  const uint32_t q_at = base, k_at = q_at + NT * C::NP * kPanel, v_at = k_at + C::NKS * kPanel;
+  const uint32_t q_at = base, k_at = q_at + NT * C::NP * kPanel, v_at = k_at + C::NKB * C::KP * C::PB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
   if (tid == 0) {
-    for (int i = 0; i < 8; ++i) { bar_init(&sm.fullQ[i], 32 * kCopyWarps); bar_init(&sm.fullV[i], 32 * kCopyWarps); }
     for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], 9 + kCopyWarps); }
-    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullK[i], 32 * kCopyWarps); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
+    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullQ[i], 32 * kCopyWarps); bar_init(&sm.fullV[i], 32 * kCopyWarps); bar_init(&sm.fullK[i], 32 * kCopyWarps); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
     for (int i = 0; i < 2; ++i) { bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.pv_done[i], 1); bar_init(&sm.o_free[i], kTile); }
     bar_init(&sm.emptyQ, 1); bar_init(&sm.o_full, 1); bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -157,32 +239,41 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   fence_after();
   const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + 2 * kTile;
 
-  auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !mbar_wait(b, parity)) fail = 1; };
+  auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait(b, parity)) fail = 1; };
   // Calls body(item) for this CTA's items, as the list warp finds them, until it marks the end; then, where one has left a mark, for those.
-  auto walk = [&](auto&& body) {
+  // By a warp, or by its first thread alone.
+  auto walk_as = [&](auto&& body, bool alone) {
     uint32_t c = 0;
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {
+      if (!alone || lane == 0) {
+        uint32_t slot = c % kItems, parity = c / kItems & 1;
 #pragma unroll 1
-      for (;; ++c) {
-        wait(&sm.item_full[c % kItems], c / kItems & 1);
-        if (__any_sync(0xffffffffu, fail)) { fail = 1; break; }     // (without its item a warp has nothing to go by)
-        const Item& w = sm.item[c % kItems];
-        const bool end = w.t.ok == 0;
-        if (!end) body(w);
-        __syncwarp();
-        if (lane == 0) bar_arrive(&sm.item_free[c % kItems]);
-        if (end) { ++c; break; }
+        for (;;) {
+          wait(&sm.item_full[slot], parity);
+          if (!alone) fail = __any_sync(0xffffffffu, fail);
+          if (fail) break;                                 // (without its item a role has nothing to go by)
+          const Item& w = sm.item[slot];
+          const bool end = w.t.ok == 0;
+          if (!end) body(w);
+          if (!alone) __syncwarp();
+          if (lane == 0) bar_arrive(&sm.item_free[slot]);
+          ++c;
+          if (++slot == kItems) { slot = 0; parity ^= 1; }
+          if (end) break;
+        }
       }
+      __syncwarp();
       if (round == 0) {
         __syncthreads();
         uint32_t any = 0;
         for (int i = 0; i < 32; ++i) any |= sm.redo[i];
-        if (!any) break;                                        // (alike in all threads)
+        if (!any) break;                                   // (alike in all threads)
       }
     }
   };
-  auto rows_of_block = [&](const Item& w, int j) { return min(kTile, w.k1 - w.k0 - j * kTile); };
+  auto walk = [&](auto&& body) { walk_as(body, false); };
+  auto walk_one = [&](auto&& body) { walk_as(body, true); };
 
   if (warp == kListWarp) {
     // ------------------------------------------------------------------ items
@@ -190,16 +281,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {
       int li = 0;
-      int64_t idx = blockIdx.x;
+      int idx = blockIdx.x;
 #pragma unroll 1
       for (bool more = true; more; idx += gridDim.x, ++li) {
         if (idx < g.items && round && !(sm.redo[(li >> 5) & 31] >> (li & 31) & 1u)) continue;
-        const int half = (int)(idx % C::HALVES);
-        int64_t r = idx / C::HALVES;
-        const int hk = (int)(r % a.s.Hk);
-        r /= a.s.Hk;
-        const int split = (int)(r % a.nsplit);
-        const int64_t unit = r / a.nsplit;
+        const int half = idx % C::HALVES, i1 = idx / C::HALVES, i2 = i1 / a.s.Hk, hk = i1 - i2 * a.s.Hk, unit = i2 / a.nsplit, split = i2 - unit * a.nsplit;
 #pragma unroll 1
         for (int mode = round; more && mode <= 2 * round; ++mode, ++c) {
           wait(&sm.item_free[c % kItems], (c / kItems & 1) ^ 1);
@@ -212,10 +298,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           int k0 = 0, k1 = 0, nb = 0;
           bool missing = false;
           if (t.ok == 1) {
-            const int blocks = (t.nk + kTile - 1) / kTile, per = (blocks + a.nsplit - 1) / a.nsplit;
-            k0 = min(t.nk, split * per * kTile);
-            k1 = min(t.nk, k0 + per * kTile);
-            nb = (k1 - k0 + kTile - 1) / kTile;
+            const int blocks = (t.nk + C::BN - 1) / C::BN, per = (blocks + a.nsplit - 1) / a.nsplit;
+            k0 = min(t.nk, split * per * C::BN);
+            k1 = min(t.nk, k0 + per * C::BN);
+            nb = (k1 - k0 + C::BN - 1) / C::BN;
             if (a.c.page_table) {                          // the last position of the list in each of its pages
               const int P = a.c.page_tokens, s1 = min(t.ns, t.L) - 1, w1 = min(t.L, t.lo + (t.nc - t.ns)) - 1;
               for (int lp = lane; s1 >= 0 && lp <= s1 / P; lp += 32) missing |= tok_cache_row(a.c, a.s.window, a.s.n_sink, t.b, min(s1, lp * P + P - 1)) < 0;
@@ -223,6 +309,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             }
           }
           missing = __any_sync(0xffffffffu, missing);
+          // The queries into L2, two items before they are copied: those copies all come at once, when Q is free, and left to them HBM would
+          // idle in between.
+          if (nb && mode == 0 && half == 0) {
+            const int t0 = t.r0 / a.G, t1 = (t.r0 + t.nr - 1) / a.G;
+            for (int tok = t0 + lane; tok <= t1; tok += 32)
+              asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const bf16*>(a.in.q) + (t.row0 + tok) * a.in.q_ld + (size_t)hk * a.G * a.s.d), "r"(a.G * a.s.d * 2) : "memory");
+          }
           if (lane == 0) {
             w.t = t; w.unit = unit; w.half = half; w.split = split; w.k0 = k0; w.k1 = k1; w.nb = nb; w.nt = t.ok && t.nr > kTile ? 2 : 1; w.mode = mode; w.li = li; w.missing = missing;
             if (missing) atomicOr(a.status + t.b, TSV_ST_PAGE);
@@ -241,189 +334,172 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   } else if (warp > kListWarp) {
     // ------------------------------------------------------------------ producers
     // A thread copies one 16-byte chunk of the rows prow + ROWS i of a panel; where these rows are is worked out by the eight threads of
-    // a row together, a block ahead.
-    constexpr int ROWS = 4 * kCopyWarps, PER = kTile / ROWS, EACH = PER / 8;
+    // a row together (row i by thread i of them), a block ahead.
+    constexpr int ROWS = 4 * kCopyWarps, PQ = kTile / ROWS, PK = C::BN / ROWS;
+    static_assert(PQ == 8 && PK <= 8, "a thread of eight for each row of a thread");
     const int pt = tid - 32 * (kListWarp + 1), prow = pt >> 3, chunk = pt & 7;
     const int dch = a.s.d / 8;
-    uint32_t cQ = 0, cK = 0, cV = 0;
-    const uint32_t off = (uint32_t)prow * 128 + ((chunk ^ (prow & 7)) << 4);     // (the rows are multiples of 8 apart: the same swizzle)
+    uint32_t par_e = 0, par_k = 0, par_v = 0;              // parities of Q and of the buffers of K and V groups
+    int kb = 0, vb = 0;                                    // next buffers
+    const uint32_t off = (uint32_t)prow * 128 + ((chunk ^ (prow & 7)) << 4);     // (rows 16 apart: the same swizzle)
     walk([&](const Item& w) {
       const int nb = w.nb;
       if (nb == 0) return;
       const int mode = w.mode, half = w.half, hk = w.t.hk;
-      // ptr: this thread's chunk in panel 0 of its rows (nullptr: nothing there)
-      auto panel = [&](uint32_t at, int rows, int pan, const bf16* const (&ptr)[PER]) {     // rows: a multiple of 16
-        const bool in = pan * 8 + chunk < dch;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          if (ROWS * i >= rows) break;
-          const bool live = in && ptr[i];
-          cp16(at + off + i * ROWS * 128, live ? ptr[i] + pan * 64 : reinterpret_cast<const bf16*>(a.in.q), live);
-        }
-      };
-      // Rows of a block: a thread finds those of i = chunk, chunk + 8 and tells the others of its group, which have the same rows.
-      int64_t code[EACH];
+      int64_t code = -1;                                   // of this thread's row in the next block
       auto find = [&](int j) {
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-          const int kk = w.k0 + j * kTile + prow + ROWS * (chunk + 8 * e);
-          code[e] = kk < w.k1 ? list_row(a, w.t, kk) : -1;
-        }
+        const int kk = w.k0 + j * C::BN + prow + ROWS * chunk;
+        code = chunk < PK && kk < w.k1 ? list_row(a, w.t, kk) : -1;
       };
-      auto point = [&](bool value, const bf16* (&ptr)[PER]) {
-        unsigned long long mine[EACH];
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) mine[e] = code[e] == -1 ? 0ull : reinterpret_cast<unsigned long long>(row_ptr<bf16>(a, hk, code[e], value));
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const unsigned long long x = __shfl_sync(0xffffffffu, mine[i / 8], (lane & ~7) | (i & 7));
-          ptr[i] = x ? reinterpret_cast<const bf16*>(x) + chunk * 8 : nullptr;
-        }
-      };
-      const bf16* ptr[PER];
-      const bf16* vptr[PER];
-      wait(&sm.emptyQ, (cQ & 1) ^ 1);
-#pragma unroll 1
-      for (int tile = 0; tile < w.nt; ++tile) {
-        unsigned long long mine[EACH];
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-          const int r = tile * kTile + prow + ROWS * (chunk + 8 * e), gr = w.t.r0 + r;
-          mine[e] = r < w.t.nr ? reinterpret_cast<unsigned long long>(reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)hk * a.G + gr % a.G) * a.s.d) : 0ull;
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const unsigned long long x = __shfl_sync(0xffffffffu, mine[i / 8], (lane & ~7) | (i & 7));
-          ptr[i] = x ? reinterpret_cast<const bf16*>(x) + chunk * 8 : nullptr;
-        }
-#pragma unroll 1
-        for (int p = 0; p < C::NP; ++p) {
-          // (in the order in which S takes them: the item's own output columns last where K is V)
-          panel(q_at + (tile * C::NP + p) * kPanel, kTile, SHARED && C::KP ? (p + (half + 1) * C::VP) % C::NP : p, ptr);
-          bar_arrive_copied(&sm.fullQ[tile * C::NP + p]);
-        }
-      }
-      ++cQ;
+      // Groups of panels: of block j those of K that only S reads and that of the output columns, of Q each tile's.
+      // The first block comes before Q: its buffers are free before Q's, which the item before reads to its last block.
       find(0);
 #pragma unroll 1
-      for (int j = 0; j < nb; ++j) {
-        const int rows16 = (rows_of_block(w, j) + 15) & ~15;
-        point(false, ptr);
-        if (!SHARED) point(true, vptr);
+      for (int j = 0;; ++j) {
+        const int first = j == 1 ? -w.nt * C::NG : 0, last = j < nb ? C::KG + 1 : 0;
+        const int64_t now = code;
         if (j + 1 < nb) find(j + 1);
+        const int rows16 = (min(C::BN, w.k1 - w.k0 - j * C::BN) + 15) & ~15;
 #pragma unroll 1
-        for (int p = 0; p < C::KP; ++p) {
-          const int slot = cK % (C::NKS ? C::NKS : 1);
-          wait(&sm.emptyK[slot], (cK / (C::NKS ? C::NKS : 1) & 1) ^ 1);
-          panel(k_at + slot * kPanel, rows16, SHARED ? (p + (half + 1) * C::VP) % C::NP : p, ptr);
-          bar_arrive_copied(&sm.fullK[slot]);
-          ++cK;
-        }
-        const int buf = cV % C::NVB;
-        wait(&sm.emptyV[buf], (cV / C::NVB & 1) ^ 1);
+        for (int grp = first; grp < last; ++grp) {
+          const bool is_q = grp < 0, is_v = grp == C::KG;
+          const int qg = grp + w.nt * C::NG;               // (tile, group) of Q
+          unsigned long long mine = 0;
+          if (is_q) {
+            const int r = qg / C::NG * kTile + prow + ROWS * chunk, gr = w.t.r0 + r;
+            if (r < w.t.nr) mine = reinterpret_cast<unsigned long long>(reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)hk * a.G + gr % a.G) * a.s.d);
+          } else if (now != -1) {
+            mine = reinterpret_cast<unsigned long long>(row_ptr<bf16>(a, hk, now, is_v));
+          }
+          // in the order in which S takes them: the item's own output columns last where K is V
+          const int g = is_q ? qg % C::NG : grp;
+          const int pan0 = is_v ? half * C::VP : SHARED && C::KG ? (g + half + 1) % C::NG * C::GP : g * C::GP;
+          const int rows = is_q ? kTile : rows16;
+          uint64_t* bar;
+          uint32_t to;
+          if (is_q) {
+            if (grp == first) { wait(&sm.emptyQ, par_e & 1 ^ 1); par_e ^= 1; }
+            bar = sm.fullQ + qg;
+            to = q_at + qg * C::GP * kPanel;
+          } else if (is_v) {
+            wait(&sm.emptyV[vb], (par_v >> vb & 1) ^ 1);
+            par_v ^= 1u << vb;
+            bar = sm.fullV + vb;
+            to = v_at + vb * C::VP * C::PB;
+            vb = vb + 1 == C::NVB ? 0 : vb + 1;
+          } else {
+            wait(&sm.emptyK[kb], (par_k >> kb & 1) ^ 1);
+            par_k ^= 1u << kb;
+            bar = sm.fullK + kb;
+            to = k_at + kb * C::GP * C::PB;
+            kb = kb + 1 == C::NKB * C::KG ? 0 : kb + 1;
+          }
+          to += off;
+          const bf16* ptr[PQ];                             // this thread's chunk in the group's first panel, of its rows (nullptr: nothing there)
+#pragma unroll
+          for (int i = 0; i < PQ; ++i) {
+            const unsigned long long x = __shfl_sync(0xffffffffu, mine, (lane & ~7) | i);
+            ptr[i] = x ? reinterpret_cast<const bf16*>(x) + pan0 * 64 + chunk * 8 : nullptr;
+          }
+          const int stride = is_q ? kPanel : C::PB;
 #pragma unroll 1
-        for (int p = 0; p < C::VP; ++p) {
-          const uint32_t at = v_at + (buf * C::VP + p) * kPanel;
-          panel(at, rows16, half * C::VP + p, SHARED ? ptr : vptr);
-          if (mode == 2) {
+          for (int p = 0; p < C::GP; ++p) {
+            const bool in = (pan0 + p) * 8 + chunk < dch;
+#pragma unroll
+            for (int i = 0; i < PQ; ++i) {
+              if (ROWS * i >= rows) break;
+              const bool live = in && ptr[i];
+              cp16(to + p * stride + i * ROWS * 128, live ? ptr[i] + p * 64 : reinterpret_cast<const bf16*>(a.in.q), live);
+            }
+          }
+          if (mode == 2 && is_v) {                         // (what this thread has copied)
             cp_commit();
             cp_wait<0>();
-#pragma unroll
-            for (int i = 0; i < PER; ++i) if (ROWS * i < rows16) make_finite<bf16>(smem_raw + (at + off + i * ROWS * 128 - smem_u32(smem_raw)));
-            bar_arrive(&sm.fullV[buf * C::VP + p]);
+            for (int p = 0; p < C::GP; ++p)
+              for (int i = 0; ROWS * i < rows; ++i) make_finite<bf16>(smem_raw + (to + p * stride + i * ROWS * 128 - smem_u32(smem_raw)));
+            bar_arrive(bar);
           } else {
-            bar_arrive_copied(&sm.fullV[buf * C::VP + p]);
+            bar_arrive_copied(bar);
           }
         }
-        ++cV;
+        if (j >= nb) break;
       }
     });
     cp_commit();
     cp_wait<0>();
   } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------------ products
+    // ------------------------------------------------------------------ products (one thread)
     const uint32_t idesc_v = make_idesc(C::OC, 1);
-    uint32_t cK = 0, cVs = 0, cVo = 0;                     // uses so far: K panels, V buffers by S and by O
-    uint32_t cS = 0, par_q = 0, par_p = 0, par_o = 3;      // blocks' scores; parities of a tile's fullQ and o_free, of p_ready
-    const bool one = lane == 0;
-    walk([&](const Item& w) {
-      const int nb = w.nb, nt = NT == 2 ? w.nt : 1;
+    uint32_t par_q = 0, par_k = 0, par_vs = 0, par_vo = 0, par_p = 0, par_o = 3;     // parities: per tile, buffers (of V for S and for O), S buffer, tile
+    int kb = 0, vs = 0, vo = 0, sx = 0;                    // next K buffer, V buffer (for S, for O), S buffer of one tile
+    walk_one([&](const Item& w) {
+      const int nb = w.nb, nt = NT == 2 ? w.nt : 1, k_all = w.k1 - w.k0;
       if (nb == 0) return;
-      const int k_all = w.k1 - w.k0;
-      // scores of panels p0 .. p1 - 1 of block j and tile t, into S buffer x
-      auto scores = [&](int j, int t, int x, int p0, int p1) {
-        const uint32_t idesc = make_idesc((min(kTile, k_all - j * kTile) + 15) & ~15, 0), dst = s_col + x * kTile;
+      // A step: scores of block sb (of tile t), output of the block before.  Two tiles: P V first, whose P lies where the scores will.
+      // One tile: the scores go to the other buffer, and P V as soon as P is there (with the scores first, P V waited for copies
+      // whose buffers it was to free).
+      int sb = 0, ob = -1, t = 0;
+#pragma unroll 1
+      while (ob < nb) {
+        int g = sb < nb ? 0 : C::NG, at_k = kb;
+        bool out = ob < 0;
+        const int xs = NT == 2 ? t : sx, xo = NT == 2 ? t : sx ^ 1;
+        const uint32_t idesc = make_idesc((min(C::BN, k_all - sb * C::BN) + 15) & ~15, 0), dst = s_col + xs * kTile;
         const bool last = t == nt - 1;
-        for (int p = p0; p < p1; ++p) {
-          if (j == 0) wait(&sm.fullQ[t * C::NP + p], par_q >> t & 1);
-          const bool ring = p < C::KP;
-          const uint32_t kp = cK + p, slot = kp % (C::NKS ? C::NKS : 1);
-          uint32_t at;
-          if (ring) {
-            wait(&sm.fullK[slot], kp / (C::NKS ? C::NKS : 1) & 1);
-            at = k_at + slot * kPanel;
-          } else {
-            const int buf = cVs % C::NVB;
-            wait(&sm.fullV[buf * C::VP + p - C::KP], cVs / C::NVB & 1);
-            at = v_at + (buf * C::VP + p - C::KP) * kPanel;
-          }
-          fence_proxy();
-          fence_after();
-          if (one) {
-            const uint64_t qd = make_desc(q_at + (t * C::NP + p) * kPanel, 16, 1024), kd = make_desc(at, 16, 1024);
+#pragma unroll 1
+        for (uint32_t spins = 0; g < C::NG || !out; ++spins) {
+          if (!out && (NT == 2 || fail || g == C::NG || (bar_ready(&sm.p_ready[xo], par_p >> xo & 1) && (ob || bar_ready(&sm.o_free[0], par_o & 1))))) {
+            // O (+)= P V of block ob
+            if (!SHARED) wait(&sm.fullV[vo], par_vo >> vo & 1);
+            if (ob == 0) { wait(&sm.o_free[t], par_o >> t & 1); par_o ^= 1u << t; }
+            wait(&sm.p_ready[xo], par_p >> xo & 1);
+            par_p ^= 1u << xo;
+            fence_proxy();
+            fence_after();
+            const uint64_t vd = make_desc(v_at + vo * C::VP * C::PB, C::PB, 1024);
+            const uint32_t pc = s_col + xo * kTile, oc = o_col + t * C::OC;
+            const int left = k_all - ob * C::BN;
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) mma_ss(dst, qd + 2 * ks, kd + 2 * ks, idesc, (p | ks) != 0);
-            if (ring && last) mma_commit(&sm.emptyK[slot]);
+            for (int k = 0; k < C::BN / 16; ++k) {
+              if (16 * k >= left) break;
+              mma_ts(oc, pc + 8 * k, vd + k * (2048 >> 4), idesc_v, k ? 1u : (uint32_t)ob);
+            }
+            if (last) { mma_commit(&sm.emptyV[vo]); par_vo ^= 1u << vo; vo = vo + 1 == C::NVB ? 0 : vo + 1; }
+            mma_commit(&sm.pv_done[t]);
+            if (NT == 1 && ob == nb - 1) mma_commit(&sm.o_full);
+            out = true;
+          } else if (g < C::NG) {
+            const bool k_only = g < C::KG;
+            uint64_t* b = k_only ? &sm.fullK[at_k] : &sm.fullV[vs];
+            const uint32_t parity = (k_only ? par_k >> at_k : par_vs >> vs) & 1;
+            if (out || fail || bar_ready(b, parity)) {
+              wait(b, parity);
+              if (sb == 0) wait(&sm.fullQ[t * C::NG + g], par_q >> t & 1);
+              fence_proxy();
+              fence_after();
+              const uint64_t qd = make_desc(q_at + (t * C::NG + g) * C::GP * kPanel, 16, 1024);
+              const uint64_t kd = make_desc(k_only ? k_at + at_k * C::GP * C::PB : v_at + vs * C::VP * C::PB, 16, 1024);
+#pragma unroll
+              for (int i = 0; i < 4 * C::GP; ++i)
+                mma_ss(dst, qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), idesc, i ? 1u : (uint32_t)g);
+              if (k_only) {
+                if (last) { mma_commit(&sm.emptyK[at_k]); par_k ^= 1u << at_k; }
+                at_k = at_k + 1 == C::NKB * C::KG ? 0 : at_k + 1;
+              }
+              if (++g == C::NG) {
+                mma_commit(&sm.s_full[xs]);
+                if (last && sb == nb - 1) mma_commit(&sm.emptyQ);
+              }
+              spins = 0;
+            }
           }
-          __syncwarp();
+          if (spins > (WAIT_LIMIT << 8)) fail = 1;          // (some 30 cycles each)
         }
-        if (p1 < C::NP) return;
-        if (one) {
-          mma_commit(&sm.s_full[x]);
-          if (last && j == nb - 1) mma_commit(&sm.emptyQ);
+        if (sb < nb) {
+          if (last) { kb = at_k; par_vs ^= 1u << vs; vs = vs + 1 == C::NVB ? 0 : vs + 1; }
+          if (NT == 1) sx ^= 1;
         }
-        __syncwarp();
-        if (last) { cK += C::KP; ++cVs; ++cS; }
-      };
-      auto output = [&](int j, int t, int x) {
-        const int buf = cVo % C::NVB;
-        const bool last = t == nt - 1;
-        if (!SHARED)
-          for (int p = 0; p < C::VP; ++p) wait(&sm.fullV[buf * C::VP + p], cVo / C::NVB & 1);
-        if (j == 0) { wait(&sm.o_free[t], par_o >> t & 1); par_o ^= 1u << t; }
-        wait(&sm.p_ready[x], par_p >> x & 1);
-        par_p ^= 1u << x;
-        fence_proxy();
-        fence_after();
-        const int steps = (min(kTile, k_all - j * kTile) + 15) / 16;
-        if (one) {
-          const uint64_t vd = make_desc(v_at + buf * C::VP * kPanel, kPanel, 1024);
-          for (int ks = 0; ks < steps; ++ks) mma_ts(o_col + t * C::OC, s_col + x * kTile + ks * 8, vd + ks * (2048 >> 4), idesc_v, (j | ks) != 0);
-          if (last) mma_commit(&sm.emptyV[buf]);
-          mma_commit(&sm.pv_done[t]);
-          if (NT == 1 && j == nb - 1) mma_commit(&sm.o_full);
-        }
-        __syncwarp();
-        if (last) ++cVo;
-      };
-      if (NT == 2) {
-        for (int t = 0; t < nt; ++t) scores(0, t, t, 0, C::NP);
-        for (int j = 0; j < nb; ++j)
-          for (int t = 0; t < nt; ++t) {
-            output(j, t, t);
-            if (j + 1 < nb) scores(j + 1, t, t, 0, C::NP);
-          }
-      } else {
-        // The scores of the next block under the softmax of this one: all of them, or, where the panels that both products read have one
-        // buffer, those of the other panels.
-        constexpr int AHEAD = SHARED && C::NVB == 1 ? C::KP : C::NP;
-        scores(0, 0, cS & 1, 0, C::NP);
-        for (int j = 0; j < nb; ++j) {
-          const int x = (cS - 1) & 1;                      // (of block j)
-          if (AHEAD && j + 1 < nb) scores(j + 1, 0, x ^ 1, 0, AHEAD);
-          output(j, 0, x);
-          if (AHEAD < C::NP && j + 1 < nb) scores(j + 1, 0, x ^ 1, AHEAD, C::NP);
-        }
+        if (last) { t = 0; ++sb; ++ob; } else ++t;
       }
       par_q ^= nt == 2 ? 3u : 1u;                          // (an item of one tile does not use the other's)
     });
@@ -548,20 +624,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         uint32_t an;
         const int p = position(w, rt + row, an);
         for (uint32_t todo = __ballot_sync(FULL, bad); todo; todo &= todo - 1) {
-          const int x = __ffs(todo) - 1, gr = t.r0 + r0 + x, pr = __shfl_sync(FULL, p, x);
-          const uint32_t ar = __shfl_sync(FULL, an, x);
-          const bf16* q = reinterpret_cast<const bf16*>(a.in.q) + (t.row0 + gr / a.G) * a.in.q_ld + ((size_t)t.hk * a.G + gr % a.G) * a.s.d;
-          float m, ls, ov[16];
-          if (!exact_row<bf16>(a, t, w.depth, q, pr, ar, w.k0, w.k1, m, ls, ov)) continue;
-          const size_t pa = part_at(w, r0 + x);
-          bf16* o = out_at(t, r0 + x);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int col = lane + 32 * i;
-            if (col >= a.s.d || col < w.half * C::OC || col >= (w.half + 1) * C::OC) continue;
-            if (a.nsplit > 1) a.po[pa * a.s.d + col] = ov[i]; else o[col] = from_f<bf16>(ov[i] / ls);
-          }
-          if (a.nsplit > 1 && lead && lane == 0) a.pml[pa] = make_float2(m, ls);
+          const int x = __ffs(todo) - 1;
+          exact_output(a, t, w.depth, t.r0 + r0 + x, __shfl_sync(FULL, p, x), __shfl_sync(FULL, an, x), w.k0, w.k1, w.half * C::OC,
+                       min(a.s.d, (w.half + 1) * C::OC), part_at(w, r0 + x));
         }
       }
     };
@@ -600,98 +665,75 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             if ((an >> j & 1u) && (t.L + w.depth[j] > p - a.s.window || t.L + w.depth[j] < a.s.n_sink)) nodes |= 1u << j;
         // keys that every row of the warp sees
         const int all0 = __reduce_max_sync(FULL, kmin), all1 = min(min(__reduce_min_sync(FULL, kmax) + 1, nc), k1);
-        auto visible = [&](int c0) {                       // keys c0 .. c0 + 31 of the list, a bit each
-          uint32_t m = bits(kmin - c0, min(kmax + 1, nc) - c0) | bits(-c0, min(ksink, nc) - c0);
-          if (tree) {
-            const int s = nc - c0;
-            if (s < 32 && s > -32) m |= s >= 0 ? nodes << s : nodes >> -s;
-          }
-          m &= bits(0, k1 - c0);
-          if (missing)
-            for (uint32_t x = m; x; x &= x - 1) { const int i = __ffs(x) - 1; if (list_row(a, t, c0 + i) == -1) m &= ~(1u << i); }
-          return m;
-        };
         float ref = -INFINITY;
-        uint64_t l2[2] = {0, 0};                           // (two sums of two)
+        uint64_t l2[4] = {0, 0, 0, 0};                     // (four sums of two)
         const uint64_t scale2 = pair2(a.scale2, a.scale2);
 #pragma unroll 1
         for (int j = 0; j < nb; ++j) {
-          const int x = NT == 2 ? tile : (int)(cS & 1), c0 = k0 + j * kTile, slabs = (min(kTile, k1 - c0) + 31) / 32;
+          const int x = NT == 2 ? tile : (int)(cS & 1), c0 = k0 + j * C::BN, slabs = (min(C::BN, k1 - c0) + 63) / 64;
           const uint32_t scol = s_col + x * kTile + lane_at;
           wait(&sm.s_full[x], par_s >> x & 1);
           par_s ^= 1u << x;
           fence_after();
-          uint32_t sv[2][32];
-          tmem_ld32_nowait(scol, sv[0]);
-          auto slab = [&](int i, uint32_t (&s)[32], uint32_t (&ahead)[32]) {
-            const int c = c0 + 32 * i;
-            const bool whole = !missing && c >= all0 && c + 32 <= all1;
-            const uint32_t vis = whole ? FULL : visible(c);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            tmem_regs_ready(s);
-            if (i + 1 < slabs) tmem_ld32_nowait(scol + 32 * (i + 1), ahead);
+#pragma unroll 1
+          for (int i = 0; i < slabs; ++i) {
+            const int c = c0 + 64 * i;
+            uint32_t sv[64];
+            tmem_ld32_nowait(scol + 64 * i, sv);
+            tmem_ld32_nowait(scol + 64 * i + 32, sv + 32);
+            const bool whole = !missing && c >= all0 && c + 64 <= all1;
+            uint32_t vis[2] = {FULL, FULL};
             if (!whole) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) if (!(vis >> e & 1u)) s[e] = 0xff800000u;
+              for (int v = 0; v < 2; ++v) {
+                const int cv = c + 32 * v, x = nc - cv;
+                vis[v] = bits(kmin - cv, min(kmax + 1, nc) - cv) | bits(-cv, min(ksink, nc) - cv);
+                if (tree && x < 32 && x > -32) vis[v] |= x >= 0 ? nodes << x : nodes >> -x;
+                vis[v] &= bits(0, k1 - cv);
+                if (missing) vis[v] = have_pages(a, t, cv, vis[v]);
+              }
             }
-            float m4[4];
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            tmem_regs_ready(sv);
+            tmem_regs_ready(sv + 32);
+            if (!whole) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) m4[e] = fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 4]));
+              for (int e = 0; e < 64; ++e) if (!(vis[e >> 5] >> (e & 31) & 1u)) sv[e] = 0xff800000u;
+            }
+            float m8[8];
 #pragma unroll
-            for (int e = 8; e < 32; e += 2) m4[(e >> 1) & 3] = fmaxf(fmaxf(m4[(e >> 1) & 3], __uint_as_float(s[e])), __uint_as_float(s[e + 1]));
-            const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale2;
+            for (int e = 0; e < 8; ++e) m8[e] = fmaxf(fmaxf(__uint_as_float(sv[e]), __uint_as_float(sv[e + 8])), __uint_as_float(sv[e + 16]));
+#pragma unroll
+            for (int e = 24; e < 56; e += 16)
+#pragma unroll
+              for (int x = 0; x < 8; ++x) m8[x] = fmaxf(fmaxf(m8[x], __uint_as_float(sv[e + x])), __uint_as_float(sv[e + 8 + x]));
+#pragma unroll
+            for (int x = 0; x < 8; ++x) m8[x] = fmaxf(m8[x], __uint_as_float(sv[56 + x]));
+            const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])), fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * a.scale2;
             const bool up = mx > ref + kGap || (ref == -INFINITY && mx > ref);
             if (__any_sync(FULL, up)) {                    // (alike in the warp: accesses to tensor memory are the whole warp's)
               const float to = up ? ceilf(mx) : ref, f = up && ref != -INFINITY ? power_of_two(ref - to) : 1.f;
               ref = to;
               if (__any_sync(FULL, f != 1.f)) {
                 const uint64_t f2 = pair2(f, f);
-                l2[0] = fma2(l2[0], f2, 0); l2[1] = fma2(l2[1], f2, 0);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                if (i + 1 < slabs) tmem_regs_ready(ahead);
-                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-#pragma unroll 1
-                for (int v = 0; v < i; ++v) {              // P of this block so far
-                  uint32_t r[16];
-                  tmem_ld16(scol + 16 * v, r);
 #pragma unroll
-                  for (int e = 0; e < 16; ++e) {
-                    const float2 pv = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r[e]));
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(pv.x * f, pv.y * f);
-                    r[e] = *reinterpret_cast<const uint32_t*>(&h);
-                  }
-                  tmem_st16(scol + 16 * v, r);
-                }
-                if (j) {
-                  wait_pv(cS);
-#pragma unroll 1
-                  for (int v = 0; v < C::OC; v += 16) {
-                    uint32_t r[16];
-                    tmem_ld16(o_col + tile * C::OC + lane_at + v, r);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
-                    tmem_st16(o_col + tile * C::OC + lane_at + v, r);
-                  }
-                }
+                for (int x = 0; x < 4; ++x) l2[x] = fma2(l2[x], f2, 0);
+                if (j) wait_pv(cS);
+                rescale(scol, 2 * i, o_col + tile * C::OC + lane_at, j ? C::OC : 0, f);
               }
             }
             const float neg = ref == -INFINITY ? 0.f : -ref;
             const uint64_t neg2 = pair2(neg, neg);
-            uint32_t pk[16];
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float2 y = unpair(fma2(pair2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, neg2));
+            for (int e = 0; e < 64; e += 2) {
+              const float2 y = unpair(fma2(pair2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), scale2, neg2));
               const float p0 = ex2(y.x), p1 = ex2(y.y);
-              l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], pair2(p0, p1));
+              l2[(e >> 1) & 3] = add2(l2[(e >> 1) & 3], pair2(p0, p1));
               const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-              pk[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+              sv[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            tmem_st16(scol + 16 * i, pk);
-          };
-#pragma unroll 1
-          for (int i = 0; i < slabs; i += 2) {
-            slab(i, sv[0], sv[1]);
-            if (i + 1 < slabs) slab(i + 1, sv[1], sv[0]);
+            tmem_st16(scol + 32 * i, sv);
+            tmem_st16(scol + 32 * i + 16, sv + 16);
           }
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           fence_before();
@@ -699,7 +741,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           bar_arrive(&sm.p_ready[x]);
           ++cS;
         }
-        const float2 la = unpair(l2[0]), lb = unpair(l2[1]);
+        const float2 la = unpair(add2(l2[0], l2[1])), lb = unpair(add2(l2[2], l2[3]));
         const float sum = (la.x + la.y) + (lb.x + lb.y);
         if (NT == 1) {
           wait(&sm.stat_free, (n & 1) ^ 1);
@@ -724,10 +766,12 @@ int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
   typedef Cfg<DP, SHARED> C;
   TcArgs g;
   g.a = a;
-  g.items = units * a.s.Hk * a.nsplit * C::HALVES;
+  const int64_t items = units * a.s.Hk * a.nsplit * C::HALVES;
+  if (items > 0x7fffffff - 148) return TSV_ERR_LIMIT;
+  g.items = (int32_t)items;
   if (!ensure_smem((const void*)attn_tc_kernel<DP, SHARED>, C::SMEM)) return TSV_ERR_CUDA;
   TSV_PREP((attn_tc_kernel<DP, SHARED>));
-  const int64_t grid = g.items < 148 ? g.items : 148;
+  const int grid = g.items < 148 ? g.items : 148;
   attn_tc_kernel<DP, SHARED><<<(unsigned)grid, kTcThreads, C::SMEM, st>>>(g);
   count_launch();
   return TSV_OK;
