@@ -12,8 +12,8 @@ from typing import Optional, Sequence
 import torch
 
 from . import binding as tsv
-from .binding import TsvError, _aligned, _lib, _p, _stream
-from .tokens import ST_PAGE, ST_POOL, _check  # noqa: F401
+from .binding import TsvError, _aligned, _lib, _p
+from .tokens import ST_PAGE, ST_POOL, _bad, _device, _flat, _i32, _on  # noqa: F401
 
 MAX_LIST = 1024
 
@@ -54,8 +54,10 @@ class PagePool:
                 raise TsvError(tsv.ERR_SHAPE, f"PagePool: a {what} must be contiguous on {page_table.device} and divide into {parts}, got {tuple(t.shape)}")
         arrays = lambda ts, parts: (CPageArray * max(1, len(ts)))(*[CPageArray(t.data_ptr(), t.numel() // parts * t.element_size()) for t in ts])
         self._planes, self._rows = arrays(self.planes, n), arrays(self.rows, slots)
-        self.c = CPagePool(_check("page_table", page_table, torch.int32, slots * max_pages), _check("ref", ref, torch.int32, n), slots, max_pages, n,
+        dev = page_table.get_device()
+        self.c = CPagePool(_flat("page_table", page_table, _i32, slots * max_pages, dev), _flat("ref", ref, _i32, n, dev), slots, max_pages, n,
                            page_tokens, _at(self._planes), _at(self._rows), len(self.planes), len(self.rows))
+        self.device = dev
 
     @staticmethod
     def of_layers(caches: Sequence[tsv.LayerCache], ref: Optional[torch.Tensor] = None) -> "PagePool":
@@ -80,38 +82,49 @@ def alloc_workspace(pool: PagePool) -> torch.Tensor:
     return torch.empty(n + 256, dtype=torch.uint8, device=pool.page_table.device)
 
 
-def _list(n: int, *lists: torch.Tensor):
-    return [_check("list", t, torch.int32, n) for t in lists]
-
-
-def _raise(r: int, where: str) -> None:
-    if r:
-        raise TsvError(r, where)
+def _here(pool: PagePool, workspace: Optional[torch.Tensor] = None) -> int:
+    dev = _device()
+    if pool.device != dev:
+        _bad("pool", "a pool", pool.page_table)
+    if workspace is not None and workspace.get_device() != dev:
+        _bad("workspace", "a workspace", workspace)
+    return dev
 
 
 def pages_assign(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor,
                  stream=None) -> None:
     """Logical pages first[i] .. last[i] - 1 of slots[i] that have no page get the free ones with the lowest numbers."""
-    n = slots.numel()
+    n, dev = slots.numel(), _here(pool, workspace)
     wp, wn = _aligned(workspace)
-    _raise(_lib.pages_assign(_at(pool.c), n, *_list(n, slots, first, last), wp, wn, *_list(n, status), _stream(stream)), "pages_assign")
+    r = _lib.pages_assign(_at(pool.c), n, _flat("slots", slots, _i32, n, dev), _flat("first", first, _i32, n, dev), _flat("last", last, _i32, n, dev), wp, wn,
+                          _flat("status", status, _i32, n, dev), _on(stream, dev))
+    if r:
+        raise TsvError(r, "pages_assign")
 
 
 def pages_free(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """slots[i] gives up its logical pages first[i] .. last[i] - 1."""
-    n = slots.numel()
-    _raise(_lib.pages_free(_at(pool.c), n, *_list(n, slots, first, last, status), _stream(stream)), "pages_free")
+    n, dev = slots.numel(), _here(pool)
+    r = _lib.pages_free(_at(pool.c), n, _flat("slots", slots, _i32, n, dev), _flat("first", first, _i32, n, dev), _flat("last", last, _i32, n, dev),
+                        _flat("status", status, _i32, n, dev), _on(stream, dev))
+    if r:
+        raise TsvError(r, "pages_free")
 
 
 def pages_fork(pool: PagePool, src: torch.Tensor, dst: torch.Tensor, L: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """dst[i], a slot without pages, becomes a copy of src[i] with L[src[i]] tokens: full pages shared, the last one and the rows copied."""
-    n = src.numel()
+    n, dev = src.numel(), _here(pool, workspace)
     wp, wn = _aligned(workspace)
-    _raise(_lib.pages_fork(_at(pool.c), n, *_list(n, src, dst), _check("L", L, torch.int32, pool.c.slots), wp, wn, *_list(n, status), _stream(stream)),
-           "pages_fork")
+    r = _lib.pages_fork(_at(pool.c), n, _flat("src", src, _i32, n, dev), _flat("dst", dst, _i32, n, dev), _flat("L", L, _i32, pool.c.slots, dev), wp, wn,
+                        _flat("status", status, _i32, n, dev), _on(stream, dev))
+    if r:
+        raise TsvError(r, "pages_fork")
 
 
 def pages_compact(pool: PagePool, n_used: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """The used pages move to the lowest numbers, contents, table and counts; n_used (int32, 1 value) becomes their number."""
+    dev = _here(pool, workspace)
     wp, wn = _aligned(workspace)
-    _raise(_lib.pages_compact(_at(pool.c), _check("n_used", n_used, torch.int32, 1), wp, wn, _stream(stream)), "pages_compact")
+    r = _lib.pages_compact(_at(pool.c), _flat("n_used", n_used, _i32, 1, dev), wp, wn, _on(stream, dev))
+    if r:
+        raise TsvError(r, "pages_compact")

@@ -12,12 +12,13 @@ from __future__ import annotations
 
 import ctypes as C
 from dataclasses import dataclass, field
+from struct import Struct
 from typing import Optional
 
 import torch
 
 from . import binding as tsv
-from .binding import TsvError, _aligned, _lib, _p, _stream
+from .binding import TsvError, _aligned, _lib, _p
 
 ST_PAGE, ST_POOL = 64, 128
 
@@ -49,6 +50,15 @@ _lib.token_commit.restype = C.c_int
 _lib.token_commit.argtypes = [_p, _p, _p, _p, _p, C.c_int32, _p, _p, _p]
 
 _at = C.addressof
+# The structs of a call as bytes: ctypes takes some microseconds to make one, these are made anew for every call.
+_pack_cache, _pack_batch, _pack_rows = Struct("3PqP2i").pack, Struct("3Pq").pack, Struct("3P3q").pack
+assert Struct("3PqP2i").size == C.sizeof(CTokCache) and Struct("3Pq").size == C.sizeof(CTokBatch) and Struct("3P3q").size == C.sizeof(CTokRows)
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_i32, _i64, _f32 = torch.int32, torch.int64, torch.float32
+
+
+def _on(stream, dev: int) -> int:
+    return _raw_stream(dev) if stream is None else stream.cuda_stream
 
 
 @dataclass
@@ -74,28 +84,30 @@ class TokenShape:
                            self.max_n, self.max_L, float(self.sm_scale), 0)
 
 
-def _check(where: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int) -> int:
-    """Pointer of a contiguous tensor of at least `numel` elements on the current device (None: 0)."""
-    if t is None:
-        return 0
-    if t.dtype != dtype or t.numel() < numel or not t.is_contiguous():
-        raise TsvError(tsv.ERR_SHAPE, f"{where}: expected a contiguous {dtype} tensor of {numel} elements, got {t.dtype} {tuple(t.shape)}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise TsvError(tsv.ERR_SHAPE, f"{where}: the tensor is on {t.device}, not on the current CUDA device")
+def _bad(where: str, expected: str, t) -> None:
+    got = f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else repr(t)
+    raise TsvError(tsv.ERR_SHAPE, f"{where}: expected {expected} on the current CUDA device, got {got}")
+
+
+def _flat(where: str, t: torch.Tensor, dtype: torch.dtype, numel: int, dev: int) -> int:
+    """Pointer of a contiguous tensor of at least `numel` elements on device dev."""
+    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or t.get_device() != dev:
+        _bad(where, f"a contiguous {dtype} tensor of {numel} elements", t)
     return t.data_ptr()
 
 
-def _vectors(where: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, d: int):
+def _maybe(where: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, dev: int) -> int:
+    return 0 if t is None else _flat(where, t, dtype, numel, dev)
+
+
+def _vectors(where: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, d: int, dev: int):
     """Pointer and row stride of a [>= rows, heads, d] tensor whose heads follow each other in a row."""
     s = t.shape
-    if t.dtype != dtype or len(s) != 3 or s[0] < rows or s[1] != heads or s[2] != d:
-        raise TsvError(tsv.ERR_SHAPE, f"{where}: expected a {dtype} tensor [{rows}, {heads}, {d}], got {t.dtype} {tuple(s)}")
-    st = t.stride()
-    if (d > 1 and st[2] != 1) or (heads > 1 and st[1] != d):
-        raise TsvError(tsv.ERR_SHAPE, f"{where}: the heads of a row must follow each other, strides are {st}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise TsvError(tsv.ERR_SHAPE, f"{where}: the tensor is on {t.device}, not on the current CUDA device")
-    return t.data_ptr(), (st[0] if s[0] > 1 else heads * d)
+    if t.dtype is dtype and len(s) == 3 and s[0] >= rows and s[1] == heads and s[2] == d and t.get_device() == dev:
+        ld, hs, es = t.stride()
+        if es == 1 and (hs == d or heads == 1):
+            return t.data_ptr(), (ld if s[0] > 1 else heads * d)
+    _bad(where, f"a {dtype} tensor [{rows}, {heads}, {d}] whose rows are contiguous", t)
 
 
 @dataclass
@@ -105,9 +117,9 @@ class TokenBatch:
     n: torch.Tensor                           # [B] int32
     parent: Optional[torch.Tensor] = None     # [rows] int32, node of the same sequence, -1 for node 0
 
-    def struct(self, B: int, rows: int) -> CTokBatch:
-        return CTokBatch(_check("row0", self.row0, torch.int64, B), _check("n", self.n, torch.int32, B),
-                         _check("parent", self.parent, torch.int32, rows) or None, rows)
+    def pack(self, B: int, rows: int, dev: int) -> bytes:
+        return _pack_batch(_flat("row0", self.row0, _i64, B, dev), _flat("n", self.n, _i32, B, dev),
+                           0 if self.parent is None else _flat("parent", self.parent, _i32, rows, dev), rows)
 
 
 @dataclass
@@ -124,16 +136,12 @@ class TokenCache:
         """The token-level KV of a verify layer: its window ring, or its pool's third physical layer (n_sink = 0 for a ring)."""
         return TokenCache(cache.L, cache.win_kv, None, cache.page_table, cache.page_tokens)
 
-    def struct(self, shape: TokenShape) -> CTokCache:
-        dt, width = shape.torch_dtype, shape.Hk * shape.d
-        rows = self.k.numel() // width
-        k = _check("cache.k", self.k, dt, width)
-        v = _check("cache.v", self.v, dt, rows * width)
-        pt, mp = None, 0
-        if self.page_table is not None:
-            mp = self.page_table.shape[1]
-            pt = _check("page_table", self.page_table, torch.int32, shape.B * mp)
-        return CTokCache(_check("L", self.L, torch.int32, shape.B), k, v or None, rows, pt, self.page_tokens, mp)
+    def pack(self, shape: TokenShape, dev: int) -> bytes:
+        dt, width, k, table = shape.torch_dtype, shape.Hk * shape.d, self.k, self.page_table
+        rows = k.numel() // width
+        return _pack_cache(_flat("L", self.L, _i32, shape.B, dev), _flat("cache.k", k, dt, width, dev), _maybe("cache.v", self.v, dt, rows * width, dev), rows,
+                           0 if table is None else _flat("page_table", table, _i32, shape.B * table.shape[1], dev), self.page_tokens,
+                           0 if table is None else table.shape[1])
 
 
 def alloc_token_cache(shape: TokenShape, values: bool = True, device="cuda") -> TokenCache:
@@ -167,47 +175,53 @@ def qk_norm_rope(shape: TokenShape, L: torch.Tensor, batch: TokenBatch, q: Optio
                  inv_freq: Optional[torch.Tensor], first: int, pairs: bool, status: torch.Tensor, stream=None) -> None:
     """q [rows, H, d], k [rows, Hk, d] -> q_out, k_out (may be the inputs): per-head RMS norm with weights [d] fp32, then dims first ..
     first + 2 len(inv_freq) - 1 rotated to the tokens' positions; pairs: neighbouring dims turn together (else i and i + rot / 2)."""
-    dt, f32 = shape.torch_dtype, torch.float32
+    dt, dev = shape.torch_dtype, _device()
     some = q if q is not None else k
     if some is None:
         raise TsvError(tsv.ERR_NULL, "qk_norm_rope")
-    rows = some.shape[0]
-    b = batch.struct(shape.B, rows)
-    qi = qo = ki = ko = (None, 0)
+    rows, H, Hk, d = some.shape[0], shape.H, shape.Hk, shape.d
+    qp = qo = kp = ko = ql = qol = kl = kol = 0
     if q is not None:
-        qi, qo = _vectors("q", q, dt, rows, shape.H, shape.d), _vectors("q_out", q_out, dt, rows, shape.H, shape.d)
+        (qp, ql), (qo, qol) = _vectors("q", q, dt, rows, H, d, dev), _vectors("q_out", q_out, dt, rows, H, d, dev)
     if k is not None:
-        ki, ko = _vectors("k", k, dt, rows, shape.Hk, shape.d), _vectors("k_out", k_out, dt, rows, shape.Hk, shape.d)
-    io = CTokRows(qi[0], ki[0], None, qi[1], ki[1], 0)
+        (kp, kl), (ko, kol) = _vectors("k", k, dt, rows, Hk, d, dev), _vectors("k_out", k_out, dt, rows, Hk, d, dev)
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    _raise(_lib.qk_norm_rope(_at(shape.c), _check("L", L, torch.int32, shape.B), _at(b), _at(io), _check("wq", wq, f32, shape.d),
-                             _check("wk", wk, f32, shape.d), eps, _check("inv_freq", inv_freq, f32, rot // 2), rot, first, pairs, qo[0], qo[1],
-                             ko[0], ko[1], _check("status", status, torch.int32, shape.B), _stream(stream)), "qk_norm_rope")
+    r = _lib.qk_norm_rope(_at(shape.c), _flat("L", L, _i32, shape.B, dev), batch.pack(shape.B, rows, dev), _pack_rows(qp, kp, 0, ql, kl, 0),
+                          _maybe("wq", wq, _f32, d, dev), _maybe("wk", wk, _f32, d, dev), eps, _maybe("inv_freq", inv_freq, _f32, rot // 2, dev), rot, first,
+                          pairs, qo, qol, ko, kol, _flat("status", status, _i32, shape.B, dev), _on(stream, dev))
+    if r:
+        raise TsvError(r, "qk_norm_rope")
 
 
-def _kv(shape: TokenShape, q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor]) -> CTokRows:
-    dt, rows = shape.torch_dtype, k.shape[0]
-    qp, qs = _vectors("q", q, dt, rows, shape.H, shape.d) if q is not None else (None, 0)
-    kp, ks = _vectors("k", k, dt, rows, shape.Hk, shape.d)
-    vp, vs = _vectors("v", v, dt, rows, shape.Hk, shape.d) if v is not None else (None, 0)
-    return CTokRows(qp, kp, vp, qs, ks, vs)
+def _kv(shape: TokenShape, q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], dev: int) -> bytes:
+    dt, rows, Hk, d = shape.torch_dtype, k.shape[0], shape.Hk, shape.d
+    qp, qs = _vectors("q", q, dt, rows, shape.H, d, dev) if q is not None else (0, 0)
+    kp, ks = _vectors("k", k, dt, rows, Hk, d, dev)
+    vp, vs = _vectors("v", v, dt, rows, Hk, d, dev) if v is not None else (0, 0)
+    return _pack_rows(qp, kp, vp, qs, ks, vs)
 
 
 def window_sink_attn(shape: TokenShape, cache: TokenCache, batch: TokenBatch, q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor],
                      out: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """out [rows, H, d]: every new token's attention to the sinks and its window, committed (cache) and new (k, v) tokens."""
-    rows = k.shape[0]
-    b, c, io = batch.struct(shape.B, rows), cache.struct(shape), _kv(shape, q, k, v)
+    rows, dev = k.shape[0], _device()
+    if workspace.get_device() != dev:
+        _bad("workspace", "a workspace", workspace)
     wp, wn = _aligned(workspace)
-    _raise(_lib.window_sink_attn(_at(shape.c), _at(c), _at(b), _at(io), _check("out", out, shape.torch_dtype, rows * shape.H * shape.d), wp, wn,
-                                 _check("status", status, torch.int32, shape.B), _stream(stream)), "window_sink_attn")
+    r = _lib.window_sink_attn(_at(shape.c), cache.pack(shape, dev), batch.pack(shape.B, rows, dev), _kv(shape, q, k, v, dev),
+                              _flat("out", out, shape.torch_dtype, rows * shape.H * shape.d, dev), wp, wn, _flat("status", status, _i32, shape.B, dev),
+                              _on(stream, dev))
+    if r:
+        raise TsvError(r, "window_sink_attn")
 
 
 def token_commit(shape: TokenShape, cache: TokenCache, batch: TokenBatch, k: torch.Tensor, v: Optional[torch.Tensor], status: torch.Tensor,
                  path: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, stream=None) -> None:
     """Rows of new tokens (all n[b] of a sequence, or the first count[b] nodes of path[b]) into the cache; L[b] grows by them."""
-    b, c, io = batch.struct(shape.B, k.shape[0]), cache.struct(shape), _kv(shape, None, k, v)
+    dev = _device()
     ld = 0 if path is None else path.shape[1]
-    _raise(_lib.token_commit(_at(shape.c), _at(c), _at(b), _at(io), _check("path", path, torch.int32, shape.B * ld) or None, ld,
-                             _check("count", count, torch.int32, shape.B) or None, _check("status", status, torch.int32, shape.B), _stream(stream)),
-           "token_commit")
+    r = _lib.token_commit(_at(shape.c), cache.pack(shape, dev), batch.pack(shape.B, k.shape[0], dev), _kv(shape, None, k, v, dev),
+                          _maybe("path", path, _i32, shape.B * ld, dev), ld, _maybe("count", count, _i32, shape.B, dev),
+                          _flat("status", status, _i32, shape.B, dev), _on(stream, dev))
+    if r:
+        raise TsvError(r, "token_commit")

@@ -166,14 +166,17 @@ def test_wrappers_refuse_what_the_library_cannot_see(api):
     for dt, rows, heads, t in [(torch.bfloat16, 5, 4, z(5, 4, 16, dt=torch.float32)), (torch.bfloat16, 5, 4, z(4, 4, 16)), (torch.bfloat16, 5, 4, z(5, 2, 16)),
                                (torch.bfloat16, 5, 4, z(5, 64)), (torch.bfloat16, 5, 4, z(5, 16, 4).transpose(1, 2)), (torch.bfloat16, 5, 4, z(5, 4, 16))]:
         with pytest.raises(tsv.TsvError) as e:
-            tk._vectors("q", t, dt, rows, heads, 16)
+            tk._vectors("q", t, dt, rows, heads, 16, 0)
         assert e.value.code == tsv.ERR_SHAPE
     with pytest.raises(tsv.TsvError):
-        tk.TokenBatch(i32(2), i32(2)).struct(2, 5)
+        tk.TokenBatch(i32(2), i32(2)).pack(2, 5, -1)
     with pytest.raises(tsv.TsvError):
-        batch.struct(3, 5)
+        batch.pack(3, 5, -1)
     with pytest.raises(tsv.TsvError):
-        tk.token_commit(s, tk.alloc_token_cache(s, device="cpu"), batch, z(5, 2, 16), z(5, 2, 16), i32(2))
+        batch.pack(2, 5, 0)
+    with pytest.raises(tsv.TsvError):
+        tk.alloc_token_cache(s, device="cpu").pack(s, 0)
+    assert len(batch.pack(2, 5, -1)) == C.sizeof(tk.CTokBatch) and len(tk.alloc_token_cache(s, device="cpu").pack(s, -1)) == C.sizeof(tk.CTokCache)
     with pytest.raises(tsv.TsvError):
         tk.TokenShape("fp16", 1, 1, 1, 8, 1)
     with pytest.raises(tsv.TsvError):
