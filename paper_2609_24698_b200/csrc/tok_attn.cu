@@ -20,11 +20,11 @@ using tc::smem_u32;
 constexpr int kRows = 16;             // query rows of a tile
 constexpr int kThreads = 128;
 
-// Keys of this split: whole blocks of KB keys, the same number for every split.
-__device__ __forceinline__ void split_range(const AttnArgs& a, const TileList& t, int KB, int& k0, int& k1) {
-  const int blocks = (t.nk + KB - 1) / KB, per = (blocks + a.nsplit - 1) / a.nsplit;
-  k0 = min(t.nk, (int)blockIdx.z * per * KB);
-  k1 = min(t.nk, k0 + per * KB);
+// Keys of this share: a multiple of 16, the same number for every share.
+__device__ __forceinline__ void split_range(const AttnArgs& a, const TileList& t, int& k0, int& k1) {
+  const int per = ((t.nk + a.nsplit - 1) / a.nsplit + 15) & ~15;
+  k0 = min(t.nk, (int)blockIdx.z * per);
+  k1 = min(t.nk, k0 + per);
 }
 __device__ __forceinline__ size_t part_index(const AttnArgs& a) {      // of this CTA's first partial row
   return (((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.nsplit + blockIdx.z) * kRows;
@@ -53,26 +53,126 @@ __device__ __forceinline__ void row_facts(const AttnArgs& a, const TileList& t, 
   p = t.L + (a.bt.parent ? depth[tok] : tok);
   an = a.bt.parent ? anc[tok] : 0;
 }
-// Those rows of `bad` (a bit per row) that see something not finite, by their definition, a warp each.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t saddr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float2 ld_rank2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_rank4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+// What both kernels keep of a tile, and its share of the result: sum of weights and of weighted values at the maximum m.
+struct TileCtl {
+  float2 ml[kRows];
+  int depth[TSV_MAX_D];
+  uint32_t anc[TSV_MAX_D];
+  int pos[kRows];
+  uint32_t row_anc[kRows];
+  TileList t;
+  uint32_t bad;
+};
+
+// The tile of this CTA; false (alike in all CTAs of a cluster) where there is nothing to attend to.
 template <typename T>
-__device__ __forceinline__ void exact_rows(const AttnArgs& a, const TileList& t, const int* depth, const uint32_t* anc, uint32_t bad, int k0, int k1) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int r = warp; r < t.nr; r += kThreads / 32) {
-    if (!(bad >> r & 1u)) continue;
-    int p;
-    uint32_t an;
-    row_facts(a, t, depth, anc, r, p, an);
-    float m, l, o[16];
-    if (!exact_row<T>(a, t, depth, query_row<T>(a, t, r), p, an, k0, k1, m, l, o)) continue;
-    if (a.nsplit > 1) {
-      const size_t at = part_index(a) + r;
-      for (int i = 0; i < 16; ++i) if (lane + 32 * i < a.s.d) a.po[at * a.s.d + lane + 32 * i] = o[i];
-      if (lane == 0) a.pml[at] = make_float2(m, l);
+__device__ __forceinline__ bool begin_tile(const AttnArgs& a, TileCtl& sm) {
+  if (threadIdx.x < 32) {
+    const TileList t = make_list(a, blockIdx.x, blockIdx.y, kRows, sm.depth, sm.anc);
+    if (threadIdx.x == 0) { sm.t = t; sm.bad = 0; }
+  }
+  __syncthreads();
+  const TileList& t = sm.t;
+  if (t.ok != 1) {
+    if (t.ok == 2 && (a.nsplit == 1 || (a.cluster && blockIdx.z == 0))) zero_rows<T>(a, t);
+    return false;
+  }
+  if (threadIdx.x < kRows) {
+    int p = 0;
+    uint32_t an = 0;
+    if ((int)threadIdx.x < t.nr) row_facts(a, t, sm.depth, sm.anc, threadIdx.x, p, an);
+    sm.pos[threadIdx.x] = p; sm.row_anc[threadIdx.x] = an;
+  }
+  return true;
+}
+
+// From o [16][ld] and sm.ml in shared memory, written by this CTA before, to the output: through the partial outputs, or at once, the
+// shares of a cluster's CTAs joined in order.  Rows of sm.bad that see something not finite are computed by definition first.
+template <typename T>
+__device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* o, int ld, int k0, int k1) {
+  const TileList& t = sm.t;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, d = a.s.d;
+  __syncthreads();
+  if (sm.bad) {
+    for (int r = warp; r < t.nr; r += kThreads / 32) {
+      if (!(sm.bad >> r & 1u)) continue;
+      float m, l, x[16];
+      if (!exact_row<T>(a, t, sm.depth, query_row<T>(a, t, r), sm.pos[r], sm.row_anc[r], k0, k1, m, l, x)) continue;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) if (lane + 32 * i < d) o[r * ld + lane + 32 * i] = x[i];
+      if (lane == 0) sm.ml[r] = make_float2(m, l);
+    }
+    __syncthreads();
+  }
+  const int nv = d / 4;
+  if (a.nsplit > 1 && !a.cluster) {
+    const size_t at = part_index(a);
+    for (int i = tid; i < t.nr * nv; i += kThreads) {
+      const int r = i / nv, c = i % nv * 4;
+      *reinterpret_cast<float4*>(a.po + (at + r) * d + c) = *reinterpret_cast<const float4*>(o + r * ld + c);
+    }
+    if (tid < t.nr) a.pml[at + tid] = sm.ml[tid];
+    return;
+  }
+  const int shares = a.nsplit;
+  if (shares > 1) cluster_sync();                         // every CTA's share is there
+  const uint32_t o_at = smem_u32(o), ml_at = smem_u32(sm.ml);
+  for (int i = tid + kThreads * (shares > 1 ? (int)blockIdx.z : 0); i < t.nr * nv; i += kThreads * shares) {
+    const int r = i / nv, c = i % nv * 4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    if (shares == 1) {
+      x = *reinterpret_cast<const float4*>(o + r * ld + c);
+      l = sm.ml[r].y;
     } else {
-      T* out = out_row<T>(a, t, r);
-      for (int i = 0; i < 16; ++i) if (lane + 32 * i < a.s.d) out[lane + 32 * i] = from_f<T>(o[i] / l);    // (every score -inf: 0 / 0, as the formula has it)
+      float2 ml[8];
+      float4 v[8];
+      float m = -INFINITY;
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (s < shares) {
+          ml[s] = ld_rank2(at_rank(ml_at + r * 8, s));
+          v[s] = ld_rank4(at_rank(o_at + (r * ld + c) * 4, s));
+          m = fmaxf(m, ml[s].x);
+        }
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (s < shares && !(ml[s].x == -INFINITY && ml[s].y == 0.f)) {           // (else nothing seen)
+          const float w = exp2f(ml[s].x - m);
+          l = fmaf(ml[s].y, w, l);
+          x.x = fmaf(v[s].x, w, x.x); x.y = fmaf(v[s].y, w, x.y); x.z = fmaf(v[s].z, w, x.z); x.w = fmaf(v[s].w, w, x.w);
+        }
+    }
+    const float inv = 1.f / l;
+    T* out = out_row<T>(a, t, r) + c;
+    if (sizeof(T) == 4) {
+      *reinterpret_cast<float4*>(out) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    } else {
+      __nv_bfloat162 h[2] = {__floats2bfloat162_rn(x.x * inv, x.y * inv), __floats2bfloat162_rn(x.z * inv, x.w * inv)};
+      *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(h);
     }
   }
+  if (shares > 1) cluster_sync();                         // nobody's share is read any more
 }
 
 __device__ __forceinline__ void ldsm4(uint32_t* r, uint32_t addr) {
@@ -97,108 +197,106 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 // Four warps: of a block of KB keys each computes the scores of a quarter (16 rows x KB / 4 keys over all of d), the row maxima go
 // through shared memory, then each adds the whole block's P V to its quarter of the output columns (d / 4: 16 rows x 128 columns are
 // 64 registers at d = 512).  P is rounded to bf16 for the product (half a step, 2^-9, of a weight; the sum of the weights is of the
-// unrounded ones); scores, maxima, sums and the output are fp32.  Rows of K and V come by 16-byte asynchronous copies, the next
-// block under the arithmetic of the current one, through the page table or from the new rows: 16-byte chunks of a row are stored at
-// chunk ^ (row & 7), which keeps every ldmatrix free of bank conflicts.  DP: d rounded up to 64, 128, 256 or 512, the rest zero.
-template <int DP, int KB, bool SHARED>
+// unrounded ones); scores, maxima, sums and the output are fp32.  Rows of K and V come by 16-byte asynchronous copies, ST - 1 blocks
+// ahead of the arithmetic (a window of 32 k tokens streams from HBM: that much has to be under way), through the page table or from the
+// new rows, whose addresses are worked out a block before their copies: 16-byte chunks of a row are stored at chunk ^ (row & 7), which
+// keeps every ldmatrix free of bank conflicts.  DP: d rounded up to 64, 128, 256 or 512, the rest zero.
+template <int DP, bool SHARED>
+struct MmaCfg {
+  static constexpr int KB = DP <= 128 ? 64 : 32;
+  static constexpr int ST = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 3) : DP == 256 ? (SHARED ? 4 : 3) : SHARED ? 4 : 2;
+};
+template <int DP, bool SHARED>
 struct MmaSmem {
+  static constexpr int KB = MmaCfg<DP, SHARED>::KB, ST = MmaCfg<DP, SHARED>::ST;
   alignas(16) bf16 q[kRows * DP];
-  bf16 k[2][KB * DP];
-  bf16 v[SHARED ? 1 : 2][SHARED ? 8 : KB * DP];
+  bf16 k[ST][KB * DP];                // (and the output at the end)
+  bf16 v[SHARED ? 1 : ST][SHARED ? 8 : KB * DP];
   bf16 p[kRows * KB];
-  int64_t code[2][KB];
+  const bf16* row[ST + 1][SHARED ? 1 : 2][KB];      // where a block's rows begin (nullptr: nothing there)
   float red[4][kRows], sum[4][kRows];
-  int depth[TSV_MAX_D];
-  uint32_t anc[TSV_MAX_D];
-  int pos[kRows];
-  uint32_t row_anc[kRows];
-  TileList t;
-  uint32_t bad;
-  int missing[2];                     // a key of the block has no page
+  TileCtl c;
+  int missing[ST + 1];                // a key of the block has no page
 };
 
-template <int DP, int KB, bool SHARED>
+template <int DP, bool SHARED>
 __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  typedef MmaSmem<DP, KB, SHARED> Sm;
+  typedef MmaSmem<DP, SHARED> Sm;
   Sm& sm = *reinterpret_cast<Sm*>(smem_raw);
+  constexpr int KB = Sm::KB, ST = Sm::ST;
   constexpr int CH = DP / 8, KW = KB / 4, NT = KW / 8;    // 16-byte chunks of a row; keys of a warp, in tiles of 8
   constexpr int CW = DP / 4, CT = CW / 8;                 // output columns of a warp, in tiles of 8
+  static_assert(sizeof(float) * kRows * DP <= sizeof(sm.k), "the output lies in the blocks' place");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (warp == 0) {
-    const TileList t = make_list(a, blockIdx.x, blockIdx.y, kRows, sm.depth, sm.anc);
-    if (lane == 0) { sm.t = t; sm.bad = 0; sm.missing[0] = sm.missing[1] = 0; }
-  }
-  __syncthreads();
-  const TileList& t = sm.t;
-  if (t.ok != 1) {
-    if (t.ok == 2 && a.nsplit == 1) zero_rows<bf16>(a, t);
-    return;
-  }
+  if (tid <= ST) sm.missing[tid] = 0;
+  if (!begin_tile<bf16>(a, sm.c)) return;
+  const TileList& t = sm.c.t;
   int k0, k1;
-  split_range(a, t, KB, k0, k1);
-  if (tid < kRows) {
-    int p = 0;
-    uint32_t an = 0;
-    if (tid < t.nr) row_facts(a, t, sm.depth, sm.anc, tid, p, an);
-    sm.pos[tid] = p; sm.row_anc[tid] = an;
-  }
-  auto codes = [&](int j) {                               // the rows behind block j
-    if (tid >= KB) return;
-    const int kk = k0 + j * KB + tid;
+  split_range(a, t, k0, k1);
+  const int nb = (k1 - k0 + KB - 1) / KB;
+  auto find = [&](int j) {                                // the rows behind block j
+    if (tid >= KB || j >= nb) return;
+    const int kk = k0 + j * KB + tid, slot = j % (ST + 1);
     int64_t code = -1;
     if (kk < k1) {
       code = list_row(a, t, kk);
-      if (code == -1) { sm.missing[j & 1] = 1; atomicOr(a.status + t.b, TSV_ST_PAGE); }
+      if (code == -1) { sm.missing[slot] = 1; atomicOr(a.status + t.b, TSV_ST_PAGE); }
     }
-    sm.code[j & 1][tid] = code;
+    sm.row[slot][0][tid] = code == -1 ? nullptr : row_ptr<bf16>(a, t.hk, code, false);
+    if (!SHARED) sm.row[slot][SHARED ? 0 : 1][tid] = code == -1 ? nullptr : row_ptr<bf16>(a, t.hk, code, true);
   };
   const int dch = a.s.d / 8;
   auto load = [&](int j) {
-    const uint32_t ks = smem_u32(sm.k[j & 1]), vs = smem_u32(sm.v[SHARED ? 0 : j & 1]);
-    for (int i = tid; i < KB * CH; i += kThreads) {
-      const int r = i / CH, c = i % CH;
-      const int64_t code = sm.code[j & 1][r];
-      const bool live = code != -1 && c < dch;
-      const uint32_t at = (uint32_t)(r * CH + (c ^ (r & 7))) * 16;
-      cp16(ks + at, live ? (const void*)(row_ptr<bf16>(a, t.hk, code, false) + c * 8) : a.in.k, live);
-      if (!SHARED) cp16(vs + at, live ? (const void*)(row_ptr<bf16>(a, t.hk, code, true) + c * 8) : a.in.k, live);
+    if (j < nb) {
+      const int slot = j % (ST + 1);
+      const uint32_t ks = smem_u32(sm.k[j % ST]), vs = smem_u32(sm.v[SHARED ? 0 : j % ST]);
+#pragma unroll 4
+      for (int i = tid; i < KB * CH; i += kThreads) {
+        const int r = i / CH, c = i % CH;
+        const bf16* kp = sm.row[slot][0][r];
+        const bool live = kp && c < dch;
+        const uint32_t at = (uint32_t)(r * CH + (c ^ (r & 7))) * 16;
+        cp16(ks + at, live ? (const void*)(kp + c * 8) : a.in.k, live);
+        if (!SHARED) {
+          const bf16* vp = sm.row[slot][SHARED ? 0 : 1][r];
+          cp16(vs + at, live ? (const void*)(vp + c * 8) : a.in.k, live);
+        }
+      }
     }
+    cp_commit();                                          // (a group per block, empty ones behind the last)
   };
-  const int nb = (k1 - k0 + KB - 1) / KB;
   const uint32_t qs = smem_u32(sm.q);
   for (int i = tid; i < kRows * CH; i += kThreads) {
     const int r = i / CH, c = i % CH;
     const bool live = r < t.nr && c < dch;
     cp16(qs + (uint32_t)(r * CH + (c ^ (r & 7))) * 16, live ? (const void*)(query_row<bf16>(a, t, r) + c * 8) : a.in.q, live);
   }
-  __syncthreads();
   const int g = lane >> 2, tc = lane & 3;
+  const uint32_t ps = smem_u32(sm.p);
+  for (int pass = 0; pass < 2; ++pass) {                  // (the second one only where a result is not finite)
+  for (int j = 0; j < ST; ++j) find(j);
+  __syncthreads();                                        // (the rows' facts too)
+  for (int j = 0; j + 1 < ST; ++j) load(j);
   int rp[2];
   uint32_t ra[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) { rp[h] = sm.pos[g + 8 * h]; ra[h] = sm.row_anc[g + 8 * h]; }
-  for (int pass = 0; pass < 2; ++pass) {                  // (the second one only where a result is not finite)
-  codes(0);
-  __syncthreads();
-  if (nb) load(0);
-  cp_commit();
+  for (int h = 0; h < 2; ++h) { rp[h] = sm.c.pos[g + 8 * h]; ra[h] = sm.c.row_anc[g + 8 * h]; }
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
   float o[CT][4];
 #pragma unroll
   for (int i = 0; i < CT; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-  const uint32_t ps = smem_u32(sm.p);
   for (int j = 0; j < nb; ++j) {
-    if (j + 1 < nb) codes(j + 1);
-    cp_wait<0>();
+    const int st = j % ST, slot = j % (ST + 1);
+    cp_wait<ST - 2>();
     if (pass)                                             // (what this thread has copied)
-      for (int i = tid; i < KB * CH; i += kThreads) make_finite<bf16>((SHARED ? sm.k[j & 1] : sm.v[SHARED ? 0 : j & 1]) + (i / CH * CH + (i % CH ^ (i / CH & 7))) * 8);
+      for (int i = tid; i < KB * CH; i += kThreads) make_finite<bf16>((SHARED ? sm.k[st] : sm.v[SHARED ? 0 : st]) + (i / CH * CH + (i % CH ^ (i / CH & 7))) * 8);
     __syncthreads();                                      // block j is here; everyone is done with block j - 1
-    if (j + 1 < nb) load(j + 1);
-    cp_commit();
-    const uint32_t ks = smem_u32(sm.k[j & 1]), vs = SHARED ? ks : smem_u32(sm.v[j & 1]);
+    load(j + ST - 1);
+    find(j + ST);
+    const uint32_t ks = smem_u32(sm.k[st]), vs = SHARED ? ks : smem_u32(sm.v[SHARED ? 0 : st]);
     // scores of this warp's keys
     float s[NT][4];
 #pragma unroll
@@ -224,15 +322,15 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
       }
     }
     // masks, row maxima over the block
-    const bool missing = sm.missing[j & 1] != 0;
+    const bool missing = sm.missing[slot] != 0;
     float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int h = e >> 1, key = warp * KW + i * 8 + 2 * tc + (e & 1), kk = k0 + j * KB + key;
-        bool see = kk < k1 && list_sees(a, t, sm.depth, rp[h], ra[h], kk);
-        if (missing && see) see = sm.code[j & 1][key] != -1;
+        bool see = kk < k1 && list_sees(a, t, sm.c.depth, rp[h], ra[h], kk);
+        if (missing && see) see = sm.row[slot][0][key] != nullptr;
         s[i][e] = see ? s[i][e] * a.scale2 : -INFINITY;
         mx[h] = fmaxf(mx[h], s[i][e]);
       }
@@ -269,7 +367,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
     for (int i = 0; i < CT; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] *= alpha[e >> 1];
-    if (tid == 0) sm.missing[j & 1] = 0;                  // (block j + 2's, set behind the next barrier)
+    if (tid == 0) sm.missing[slot] = 0;                   // (the block's after next, set behind the next barrier)
     __syncthreads();
     // P V, this warp's columns
 #pragma unroll
@@ -294,83 +392,82 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
     if (tc == 0) sm.sum[warp][g + 8 * h] = l[h];
   }
-  __syncthreads();
+  cp_wait<0>();
+  __syncthreads();                                        // (and everyone is done with the blocks)
+  float* os = reinterpret_cast<float*>(sm.k);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int r = g + 8 * h;
     l[h] = sm.sum[0][r] + sm.sum[1][r] + sm.sum[2][r] + sm.sum[3][r];
-    // (nothing of this split seen: {-inf, 0} and zeros; without splits every row sees its own key)
+    // (nothing of this share seen: {-inf, 0} and zeros; without shares every row sees its own key)
     bool bad = !is_finite(l[h]) || (m[h] == -INFINITY && a.nsplit == 1);
 #pragma unroll
-    for (int i = 0; i < CT; ++i) bad |= !is_finite(o[i][2 * h]) || !is_finite(o[i][2 * h + 1]);
-    if (bad && pass == 0 && r < t.nr) atomicOr(&sm.bad, 1u << r);
-    const float inv = a.nsplit > 1 ? 1.f : 1.f / l[h];
-    if (r < t.nr) {
-      bf16* out = out_row<bf16>(a, t, r);
-      const size_t at = part_index(a) + r;
-#pragma unroll
-      for (int i = 0; i < CT; ++i) {
-        const int col = warp * CW + i * 8 + 2 * tc;
-        if (col >= a.s.d) continue;
-        if (a.nsplit > 1) *reinterpret_cast<float2*>(a.po + at * a.s.d + col) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
-        else *reinterpret_cast<uint32_t*>(out + col) = pack2(o[i][2 * h] * inv, o[i][2 * h + 1] * inv);
-      }
-      if (a.nsplit > 1 && warp == 0 && tc == 0) a.pml[at] = make_float2(m[h], l[h]);
+    for (int i = 0; i < CT; ++i) {
+      bad |= !is_finite(o[i][2 * h]) || !is_finite(o[i][2 * h + 1]);
+      *reinterpret_cast<float2*>(os + r * DP + warp * CW + i * 8 + 2 * tc) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
     }
+    if (bad && pass == 0 && r < t.nr) atomicOr(&sm.c.bad, 1u << r);
+    if (warp == 0 && tc == 0) sm.c.ml[r] = make_float2(m[h], l[h]);
   }
   __syncthreads();
-  if (!sm.bad) return;
+  if (!sm.c.bad) break;
   }
-  exact_rows<bf16>(a, t, sm.depth, sm.anc, sm.bad, k0, k1);
+  end_tile<bf16>(a, sm.c, reinterpret_cast<float*>(sm.k), DP, k0, k1);
 }
 
 // ---------------------------------------------------------------- fp32, 16 rows
 // The numerics type: FMAs in fp32.  Blocks of 32 keys in shared memory (rows padded by 16 bytes: a quarter-warp's loads of eight rows hit
-// eight different bank groups); a thread computes the scores of one key for four rows, then owns every 128th column of all 16 rows.
+// eight different bank groups), the next one's copies under the arithmetic of the current one where two fit; a thread computes the
+// scores of one key for four rows, then owns every 128th column of all 16 rows.
 constexpr int kKeys32 = 32;
 
 struct F32Ctl {
   float p[kRows][kKeys32 + 4], alpha[kRows], m[kRows], l[kRows];
-  int64_t code[kKeys32];
-  int depth[TSV_MAX_D];
-  uint32_t anc[TSV_MAX_D];
-  int pos[kRows];
-  uint32_t row_anc[kRows];
-  TileList t;
-  uint32_t bad;
+  int64_t code[2][kKeys32];
+  TileCtl c;
 };
+__host__ __device__ inline int f32_ctl() { return (int)((sizeof(F32Ctl) + 15) & ~(size_t)15); }
+inline int f32_block(const AttnArgs& a) { return 4 * (a.c.v ? 2 : 1) * kKeys32 * (a.s.d + 4); }
 
 template <int NC>       // columns of a thread
-__global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a, const int buffers) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   F32Ctl& sm = *reinterpret_cast<F32Ctl*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, d = a.s.d, ld = d + 4;
-  float* q = reinterpret_cast<float*>(smem_raw + ((sizeof(F32Ctl) + 15) & ~15));
-  float* ks = q + kRows * d;
-  float* vs = a.c.v ? ks + kKeys32 * ld : ks;
-  if (warp == 0) {
-    const TileList t = make_list(a, blockIdx.x, blockIdx.y, kRows, sm.depth, sm.anc);
-    if (lane == 0) { sm.t = t; sm.bad = 0; }
-  }
-  __syncthreads();
-  const TileList& t = sm.t;
-  if (t.ok != 1) {
-    if (t.ok == 2 && a.nsplit == 1) zero_rows<float>(a, t);
-    return;
-  }
+  float* q = reinterpret_cast<float*>(smem_raw + f32_ctl());      // (and the output at the end)
+  float* blocks = q + kRows * d;
+  const int bstride = (a.c.v ? 2 : 1) * kKeys32 * ld;
+  if (!begin_tile<float>(a, sm.c)) return;
+  const TileList& t = sm.c.t;
   int k0, k1;
-  split_range(a, t, kKeys32, k0, k1);
-  if (tid < kRows) {
-    int p = 0;
-    uint32_t an = 0;
-    if (tid < t.nr) row_facts(a, t, sm.depth, sm.anc, tid, p, an);
-    sm.pos[tid] = p; sm.row_anc[tid] = an;
-  }
-  const int nv = d / 4;
+  split_range(a, t, k0, k1);
+  const int nv = d / 4, nb = (k1 - k0 + kKeys32 - 1) / kKeys32;
   for (int i = tid; i < kRows * nv; i += kThreads) {
     const int r = i / nv, c = i % nv;
     cp16(smem_u32(q + r * d + c * 4), r < t.nr ? (const void*)(query_row<float>(a, t, r) + c * 4) : a.in.q, r < t.nr);
   }
+  auto codes = [&](int j) {
+    if (tid >= kKeys32 || j >= nb) return;
+    const int kk = k0 + j * kKeys32 + tid;
+    int64_t code = -1;
+    if (kk < k1) {
+      code = list_row(a, t, kk);
+      if (code == -1) atomicOr(a.status + t.b, TSV_ST_PAGE);
+    }
+    sm.code[j & 1][tid] = code;
+  };
+  auto load = [&](int j) {
+    if (j < nb) {
+      float* ks = blocks + (buffers > 1 ? (j & 1) * bstride : 0);
+      for (int i = tid; i < kKeys32 * nv; i += kThreads) {
+        const int r = i / nv, c = i % nv;
+        const int64_t code = sm.code[j & 1][r];
+        cp16(smem_u32(ks + r * ld + c * 4), code != -1 ? (const void*)(row_ptr<float>(a, t.hk, code, false) + c * 4) : a.in.k, code != -1);
+        if (a.c.v) cp16(smem_u32(ks + (kKeys32 + r) * ld + c * 4), code != -1 ? (const void*)(row_ptr<float>(a, t.hk, code, true) + c * 4) : a.in.k, code != -1);
+      }
+    }
+    cp_commit();
+  };
   for (int pass = 0; pass < 2; ++pass) {                  // (the second one only where a result is not finite)
   float o[NC][kRows];
 #pragma unroll
@@ -378,27 +475,18 @@ __global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a) {
 #pragma unroll
     for (int r = 0; r < kRows; ++r) o[c][r] = 0.f;
   if (tid < kRows) { sm.m[tid] = -INFINITY; sm.l[tid] = 0.f; }
-  for (int kb = k0; kb < k1; kb += kKeys32) {
-    __syncthreads();
-    if (tid < kKeys32) {
-      int64_t code = -1;
-      if (kb + tid < k1) {
-        code = list_row(a, t, kb + tid);
-        if (code == -1) atomicOr(a.status + t.b, TSV_ST_PAGE);
-      }
-      sm.code[tid] = code;
-    }
-    __syncthreads();
-    for (int i = tid; i < kKeys32 * nv; i += kThreads) {
-      const int r = i / nv, c = i % nv;
-      const int64_t code = sm.code[r];
-      cp16(smem_u32(ks + r * ld + c * 4), code != -1 ? (const void*)(row_ptr<float>(a, t.hk, code, false) + c * 4) : a.in.k, code != -1);
-      if (a.c.v) cp16(smem_u32(vs + r * ld + c * 4), code != -1 ? (const void*)(row_ptr<float>(a, t.hk, code, true) + c * 4) : a.in.k, code != -1);
-    }
-    cp_commit();
-    cp_wait<0>();
+  codes(0);
+  __syncthreads();
+  load(0);
+  codes(1);
+  for (int j = 0; j < nb; ++j) {
+    const int kb = k0 + j * kKeys32;
+    const float* ks = blocks + (buffers > 1 ? (j & 1) * bstride : 0);
+    const float* vs = a.c.v ? ks + kKeys32 * ld : ks;
+    __syncthreads();                                      // (block j + 1's rows; everyone is done with block j - 1)
+    if (buffers > 1) { load(j + 1); cp_wait<1>(); } else cp_wait<0>();
     if (pass)                                             // (what this thread has copied)
-      for (int i = tid; i < kKeys32 * nv; i += kThreads) make_finite<float>(vs + i / nv * ld + i % nv * 4);
+      for (int i = tid; i < kKeys32 * nv; i += kThreads) make_finite<float>(const_cast<float*>(vs) + i / nv * ld + i % nv * 4);
     __syncthreads();
     // scores: key `lane`, rows 4 warp ..
     float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -413,7 +501,7 @@ __global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = 4 * warp + i;
-      const bool see = kb + lane < k1 && sm.code[lane] != -1 && list_sees(a, t, sm.depth, sm.pos[r], sm.row_anc[r], kb + lane);
+      const bool see = kb + lane < k1 && sm.code[j & 1][lane] != -1 && list_sees(a, t, sm.c.depth, sm.c.pos[r], sm.c.row_anc[r], kb + lane);
       s[i] = see ? s[i] * a.scale2 : -INFINITY;
       float mx = s[i];
 #pragma unroll
@@ -426,6 +514,7 @@ __global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a) {
       if (lane == 0) { sm.alpha[r] = al; sm.m[r] = mn; sm.l[r] = sm.l[r] * al + sum; }
     }
     __syncthreads();
+    codes(j + 2);                                         // (in the place of block j's)
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       const float al = sm.alpha[r];
@@ -445,28 +534,31 @@ __global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a) {
         for (int c = 0; c < NC; ++c) o[c][r] = fmaf(p.x, v[c][0], fmaf(p.y, v[c][1], fmaf(p.z, v[c][2], fmaf(p.w, v[c][3], o[c][r]))));
       }
     }
+    if (buffers == 1) { __syncthreads(); load(j + 1); }
   }
+  cp_wait<0>();
   __syncthreads();
+  const bool again = pass == 0;
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
     if (r >= t.nr) break;
     const float l = sm.l[r];
     bool bad = !is_finite(l) || (sm.m[r] == -INFINITY && a.nsplit == 1);
-    const size_t at = part_index(a) + r;
-    float* out = a.nsplit > 1 ? a.po + at * d : out_row<float>(a, t, r);
-    const float inv = a.nsplit > 1 ? 1.f : 1.f / l;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      bad |= !is_finite(o[c][r]);
-      if (tid + c * kThreads < d) out[tid + c * kThreads] = o[c][r] * inv;
-    }
-    if (a.nsplit > 1 && tid == 0) a.pml[at] = make_float2(sm.m[r], l);
-    if (bad && pass == 0) atomicOr(&sm.bad, 1u << r);
+    for (int c = 0; c < NC; ++c) bad |= !is_finite(o[c][r]);
+    if (tid == 0) sm.c.ml[r] = make_float2(sm.m[r], l);
+    if (bad && again) atomicOr(&sm.c.bad, 1u << r);
   }
   __syncthreads();
-  if (!sm.bad) return;
+  if (!sm.c.bad || !again) {                              // (Q's place: it is not read any more)
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) if (tid + c * kThreads < d) q[r * d + tid + c * kThreads] = o[c][r];
+    break;
   }
-  exact_rows<float>(a, t, sm.depth, sm.anc, sm.bad, k0, k1);
+  }
+  end_tile<float>(a, sm.c, q, d, k0, k1);
 }
 
 // ---------------------------------------------------------------- partial outputs
@@ -521,24 +613,33 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a, c
   }
 }
 
-template <int DP, int KB, bool SHARED>
-int mma_launch(const AttnArgs& a, dim3 grid, cudaStream_t st) {
-  const int smem = (int)sizeof(MmaSmem<DP, KB, SHARED>);
-  if (!ensure_smem((const void*)attn_mma_kernel<DP, KB, SHARED>, smem)) return TSV_ERR_CUDA;
-  TSV_PREP((attn_mma_kernel<DP, KB, SHARED>));
-  attn_mma_kernel<DP, KB, SHARED><<<grid, kThreads, smem, st>>>(a);
+// A grid of tiles, key heads and shares; the shares of a tile a cluster where its CTAs join them.
+template <typename... P, typename... A>
+int launch_tiles(void (*kernel)(P...), const AttnArgs& a, dim3 grid, int smem, cudaStream_t st, A... args) {
+  if (!ensure_smem((const void*)kernel, smem)) return TSV_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = a.cluster ? a.nsplit : 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) return TSV_ERR_CUDA;
   count_launch();
   return TSV_OK;
 }
 
+template <int DP, bool SHARED>
+int mma_launch(const AttnArgs& a, dim3 grid, cudaStream_t st) {
+  TSV_PREP((attn_mma_kernel<DP, SHARED>));
+  return launch_tiles(attn_mma_kernel<DP, SHARED>, a, grid, (int)sizeof(MmaSmem<DP, SHARED>), st, a);
+}
+
 template <int NC>
 int fp32_launch(const AttnArgs& a, dim3 grid, cudaStream_t st) {
-  const int smem = (int)((sizeof(F32Ctl) + 15) & ~15) + 4 * (kRows * a.s.d + (a.c.v ? 2 : 1) * kKeys32 * (a.s.d + 4));
-  if (!ensure_smem((const void*)attn_fp32_kernel<NC>, smem)) return TSV_ERR_CUDA;
   TSV_PREP(attn_fp32_kernel<NC>);
-  attn_fp32_kernel<NC><<<grid, kThreads, smem, st>>>(a);
-  count_launch();
-  return TSV_OK;
+  const int one = f32_ctl() + 4 * kRows * a.s.d, buffers = one + 2 * f32_block(a) <= 227 * 1024 ? 2 : 1;
+  return launch_tiles(attn_fp32_kernel<NC>, a, grid, one + buffers * f32_block(a), st, a, buffers);
 }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -547,7 +648,7 @@ struct AttnPlan {
   bool tc;                // 128-row tiles on the tensor cores
   int per;                // query rows of a tile
   int64_t tiles;          // tiles over all sequences (bound)
-  int nsplit;
+  int nsplit, cluster;
   size_t off_pml;
 };
 
@@ -555,9 +656,10 @@ struct AttnPlan {
 bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s.max_n * (s.H / s.Hk) >= 48; }
 
 // Tiles and CTAs that splitting the keys aims at: those that run at a time.
-int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? 148 / tc_halves(s.d) : 2 * 148; }
+int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? 148 / tc_halves(s.d) : s.d <= 128 ? 2 * 148 : 148; }
 
-// Keys are split where the tiles alone would leave SMs without work, into shares of some blocks of keys each.
+// Keys are split where the tiles alone would leave SMs without work.  16-row tiles: into up to eight shares of 32 keys and more, a
+// cluster's CTAs, which join them; into more only where a share of eight would still be longer than 512 keys, through partial outputs.
 AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   AttnPlan p;
   p.tc = takes_tc(s);
@@ -566,11 +668,19 @@ AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   const int64_t ctas = p.tiles * s.Hk;
   int64_t reach = (int64_t)s.window + s.max_n;
   if (reach > s.max_L) reach = s.max_L;
-  const int64_t keys = reach + (s.n_sink < s.max_L ? s.n_sink : s.max_L), least = p.tc ? 512 : 128;
-  int64_t ns = (slots_of(s) + ctas - 1) / ctas;
-  if (ns > (keys + least - 1) / least) ns = (keys + least - 1) / least;
-  if (ns > 64) ns = 64;
-  p.nsplit = (int)(ns < 1 ? 1 : ns);
+  const int64_t keys = reach + (s.n_sink < s.max_L ? s.n_sink : s.max_L);
+  auto shares = [&](int64_t least) {
+    int64_t ns = slots_of(s) / ctas;                      // (no more CTAs than run at a time)
+    if (ns > (keys + least - 1) / least) ns = (keys + least - 1) / least;
+    return (int)(ns < 1 ? 1 : ns > 64 ? 64 : ns);
+  };
+  p.cluster = 0;
+  p.nsplit = shares(512);
+  if (!p.tc && p.nsplit <= 8) {
+    p.nsplit = shares(32);
+    if (p.nsplit > 8) p.nsplit = 8;
+    p.cluster = p.nsplit > 1;
+  }
   p.off_pml = up256((size_t)2 * slots_of(s) * p.per * s.d * sizeof(float));
   return p;
 }
@@ -593,6 +703,7 @@ int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_to
   a.pml = reinterpret_cast<float2*>(ws + p.off_pml);
   a.G = s.H / s.Hk;
   a.nsplit = p.nsplit;
+  a.cluster = p.cluster;
   a.scale2 = s.sm_scale * 1.4426950408889634f;
   a.status = status;
   const dim3 grid((unsigned)p.tiles, s.Hk, p.nsplit);
@@ -602,14 +713,14 @@ int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_to
   } else if (s.dtype == TSV_FP32) {
     r = s.d <= 128 ? fp32_launch<1>(a, grid, st) : s.d <= 256 ? fp32_launch<2>(a, grid, st) : fp32_launch<4>(a, grid, st);
   } else if (!c.v) {
-    r = s.d <= 64 ? mma_launch<64, 64, true>(a, grid, st) : s.d <= 128 ? mma_launch<128, 64, true>(a, grid, st)
-      : s.d <= 256 ? mma_launch<256, 64, true>(a, grid, st) : mma_launch<512, 64, true>(a, grid, st);
+    r = s.d <= 64 ? mma_launch<64, true>(a, grid, st) : s.d <= 128 ? mma_launch<128, true>(a, grid, st)
+      : s.d <= 256 ? mma_launch<256, true>(a, grid, st) : mma_launch<512, true>(a, grid, st);
   } else {
-    r = s.d <= 64 ? mma_launch<64, 64, false>(a, grid, st) : s.d <= 128 ? mma_launch<128, 64, false>(a, grid, st)
-      : s.d <= 256 ? mma_launch<256, 64, false>(a, grid, st) : mma_launch<512, 32, false>(a, grid, st);
+    r = s.d <= 64 ? mma_launch<64, false>(a, grid, st) : s.d <= 128 ? mma_launch<128, false>(a, grid, st)
+      : s.d <= 256 ? mma_launch<256, false>(a, grid, st) : mma_launch<512, false>(a, grid, st);
   }
   if (r) return r;
-  if (p.nsplit > 1) {
+  if (p.nsplit > 1 && !p.cluster) {
     const dim3 jg((unsigned)p.tiles, s.Hk, p.per / 4);
     if (s.dtype == TSV_FP32) attn_join_kernel<float><<<jg, kThreads, 0, st>>>(a, p.per);
     else attn_join_kernel<bf16><<<jg, kThreads, 0, st>>>(a, p.per);

@@ -19,7 +19,8 @@ struct AttnArgs {
   float* po;                // partial outputs [row tiles][splits][rows of a tile][d], their {max, sum} behind them
   float2* pml;
   int32_t G;                // H / Hk
-  int32_t nsplit;
+  int32_t nsplit;           // shares that a tile's keys are cut into
+  int32_t cluster;          // the shares are a cluster's CTAs, which join them (16-row tiles), and not partial outputs
   float scale2;             // softmax scale * log2(e): scores in powers of two
   int32_t* status;
 };
@@ -69,10 +70,10 @@ __device__ __forceinline__ TileList make_list(const AttnArgs& a, int64_t item, i
   TileList t;
   TokUnit u;
   t.ok = 0;
-  if (!find_unit(a.s, a.bt, a.G, per, item, a.status, u)) return t;
+  if (!find_unit(a.s, a.bt, a.c.L, a.G, per, item, a.status, u)) return t;
   const int lane = threadIdx.x & 31;
   t.b = u.b; t.n = u.n; t.row0 = u.row0; t.G = a.G; t.hk = hk;
-  t.L = __ldg(a.c.L + u.b);
+  t.L = u.L;
   t.r0 = u.unit * per;
   t.nr = (int)min((int64_t)per, (int64_t)u.n * a.G - t.r0);
   int st = t.L < 0 || (int64_t)t.L + u.n > a.s.max_L ? TSV_ST_LENGTH : 0;

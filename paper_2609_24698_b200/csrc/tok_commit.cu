@@ -91,13 +91,13 @@ __global__ void __launch_bounds__(kCommitThreads) commit_rows_kernel(const Commi
   __shared__ TokUnit s_u;
   if (threadIdx.x < 32) {
     TokUnit u;
-    const bool f = find_unit(a.s, a.bt, 1, kCommitRows, blockIdx.x, a.status, u);
+    const bool f = find_unit(a.s, a.bt, a.c.L, 1, kCommitRows, blockIdx.x, a.status, u);
     if (threadIdx.x == 0) { s_found = f && a.status[u.b] == 0; s_u = u; }
   }
   __syncthreads();
   if (!s_found) return;
   const TokUnit u = s_u;
-  const int L = a.c.L[u.b];
+  const int L = u.L;
   const int cnt = commit_count(a, u.b, u.n, L, &s_bad);
   const int i0 = u.unit * kCommitRows, i1 = min(cnt, i0 + kCommitRows);
   if (i0 < i1) commit_rows(a, u, L, cnt, i0, i1);

@@ -7,7 +7,7 @@ namespace tsv {
 
 // A piece of a sequence's new tokens: unit `unit` of `per` rows out of n[b] * rows_per_token, found by its number over the batch.
 struct TokUnit {
-  int b, unit, n;
+  int b, unit, n, L;
   int64_t row0;
 };
 
@@ -23,17 +23,19 @@ __device__ __forceinline__ int tok_count(const tsv_tok_shape& s, const tsv_tok_b
 }
 
 // Warp-collective: which sequence unit number `item` belongs to (units of `per` rows, `rpt` rows per token); false behind the last.
-// 64 sequences are requested at a time: the loads are what this costs.  (A prefix array made once would take another launch.)
-__device__ __forceinline__ bool find_unit(const tsv_tok_shape& s, const tsv_tok_batch& bt, int rpt, int per, int64_t item, int32_t* status, TokUnit& u) {
+// 64 sequences are requested at a time, their lengths (L_all) with them: the loads are what this costs.  (A prefix array made once would
+// take another launch.)
+__device__ __forceinline__ bool find_unit(const tsv_tok_shape& s, const tsv_tok_batch& bt, const int32_t* L_all, int rpt, int per, int64_t item, int32_t* status, TokUnit& u) {
   const int lane = threadIdx.x & 31;
   int64_t before = 0;
   for (int base = 0; base < s.B; base += 64) {
-    int n[2];
+    int n[2], L[2];
     int64_t row0[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      n[h] = 0; row0[h] = 0;
-      if (base + 32 * h + lane < s.B) n[h] = max(0, tok_count(s, bt, base + 32 * h + lane, status, row0[h]));
+      n[h] = 0; row0[h] = 0; L[h] = 0;
+      const int b = base + 32 * h + lane;
+      if (b < s.B) { L[h] = L_all[b]; n[h] = max(0, tok_count(s, bt, b, status, row0[h])); }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -50,6 +52,7 @@ __device__ __forceinline__ bool find_unit(const tsv_tok_shape& s, const tsv_tok_
         u.b = base + 32 * h + src;
         u.unit = (int)(item - before - __shfl_sync(0xffffffffu, x - units, src));
         u.n = __shfl_sync(0xffffffffu, n[h], src);
+        u.L = __shfl_sync(0xffffffffu, L[h], src);
         u.row0 = __shfl_sync(0xffffffffu, row0[h], src);
         return true;
       }

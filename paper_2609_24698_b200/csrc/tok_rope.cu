@@ -54,8 +54,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
   if (warp == 0) {
     TokUnit u;
     int ok = 0;                                            // 0: nothing to do, 1: rows, 2: zeros
-    if (find_unit(s, a.bt, 1, a.tpi, blockIdx.x, a.status, u)) {
-      const int L = __ldg(a.L + u.b);
+    if (find_unit(s, a.bt, a.L, 1, a.tpi, blockIdx.x, a.status, u)) {
+      const int L = u.L;
       int st = L < 0 || (int64_t)L + u.n > s.max_L ? TSV_ST_LENGTH : 0, depth = 0;
       uint32_t anc;
       if (a.bt.parent) st |= tok_tree(a.bt, u, depth, anc);
