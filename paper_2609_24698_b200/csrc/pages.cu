@@ -1,7 +1,7 @@
 // Pages of a paged pool: pages_assign, pages_free, pages_fork, pages_compact.
 //
 // Who holds what is decided by one CTA (the lists are short and each step needs the counts of the one before); the contents move in
-// a kernel over all SMs, 16 KiB of one page of one plane at a time: a copy, bound by HBM, or by launches and latency for few pages.
+// a kernel over all SMs, 32 KiB of one page of one plane at a time: a copy, bound by HBM, or by launches and latency for few pages.
 // Pages are counted in the order of their numbers, so every result is the same whatever the order of execution: the only atomics
 // are on whole numbers.
 #include "kernels.h"
@@ -14,7 +14,8 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kScan = 16;                          // pages of a lane per round of a scan
 constexpr int kCopyThreads = 256;
-constexpr int kChunk = kCopyThreads * 64;          // bytes of a work item of the copy kernel
+constexpr int kVecs = 8;                           // 16-byte vectors of a thread in a work item of the copy kernel
+constexpr int kChunk = kCopyThreads * kVecs * 16;  // bytes of one
 constexpr int kArrays = 128;                       // planes and row arrays of a launch
 
 struct Pool {
@@ -232,28 +233,41 @@ struct CopyArgs {
   int32_t renumber;                 // the table's words become the new numbers (compact)
 };
 
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const CopyArgs a) {
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
   const int per = a.chunk0[a.n], tid = threadIdx.x;
-  const int pairs = a.w.head[0];
-  for (int64_t item = blockIdx.x; item < (int64_t)pairs * per; item += gridDim.x) {
-    const int i = (int)(item / per), c = (int)(item % per);
+  const int64_t items = (int64_t)a.w.head[0] * per;
+  // Where item `item` reads and writes, and its bytes (0: none); the next one's is looked up while this one's loads are under way.
+  struct Move { const char* src; char* dst; int left; };
+  auto look_up = [&](int64_t item) {
+    Move m = {nullptr, nullptr, 0};
+    if (item >= items) return m;
+    const int i = (int)(item / per), c = (int)(item - (int64_t)i * per);
     int lo = 0, hi = a.n;                                  // the array of this chunk
     while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (a.chunk0[mid] <= c) lo = mid; else hi = mid; }
     const int2 pr = lo < a.n_planes ? a.w.pages[i] : a.w.rows[i];
-    if (pr.x < 0) continue;
+    if (pr.x < 0) return m;
     const int64_t bytes = a.bytes[lo], off = (int64_t)(c - a.chunk0[lo]) * kChunk;
-    const char* src = a.base[lo] + pr.x * bytes + off;
-    char* dst = a.base[lo] + pr.y * bytes + off;
-    const int left = (int)(bytes - off < kChunk ? bytes - off : kChunk);
-    if ((((uintptr_t)src | (uintptr_t)dst | (uintptr_t)left) & 15) == 0) {
-      uint4 v[4];
+    m.src = a.base[lo] + pr.x * bytes + off;
+    m.dst = a.base[lo] + pr.y * bytes + off;
+    m.left = (int)(bytes - off < kChunk ? bytes - off : kChunk);
+    return m;
+  };
+  Move now = look_up(blockIdx.x);
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const bool wide = (((uintptr_t)now.src | (uintptr_t)now.dst | (uintptr_t)now.left) & 15) == 0;
+    uint4 v[kVecs];
+    if (wide) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) if ((tid + k * kCopyThreads) * 16 < left) v[k] = reinterpret_cast<const uint4*>(src)[tid + k * kCopyThreads];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) if ((tid + k * kCopyThreads) * 16 < left) reinterpret_cast<uint4*>(dst)[tid + k * kCopyThreads] = v[k];
-    } else {
-      for (int k = tid * 4; k < left; k += kCopyThreads * 4) *reinterpret_cast<uint32_t*>(dst + k) = *reinterpret_cast<const uint32_t*>(src + k);
+      for (int k = 0; k < kVecs; ++k) if ((tid + k * kCopyThreads) * 16 < now.left) v[k] = reinterpret_cast<const uint4*>(now.src)[tid + k * kCopyThreads];
     }
+    const Move next = look_up(item + gridDim.x);
+    if (wide) {
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) if ((tid + k * kCopyThreads) * 16 < now.left) reinterpret_cast<uint4*>(now.dst)[tid + k * kCopyThreads] = v[k];
+    } else {
+      for (int k = tid * 4; k < now.left; k += kCopyThreads * 4) *reinterpret_cast<uint32_t*>(now.dst + k) = *reinterpret_cast<const uint32_t*>(now.src + k);
+    }
+    now = next;
   }
   if (a.renumber) {
     const int used = a.w.head[1];

@@ -562,53 +562,58 @@ __global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a, c
 }
 
 // ---------------------------------------------------------------- partial outputs
-// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, splits in order.  A warp per row.
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, shares in order.  A warp per row and 128 columns: its lanes fetch the shares' {m, l}
+// at once (at most 64 shares), then eight shares' values are under way at a time.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a, const int per) {
   __shared__ TileList s_t;
   __shared__ int depth[TSV_MAX_D];
   __shared__ uint32_t anc[TSV_MAX_D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.s.d;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.s.d, chunks = (d + 127) / 128;
   if (warp == 0) {
     const TileList t = make_list(a, blockIdx.x, blockIdx.y, per, depth, anc);
     if (lane == 0) s_t = t;
   }
   __syncthreads();
   const TileList& t = s_t;
-  if (t.ok == 2) zero_rows<T>(a, t);
+  if (t.ok == 2 && blockIdx.z == 0) zero_rows<T>(a, t);
   if (t.ok != 1) return;
-  for (int r = warp + (kThreads / 32) * blockIdx.z; r < t.nr; r += (kThreads / 32) * gridDim.z) {
+  for (int i = warp + (kThreads / 32) * blockIdx.z; i < t.nr * chunks; i += (kThreads / 32) * gridDim.z) {
+    const int r = i / chunks, col = (i % chunks * 32 + lane) * 4;
     const size_t base = (((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.nsplit) * per + r;
+    float2 ml[2];
     float m = -INFINITY;
-    for (int i = 0; i < a.nsplit; ++i) m = fmaxf(m, a.pml[base + (size_t)i * per].x);
-    float l = 0.f, o[4][4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int h = 0; h < 2; ++h) {
+      ml[h] = make_float2(-INFINITY, 0.f);
+      if (lane + 32 * h < a.nsplit) ml[h] = a.pml[base + (size_t)(lane + 32 * h) * per];
+      m = fmaxf(m, ml[h].x);
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[c][e] = 0.f;
-    for (int i = 0; i < a.nsplit; ++i) {
-      const size_t at = base + (size_t)i * per;
-      const float2 ml = a.pml[at];
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;    // (nothing seen)
-      const float w = exp2f(ml.x - m);
-      l = fmaf(ml.y, w, l);
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float w[2];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int col = (c * 32 + lane) * 4;
-        if (col < d) {
-          const float4 v = *reinterpret_cast<const float4*>(a.po + at * d + col);
-          o[c][0] = fmaf(v.x, w, o[c][0]); o[c][1] = fmaf(v.y, w, o[c][1]); o[c][2] = fmaf(v.z, w, o[c][2]); o[c][3] = fmaf(v.w, w, o[c][3]);
-        }
+    for (int h = 0; h < 2; ++h) w[h] = ml[h].x == -INFINITY && ml[h].y == 0.f ? -1.f : exp2f(ml[h].x - m);      // (-1: nothing seen)
+    float l = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
+      float4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s0 + k < a.nsplit && col < d) v[k] = *reinterpret_cast<const float4*>(a.po + (base + (size_t)(s0 + k) * per) * d + col);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float ws = __shfl_sync(0xffffffffu, s0 + k < 32 ? w[0] : w[1], (s0 + k) & 31), ls = __shfl_sync(0xffffffffu, s0 + k < 32 ? ml[0].y : ml[1].y, (s0 + k) & 31);
+        if (s0 + k >= a.nsplit || ws == -1.f) continue;
+        l = fmaf(ls, ws, l);
+        x.x = fmaf(v[k].x, ws, x.x); x.y = fmaf(v[k].y, ws, x.y); x.z = fmaf(v[k].z, ws, x.z); x.w = fmaf(v[k].w, ws, x.w);
       }
     }
-    T* out = out_row<T>(a, t, r);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int col = (c * 32 + lane) * 4;
-      if (col < d) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[col + e] = from_f<T>(o[c][e] / l);
-      }
+    if (col < d) {
+      T* out = out_row<T>(a, t, r) + col;
+      out[0] = from_f<T>(x.x / l); out[1] = from_f<T>(x.y / l); out[2] = from_f<T>(x.z / l); out[3] = from_f<T>(x.w / l);
     }
   }
 }
@@ -721,7 +726,7 @@ int launch_tok_attn(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_to
   }
   if (r) return r;
   if (p.nsplit > 1 && !p.cluster) {
-    const dim3 jg((unsigned)p.tiles, s.Hk, p.per / 4);
+    const dim3 jg((unsigned)p.tiles, s.Hk, (p.per * ((s.d + 127) / 128) + 3) / 4);
     if (s.dtype == TSV_FP32) attn_join_kernel<float><<<jg, kThreads, 0, st>>>(a, p.per);
     else attn_join_kernel<bf16><<<jg, kThreads, 0, st>>>(a, p.per);
     count_launch();

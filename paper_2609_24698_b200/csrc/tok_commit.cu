@@ -55,19 +55,24 @@ __device__ __forceinline__ int commit_count(const CommitArgs& a, int b, int n, i
   return cnt;
 }
 
+// Rows i0 .. i1 - 1 of what the sequence gives, a warp per row and plane (where a row goes is worked out once for all its vectors).
 __device__ __forceinline__ void commit_rows(const CommitArgs& a, const TokUnit& u, int L, int cnt, int i0, int i1) {
-  const int rv = a.row_vecs, planes = a.v ? 2 : 1;
-  const int64_t total = (int64_t)(i1 - i0) * rv * planes;
-  for (int64_t t = threadIdx.x; t < total; t += kCommitThreads) {
-    const int plane = (int)(t / ((int64_t)(i1 - i0) * rv));
-    const int rest = (int)(t - (int64_t)plane * (i1 - i0) * rv), i = i0 + rest / rv, vec = rest % rv;
+  const int rv = a.row_vecs, planes = a.v ? 2 : 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int t = warp; t < (i1 - i0) * planes; t += kCommitThreads / 32) {
+    const int plane = planes == 2 ? t & 1 : 0, i = i0 + (planes == 2 ? t >> 1 : t);
     // a ring's slot keeps its last writer's row: earlier ones are not written
     if (!a.c.page_table && L + i >= a.s.n_sink && i < cnt - a.s.window) continue;
     const int node = a.path ? __ldg(a.path + (size_t)u.b * a.path_ld + i) : i;
     const int64_t row = tok_cache_row(a.c, a.s.window, a.s.n_sink, u.b, L + i);
-    const char* src = reinterpret_cast<const char*>(plane ? a.v : a.k) + (u.row0 + node) * (plane ? a.v_bytes : a.k_bytes);
-    char* dst = reinterpret_cast<char*>(plane ? a.c.v : a.c.k) + row * rv * 16;
-    reinterpret_cast<uint4*>(dst)[vec] = __ldg(reinterpret_cast<const uint4*>(src) + vec);
+    const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(plane ? a.v : a.k) + (u.row0 + node) * (plane ? a.v_bytes : a.k_bytes));
+    uint4* dst = reinterpret_cast<uint4*>(plane ? a.c.v : a.c.k) + row * rv;
+    for (int v0 = lane; v0 < rv; v0 += 128) {
+      uint4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (v0 + 32 * k < rv) x[k] = __ldg(src + v0 + 32 * k);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (v0 + 32 * k < rv) dst[v0 + 32 * k] = x[k];
+    }
   }
 }
 

@@ -33,7 +33,7 @@ struct RopeArgs {
 };
 
 // The angle is exact as a product of a 30-bit and a 24-bit number in fp64; whole turns are taken off there too (what is left has
-// an error of 2^-53 of the turns, 2^-23 at 2^30 turns), and only the rest of at most half a turn goes on in fp32.
+// an error of some 2^-53 of the turns, 2^-25 at positions of 2^30), and only the rest of at most half a turn goes on in fp32.
 __device__ __forceinline__ float2 cos_sin(int pos, float freq) {
   double turns = (double)pos * (double)freq * 0.15915494309189533576888;
   turns -= rint(turns);
@@ -45,7 +45,7 @@ __device__ __forceinline__ float2 cos_sin(int pos, float freq) {
 // UPL: pairs of 16-byte vectors a lane owns (2 for fp32 heads of more than 256 dims)
 template <typename T, int UPL>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
-  constexpr int VE = Vec<T>::N;
+  constexpr int VE = Vec<T>::N, AHEAD = UPL == 1 ? 4 : 2;
   extern __shared__ float2 cs_tab[];                       // [tpi][rot / 2]
   __shared__ int s_ok, s_pos[8];
   __shared__ TokUnit s_u;
@@ -139,52 +139,62 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
         for (int e = 0; e < VE; ++e) wt[p][h * VE + e] = w && vec[p][h] >= 0 ? __ldg(w + vec[p][h] * VE + e) : 1.f;
     // (the last part first: keys have few heads, and the parts of a token that get none of the queries' rest take them)
     const int first = (which ? parts - 1 - part : part) * hpw;
-#pragma unroll 2
-    for (int h0 = first; h0 < heads; h0 += parts * hpw) {
-      const int head = h0 + gi;
-      const bool live = head < heads;
-      float x[UPL][2 * VE];
-      float ss = 0.f;
+    // four heads' loads of a lane at a time: a warp has few heads to walk over, and their latency is what it waits for
+    const int step = parts * hpw;
+#pragma unroll 1
+    for (int h0 = first; h0 < heads; h0 += AHEAD * step) {
+      uint4 raw[AHEAD][UPL][2];
 #pragma unroll
-      for (int p = 0; p < UPL; ++p)
+      for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float* xv = x[p] + h * VE;
+        for (int p = 0; p < UPL; ++p)
 #pragma unroll
-          for (int e = 0; e < VE; ++e) xv[e] = 0.f;
-          if (live && vec[p][h] >= 0 && ok == 1) ld16(in + (size_t)head * s.d + vec[p][h] * VE, xv);
+          for (int h = 0; h < 2; ++h) {
+            const int head = h0 + u * step + gi;
+            raw[u][p][h] = make_uint4(0, 0, 0, 0);
+            if (head < heads && vec[p][h] >= 0 && ok == 1) raw[u][p][h] = *reinterpret_cast<const uint4*>(in + (size_t)head * s.d + vec[p][h] * VE);
+          }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int head = h0 + u * step + gi;
+        const bool live = head < heads;
+        float x[UPL][2 * VE];
+        float ss = 0.f;
+#pragma unroll
+        for (int p = 0; p < UPL; ++p) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) ld16(reinterpret_cast<const T*>(&raw[u][p][h]), x[p] + h * VE);
+#pragma unroll
+          for (int e = 0; e < 2 * VE; ++e) ss = fmaf(x[p][e], x[p][e], ss);
         }
+        for (int o = a.group >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        const float r = 1.f / sqrtf(fmaf(ss, inv_d, a.eps));
 #pragma unroll
-      for (int p = 0; p < UPL; ++p)
+        for (int p = 0; p < UPL; ++p) {
+          float y[2 * VE];
 #pragma unroll
-        for (int e = 0; e < 2 * VE; ++e) ss = fmaf(x[p][e], x[p][e], ss);
-      for (int o = a.group >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const float r = 1.f / sqrtf(fmaf(ss, inv_d, a.eps));
+          for (int e = 0; e < 2 * VE; ++e) y[e] = ok == 1 ? x[p][e] * r * wt[p][e] : 0.f;
+          if (turn[p]) {
+            if (a.pairs) {
 #pragma unroll
-      for (int p = 0; p < UPL; ++p) {
-        float y[2 * VE];
+              for (int e = 0; e < VE; ++e) {
+                const float ya = y[2 * e], yb = y[2 * e + 1];
+                y[2 * e] = ya * cs[p][e].x - yb * cs[p][e].y;
+                y[2 * e + 1] = ya * cs[p][e].y + yb * cs[p][e].x;
+              }
+            } else {
 #pragma unroll
-        for (int e = 0; e < 2 * VE; ++e) y[e] = ok == 1 ? x[p][e] * r * wt[p][e] : 0.f;
-        if (turn[p]) {
-          if (a.pairs) {
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-              const float ya = y[2 * e], yb = y[2 * e + 1];
-              y[2 * e] = ya * cs[p][e].x - yb * cs[p][e].y;
-              y[2 * e + 1] = ya * cs[p][e].y + yb * cs[p][e].x;
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-              const float ya = y[e], yb = y[VE + e];
-              y[e] = ya * cs[p][e].x - yb * cs[p][e].y;
-              y[VE + e] = ya * cs[p][e].y + yb * cs[p][e].x;
+              for (int e = 0; e < VE; ++e) {
+                const float ya = y[e], yb = y[VE + e];
+                y[e] = ya * cs[p][e].x - yb * cs[p][e].y;
+                y[VE + e] = ya * cs[p][e].y + yb * cs[p][e].x;
+              }
             }
           }
-        }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (live && vec[p][h] >= 0) st16(out + (size_t)head * s.d + vec[p][h] * VE, y + h * VE);
+          for (int h = 0; h < 2; ++h)
+            if (live && vec[p][h] >= 0) st16(out + (size_t)head * s.d + vec[p][h] * VE, y + h * VE);
+        }
       }
     }
   }
