@@ -16,6 +16,7 @@ constexpr int kScan = 16;                          // pages of a lane per round 
 constexpr int kCopyThreads = 256;
 constexpr int kVecs = 8;                           // 16-byte vectors of a thread in a work item of the copy kernel
 constexpr int kChunk = kCopyThreads * kVecs * 16;  // bytes of one
+constexpr int kCopyCtas = 4;                       // of them per SM: all run at a time, each with the same number of items
 constexpr int kArrays = 128;                       // planes and row arrays of a launch
 
 struct Pool {
@@ -233,7 +234,7 @@ struct CopyArgs {
   int32_t renumber;                 // the table's words become the new numbers (compact)
 };
 
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyArgs a) {
   const int per = a.chunk0[a.n], tid = threadIdx.x;
   const int64_t items = (int64_t)a.w.head[0] * per;
   // Where item `item` reads and writes, and its bytes (0: none); the next one's is looked up while this one's loads are under way.
@@ -300,7 +301,7 @@ int launch_copies(const tsv_page_pool& p, const Work& w, bool rows, int64_t most
     a.chunk0[a.n] = (int32_t)chunks;
     int64_t grid = most_pairs * chunks;
     if (renumber && grid < 32) grid = 32;
-    if (grid > 148 * 8) grid = 148 * 8;
+    if (grid > 148 * kCopyCtas) grid = 148 * kCopyCtas;
     if (grid < 1) grid = 1;
     copy_kernel<<<(unsigned)grid, kCopyThreads, 0, st>>>(a);
     count_launch();

@@ -9,7 +9,7 @@ namespace tsv {
 namespace {
 
 constexpr int kCommitThreads = 256;
-constexpr int kCommitRows = 16;          // rows of a CTA where several share a sequence
+constexpr int kCommitRows = 32;          // rows of a CTA where several share a sequence
 
 struct CommitArgs {
   tsv_tok_shape s;
@@ -55,23 +55,46 @@ __device__ __forceinline__ int commit_count(const CommitArgs& a, int b, int n, i
   return cnt;
 }
 
-// Rows i0 .. i1 - 1 of what the sequence gives, a warp per row and plane (where a row goes is worked out once for all its vectors).
+// Rows i0 .. i1 - 1 of what the sequence gives.  A warp takes every eighth of the (row, plane) pairs, 32 of them at a time: a lane
+// looks up where one goes, then the warp copies one after the other, two under way at a time.
 __device__ __forceinline__ void commit_rows(const CommitArgs& a, const TokUnit& u, int L, int cnt, int i0, int i1) {
+  constexpr int W = kCommitThreads / 32;
   const int rv = a.row_vecs, planes = a.v ? 2 : 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int t = warp; t < (i1 - i0) * planes; t += kCommitThreads / 32) {
-    const int plane = planes == 2 ? t & 1 : 0, i = i0 + (planes == 2 ? t >> 1 : t);
-    // a ring's slot keeps its last writer's row: earlier ones are not written
-    if (!a.c.page_table && L + i >= a.s.n_sink && i < cnt - a.s.window) continue;
-    const int node = a.path ? __ldg(a.path + (size_t)u.b * a.path_ld + i) : i;
-    const int64_t row = tok_cache_row(a.c, a.s.window, a.s.n_sink, u.b, L + i);
-    const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(plane ? a.v : a.k) + (u.row0 + node) * (plane ? a.v_bytes : a.k_bytes));
-    uint4* dst = reinterpret_cast<uint4*>(plane ? a.c.v : a.c.k) + row * rv;
-    for (int v0 = lane; v0 < rv; v0 += 128) {
-      uint4 x[4];
+  const int pairs = (i1 - i0) * planes;
+  for (int t0 = warp; t0 < pairs; t0 += 32 * W) {
+    const int t = t0 + lane * W;
+    unsigned long long src = 0, dst = 0;
+    if (t < pairs) {
+      const int plane = planes == 2 ? t & 1 : 0, i = i0 + (planes == 2 ? t >> 1 : t);
+      // (a ring's slot keeps its last writer's row: earlier ones are not written)
+      if (a.c.page_table || L + i < a.s.n_sink || i >= cnt - a.s.window) {
+        const int node = a.path ? __ldg(a.path + (size_t)u.b * a.path_ld + i) : i;
+        const int64_t row = tok_cache_row(a.c, a.s.window, a.s.n_sink, u.b, L + i);
+        src = reinterpret_cast<unsigned long long>(plane ? a.v : a.k) + (u.row0 + node) * (plane ? a.v_bytes : a.k_bytes);
+        dst = reinterpret_cast<unsigned long long>(plane ? a.c.v : a.c.k) + row * rv * 16;
+      }
+    }
+    const int here = min(32, (pairs - t0 + W - 1) / W);
+    for (int k = 0; k < here; k += 2) {
+      const uint4* from[2];
+      uint4* to[2];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) if (v0 + 32 * k < rv) x[k] = __ldg(src + v0 + 32 * k);
+      for (int e = 0; e < 2; ++e) {
+        from[e] = reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, src, (k + e) & 31));
+        to[e] = reinterpret_cast<uint4*>(__shfl_sync(0xffffffffu, dst, (k + e) & 31));
+        if (k + e >= here) to[e] = nullptr;
+      }
+      for (int v0 = lane; v0 < rv; v0 += 128) {
+        uint4 x[2][4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) if (v0 + 32 * k < rv) dst[v0 + 32 * k] = x[k];
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) if (to[e] && v0 + 32 * j < rv) x[e][j] = __ldg(from[e] + v0 + 32 * j);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) if (to[e] && v0 + 32 * j < rv) to[e][v0 + 32 * j] = x[e][j];
+      }
     }
   }
 }
