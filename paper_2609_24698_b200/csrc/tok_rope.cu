@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kRopeThreads, UPL == 1 ? 2 : 1) rope_kernel(co
           const float2 sa = unpair(s2), sb = unpair(s3);
           float ss = (sa.x + sa.y) + (sb.x + sb.y);
           for (int o = a.group >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const float r = ok == 1 ? 1.f / sqrtf(fmaf(ss, inv_d, a.eps)) : 0.f;
+          const float r = ok == 1 ? rsqrtf(fmaf(ss, inv_d, a.eps)) : 0.f;      // (2 units in the last place)
           const uint64_t r2 = pair2(r, r);
 #pragma unroll
           for (int p = 0; p < UPL; ++p) {
