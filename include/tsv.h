@@ -451,7 +451,8 @@ int pages_fork(const tsv_page_pool *pool, int32_t n, const int32_t *src, const i
                size_t workspace_bytes, int32_t *status, void *stream);
 
 /* pages_compact -- the used pages move to the numbers 0 .. n_used - 1: the page with the i-th lowest number >= n_used to the
- * i-th lowest free number, in every plane, the table and the counts with it.  n_used: device, 1 value, written. */
+ * i-th lowest free number, in every plane, the table and the counts with it.  n_used: device, 1 value, written (-1: a bounded wait
+ * inside a kernel gave up, and contents are lost). */
 int pages_compact(const tsv_page_pool *pool, int32_t *n_used, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus

@@ -1,10 +1,11 @@
 // Pages of a paged pool: pages_assign, pages_free, pages_fork, pages_compact.
 //
 // Who holds what is decided by one CTA (the lists are short and each step needs the counts of the one before); the contents move in
-// a kernel over all SMs, 32 KiB of one page of one plane at a time: a copy, bound by HBM, or by launches and latency for few pages.
+// a kernel over all SMs, 16 KiB of one page of one plane at a time, through shared memory by bulk copies (six under way per CTA): a copy,
+// bound by HBM, or by launches and latency for few pages.
 // Pages are counted in the order of their numbers, so every result is the same whatever the order of execution: the only atomics
 // are on whole numbers.
-#include "kernels.h"
+#include "tok_common.cuh"
 
 namespace tsv {
 
@@ -14,9 +15,9 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kScan = 16;                          // pages of a lane per round of a scan
 constexpr int kCopyThreads = 256;
-constexpr int kVecs = 8;                           // 16-byte vectors of a thread in a work item of the copy kernel
-constexpr int kChunk = kCopyThreads * kVecs * 16;  // bytes of one
-constexpr int kCopyCtas = 4;                       // of them per SM: all run at a time, each with the same number of items
+constexpr int kChunk = 16384;                      // bytes of a work item of the copy kernel
+constexpr int kStages = 6, kStoreLag = 3;          // chunks of a CTA in shared memory; loads ahead of the stores
+constexpr int kCopyCtas = 2;                       // CTAs per SM
 constexpr int kArrays = 128;                       // planes and row arrays of a launch
 
 struct Pool {
@@ -231,66 +232,104 @@ struct CopyArgs {
   int32_t n, n_planes;              // arrays of this launch; the first n_planes of them are planes
   Work w;
   Pool p;
+  int32_t compact;                  // `failed` is n_used, else status
   int32_t renumber;                 // the table's words become the new numbers (compact)
+  int32_t* failed;                  // where a copy that never came is told of
+  int32_t n_failed;
 };
 
-__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyArgs a) {
-  const int per = a.chunk0[a.n], tid = threadIdx.x;
-  const int64_t items = (int64_t)a.w.head[0] * per;
-  // Where item `item` reads and writes, and its bytes (0: none); the next one's is looked up while this one's loads are under way.
-  struct Move { const char* src; char* dst; int left; };
-  auto look_up = [&](int64_t item) {
-    Move m = {nullptr, nullptr, 0};
-    if (item >= items) return m;
-    const int i = (int)(item / per), c = (int)(item - (int64_t)i * per);
-    int lo = 0, hi = a.n;                                  // the array of this chunk
-    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (a.chunk0[mid] <= c) lo = mid; else hi = mid; }
-    const int2 pr = lo < a.n_planes ? a.w.pages[i] : a.w.rows[i];
-    if (pr.x < 0) return m;
-    const int64_t bytes = a.bytes[lo], off = (int64_t)(c - a.chunk0[lo]) * kChunk;
-    m.src = a.base[lo] + pr.x * bytes + off;
-    m.dst = a.base[lo] + pr.y * bytes + off;
-    m.left = (int)(bytes - off < kChunk ? bytes - off : kChunk);
-    return m;
-  };
-  Move now = look_up(blockIdx.x);
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const bool wide = (((uintptr_t)now.src | (uintptr_t)now.dst | (uintptr_t)now.left) & 15) == 0;
-    uint4 v[kVecs];
-    if (wide) {
+// Thread 0 moves the planes' chunks: a load into the next stage once the store out of it has been read, a store three chunks behind the
+// loads.  The other warps copy the row arrays, which may be of 4-byte alignment, and renumber the table.
+// (Loads and stores through registers, 8 vectors of a thread: 289 MB of scattered pages 124 us instead of @.)
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
+  extern __shared__ __align__(128) unsigned char stage[];
+  __shared__ __align__(8) uint64_t bars[kStages];
+  const int tid = threadIdx.x, pairs = a.w.head[0];
+  const int planes = min(a.n, a.n_planes), per_plane = a.chunk0[planes], per_row = a.chunk0[a.n] - per_plane;
+  if (tid == 0) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(stage), bar = (uint32_t)__cvta_generic_to_shared(bars);
+    for (int i = 0; i < kStages; ++i) bulk_bar_init(bar + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    const int64_t items = (int64_t)pairs * per_plane;
+    char* to[kStages];
+    uint32_t size[kStages];
+    int64_t item = blockIdx.x;
+    int loaded = 0, stored = 0;                            // chunks so far
+    bool fail = false;
+    // one round of the stages, unrolled: what a stage is for stays in registers
+    while (item < items || stored < loaded) {
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) if ((tid + k * kCopyThreads) * 16 < now.left) v[k] = reinterpret_cast<const uint4*>(now.src)[tid + k * kCopyThreads];
+      for (int st = 0; st < kStages; ++st) {
+        if (item < items && loaded - stored <= kStoreLag && loaded % kStages == st) {
+          const int i = (int)(item / per_plane), c = (int)(item - (int64_t)i * per_plane);
+          int lo = 0, hi = planes;                         // the plane of this chunk
+          while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (a.chunk0[mid] <= c) lo = mid; else hi = mid; }
+          const int2 pr = a.w.pages[i];
+          const int64_t bytes = a.bytes[lo], off = (int64_t)(c - a.chunk0[lo]) * kChunk;
+          item += gridDim.x;
+          size[st] = pr.x < 0 ? 0 : (uint32_t)(bytes - off < kChunk ? bytes - off : kChunk);
+          to[st] = a.base[lo] + pr.y * bytes + off;
+          bulk_wait_read<kStages - kStoreLag - 1>();       // (the store out of this stage has been read)
+          bulk_expect(bar + 8 * st, size[st]);
+          if (size[st]) bulk_load(at + st * kChunk, a.base[lo] + pr.x * bytes + off, size[st], bar + 8 * st);
+          ++loaded;
+        }
+        const int sst = (st + kStages - kStoreLag) % kStages;      // (the store that is due behind this load)
+        if (stored < loaded && stored % kStages == sst && (loaded - stored > kStoreLag || item >= items)) {
+          if (!fail && !bulk_bar_wait(bar + 8 * sst, (stored / kStages) & 1)) fail = true;
+          if (size[sst] && !fail) bulk_store(to[sst], at + sst * kChunk, size[sst]);
+          bulk_commit();
+          ++stored;
+        }
+      }
     }
-    const Move next = look_up(item + gridDim.x);
-    if (wide) {
-#pragma unroll
-      for (int k = 0; k < kVecs; ++k) if ((tid + k * kCopyThreads) * 16 < now.left) reinterpret_cast<uint4*>(now.dst)[tid + k * kCopyThreads] = v[k];
-    } else {
-      for (int k = tid * 4; k < now.left; k += kCopyThreads * 4) *reinterpret_cast<uint32_t*>(now.dst + k) = *reinterpret_cast<const uint32_t*>(now.src + k);
+    bulk_wait();
+    if (fail)                                              // (an internal error)
+      for (int i = 0; i < a.n_failed; ++i) { if (a.compact) a.failed[i] = -1; else atomicOr(a.failed + i, TSV_ST_INTERNAL); }
+  } else if (tid >= 32) {
+    const int t = tid - 32, n = kCopyThreads - 32;
+    const int64_t items = (int64_t)pairs * per_row;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+      const int i = (int)(item / per_row), c = per_plane + (int)(item - (int64_t)i * per_row);
+      int lo = planes, hi = a.n;
+      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (a.chunk0[mid] <= c) lo = mid; else hi = mid; }
+      const int2 pr = a.w.rows[i];
+      if (pr.x < 0) continue;
+      const int64_t bytes = a.bytes[lo], off = (int64_t)(c - a.chunk0[lo]) * kChunk;
+      const char* src = a.base[lo] + pr.x * bytes + off;
+      char* dst = a.base[lo] + pr.y * bytes + off;
+      const int left = (int)(bytes - off < kChunk ? bytes - off : kChunk);
+      if ((((uintptr_t)src | (uintptr_t)dst | (uintptr_t)left) & 15) == 0)
+        for (int k = t * 16; k < left; k += n * 16) *reinterpret_cast<uint4*>(dst + k) = *reinterpret_cast<const uint4*>(src + k);
+      else
+        for (int k = t * 4; k < left; k += n * 4) *reinterpret_cast<uint32_t*>(dst + k) = *reinterpret_cast<const uint32_t*>(src + k);
     }
-    now = next;
-  }
-  if (a.renumber) {
-    const int used = a.w.head[1];
-    const int64_t words = (int64_t)a.p.slots * a.p.max_pages;
-    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + tid; i < words; i += (int64_t)gridDim.x * kCopyThreads) {
-      const int pg = a.p.table[i];
-      if (pg >= used && pg < a.p.n_pages) a.p.table[i] = a.w.list[pg];
+    if (a.renumber) {
+      const int used = a.w.head[1];
+      const int64_t words = (int64_t)a.p.slots * a.p.max_pages;
+      for (int64_t i = (int64_t)blockIdx.x * n + t; i < words; i += (int64_t)gridDim.x * n) {
+        const int pg = a.p.table[i];
+        if (pg >= used && pg < a.p.n_pages) a.p.table[i] = a.w.list[pg];
+      }
     }
   }
 }
 
 Pool pool_of(const tsv_page_pool& p) { return {p.page_table, p.ref, p.slots, p.max_pages, p.n_pages, p.page_tokens}; }
 
-int launch_copies(const tsv_page_pool& p, const Work& w, bool rows, int64_t most_pairs, bool renumber, cudaStream_t st) {
+int launch_copies(const tsv_page_pool& p, const Work& w, bool rows, int64_t most_pairs, bool renumber, int32_t* failed, int n_failed, cudaStream_t st) {
   const int total = p.n_planes + (rows ? p.n_rows : 0);
   TSV_PREP(copy_kernel);
+  if (!ensure_smem((const void*)copy_kernel, kStages * kChunk)) return TSV_ERR_CUDA;
   for (int at = 0; at < total || (at == 0 && renumber); at += kArrays) {
     CopyArgs a;
     a.n = total - at < kArrays ? total - at : kArrays;
     a.n_planes = p.n_planes - at < 0 ? 0 : p.n_planes - at;
     a.w = w; a.p = pool_of(p);
+    a.compact = renumber;
     a.renumber = renumber && at == 0;
+    a.failed = failed; a.n_failed = n_failed;
     int64_t chunks = 0;
     for (int i = 0; i < a.n; ++i) {
       const tsv_page_array& x = at + i < p.n_planes ? p.planes[at + i] : p.rows[at + i - p.n_planes];
@@ -303,7 +342,7 @@ int launch_copies(const tsv_page_pool& p, const Work& w, bool rows, int64_t most
     if (renumber && grid < 32) grid = 32;
     if (grid > 148 * kCopyCtas) grid = 148 * kCopyCtas;
     if (grid < 1) grid = 1;
-    copy_kernel<<<(unsigned)grid, kCopyThreads, 0, st>>>(a);
+    copy_kernel<<<(unsigned)grid, kCopyThreads, kStages * kChunk, st>>>(a);
     count_launch();
   }
   return cudaGetLastError() == cudaSuccess ? TSV_OK : TSV_ERR_CUDA;
@@ -335,7 +374,7 @@ int launch_pages_fork(const tsv_page_pool& p, int n, const int32_t* src, const i
   TSV_PREP(list_kernel<true>);
   list_kernel<true><<<1, kPlanThreads, 0, st>>>(pool_of(p), n, src, dst, nullptr, nullptr, L, w, status);
   count_launch();
-  return launch_copies(p, w, true, n, false, st);
+  return launch_copies(p, w, true, n, false, status, n, st);
 }
 
 int launch_pages_compact(const tsv_page_pool& p, int32_t* n_used, char* ws, cudaStream_t st) {
@@ -343,7 +382,7 @@ int launch_pages_compact(const tsv_page_pool& p, int32_t* n_used, char* ws, cuda
   TSV_PREP(compact_kernel);
   compact_kernel<<<1, kPlanThreads, 0, st>>>(pool_of(p), w, n_used);
   count_launch();
-  return launch_copies(p, w, false, p.n_pages / 2, true, st);
+  return launch_copies(p, w, false, p.n_pages / 2, true, n_used, 1, st);
 }
 
 }  // namespace tsv

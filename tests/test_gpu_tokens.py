@@ -466,6 +466,23 @@ def test_commit(api, dtype, Hk, d, shared, page, n, window, paths):
     assert lay.cache.L.tolist() == [a + len(w) for a, w in zip(L, want)] and not lay.status.any()
 
 
+@pytest.mark.parametrize("Hk,shared", [(48, False), (24, True)])
+def test_commit_of_wide_rows(api, Hk, shared):
+    """Rows of keys and values that a CTA's shared memory holds none of, or one."""
+    _, tk, _ = api
+    lay = Layer(tk, "fp32", Hk, Hk, 512, shared, window=4, sinks=0, L=[3, 0, 9], n=[70, 0, 2], page=16, seed=1)
+    exp = [x.clone() for x in [lay.cache.k] + ([] if shared else [lay.cache.v])]
+    for b in range(3):
+        for i in range(lay.n[b]):
+            pos = lay.L[b] + i
+            for e, src in zip(exp, [lay.k, lay.v]):
+                e[lay.table[b, pos // 16] * 16 + pos % 16] = src[lay.row0[b] + i]
+    tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, lay.status)
+    for x, e in zip([lay.cache.k] + ([] if shared else [lay.cache.v]), exp):
+        assert torch.equal(x.nan_to_num(9), e.nan_to_num(9))
+    assert lay.cache.L.tolist() == [73, 0, 11] and not lay.status.any()
+
+
 @pytest.mark.parametrize("big", [False, True])
 def test_commit_flags(api, big):
     tsv, tk, _ = api
