@@ -5,9 +5,11 @@
 //   warps 4-7    softmax of the second tile; where there is one tile, its epilogue, under the next item's scores and softmax
 //   warp 8       issues the products: S = Q K^T, then O += P V with P as the A operand straight from tensor memory
 //   warp 9       finds the items ahead of the others: tile, keys, tree
-//   warps 10-13  copy Q, K and V rows into shared memory (16-byte asynchronous copies: rows come from pages, a ring or the call's own
-//                tensors, any of them with strides of their own, which no tensor map describes); a barrier counts a panel's copies as
-//                they land, and the thread that issues the products orders them before its reads (fence.proxy.async)
+//   warps 10-13  copy groups of panels of K and V into shared memory, 32 rows each: two for what only S reads, two for the output columns, or
+//                all four for these where K is V (a wait for a barrier's phase is only good for a thread that sees all of them).  Rows come by 16-byte asynchronous copies: from pages, a ring or the call's own tensors, any of
+//                them with strides of their own, which no tensor map describes; a barrier counts a group's copies as they land, and the
+//                thread that issues the products orders them before its reads (fence.proxy.async)
+//   warp 14      Q, by TMA where the heads of a key head fill a box evenly, else like K and V
 // K and V live in panels of 128 rows (64 at d = 512) x 64 columns (128-byte swizzle): K row-major is the K-major operand of S, and the same
 // layout read MN-major the operand of P V, so that where the keys are the values one copy serves both products.  Two tiles share a
 // block of K and V: copies (half of the shared-memory traffic of a tile) and their instructions per product halve, and one tile's
@@ -22,6 +24,9 @@
 // where a later slab exceeds it by more than 2^10 (bf16 and fp32 have the range for weights above one), and then what is there of
 // P, the sum and O are multiplied by a power of two, exactly.  Nearly never after the first slab.
 // P is rounded to bf16 for the product (2^-9 of a weight); scores, sums and O are fp32.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include "tc_common.cuh"
 #include "tok_attn.cuh"
 
@@ -32,7 +37,7 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 128;            // query rows of a tile; columns of an S buffer
-constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 4, kTcThreads = 32 * (10 + kCopyWarps);
+constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 5, kTcThreads = 32 * (10 + kCopyWarps);
 constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
 constexpr float kGap = 10.f;          // log2 units by which a maximum may exceed the row's reference
@@ -51,6 +56,7 @@ struct Cfg {
   static constexpr int PB = BN * 128;                        // bytes of a panel of keys
   static constexpr int NKB = KP == 0 ? 0 : DP == 64 ? 4 : DP == 128 ? 2 : 1;          // buffers of a block's K groups
   static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : SHARED ? 2 : 1;   // of its V group
+  static constexpr int TEAM = KG ? 2 : 4;                    // warps that copy a group of K or V
   static constexpr int SMEM = kCtl + NT * NP * kPanel + (NKB * KP + NVB * VP) * PB;
 };
 
@@ -152,9 +158,15 @@ __device__ __forceinline__ float power_of_two(float x) {
 }
 
 struct TcArgs {
+  alignas(64) CUtensorMap q;    // [rows][H][d]; a box is 128 rows of a tile (G heads of 128 / G tokens, or 128 heads of one) x 64 columns
   AttnArgs a;
   int32_t items;
+  int32_t q_box;                // the queries come by it
 };
+__device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
 
 // What is rare stays out of the loops' code: at some 150 KB of it, the warp that issues the products took a thousand cycles for the forty
 // instructions of a panel.
@@ -224,7 +236,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
   if (tid == 0) {
     for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], 9 + kCopyWarps); }
-    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullQ[i], 32 * kCopyWarps); bar_init(&sm.fullV[i], 32 * kCopyWarps); bar_init(&sm.fullK[i], 32 * kCopyWarps); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
+    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.fullV[i], 32 * C::TEAM); bar_init(&sm.fullK[i], 32 * C::TEAM); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
     for (int i = 0; i < 2; ++i) { bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.pv_done[i], 1); bar_init(&sm.o_free[i], kTile); }
     bar_init(&sm.emptyQ, 1); bar_init(&sm.o_full, 1); bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -333,98 +345,111 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     }
   } else if (warp > kListWarp) {
     // ------------------------------------------------------------------ producers
-    // A thread copies one 16-byte chunk of the rows prow + ROWS i of a panel; where these rows are is worked out by the eight threads of
-    // a row together (row i by thread i of them), a block ahead.
-    constexpr int ROWS = 4 * kCopyWarps, PQ = kTile / ROWS, PK = C::BN / ROWS;
-    static_assert(PQ == 8 && PK <= 8, "a thread of eight for each row of a thread");
-    const int pt = tid - 32 * (kListWarp + 1), prow = pt >> 3, chunk = pt & 7;
-    const int dch = a.s.d / 8;
-    uint32_t par_e = 0, par_k = 0, par_v = 0;              // parities of Q and of the buffers of K and V groups
-    int kb = 0, vb = 0;                                    // next buffers
-    const uint32_t off = (uint32_t)prow * 128 + ((chunk ^ (prow & 7)) << 4);     // (rows 16 apart: the same swizzle)
-    walk([&](const Item& w) {
-      const int nb = w.nb;
-      if (nb == 0) return;
-      const int mode = w.mode, half = w.half, hk = w.t.hk;
-      int64_t code = -1;                                   // of this thread's row in the next block
-      auto find = [&](int j) {
-        const int kk = w.k0 + j * C::BN + prow + ROWS * chunk;
-        code = chunk < PK && kk < w.k1 ? list_row(a, w.t, kk) : -1;
-      };
-      // Groups of panels: of block j those of K that only S reads and that of the output columns, of Q each tile's.
-      // The first block comes before Q: its buffers are free before Q's, which the item before reads to its last block.
-      find(0);
-#pragma unroll 1
-      for (int j = 0;; ++j) {
-        const int first = j == 1 ? -w.nt * C::NG : 0, last = j < nb ? C::KG + 1 : 0;
-        const int64_t now = code;
-        if (j + 1 < nb) find(j + 1);
-        const int rows16 = (min(C::BN, w.k1 - w.k0 - j * C::BN) + 15) & ~15;
-#pragma unroll 1
-        for (int grp = first; grp < last; ++grp) {
-          const bool is_q = grp < 0, is_v = grp == C::KG;
-          const int qg = grp + w.nt * C::NG;               // (tile, group) of Q
-          unsigned long long mine = 0;
-          if (is_q) {
-            const int r = qg / C::NG * kTile + prow + ROWS * chunk, gr = w.t.r0 + r;
-            if (r < w.t.nr) mine = reinterpret_cast<unsigned long long>(reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)hk * a.G + gr % a.G) * a.s.d);
-          } else if (now != -1) {
-            mine = reinterpret_cast<unsigned long long>(row_ptr<bf16>(a, hk, now, is_v));
-          }
-          // in the order in which S takes them: the item's own output columns last where K is V
-          const int g = is_q ? qg % C::NG : grp;
-          const int pan0 = is_v ? half * C::VP : SHARED && C::KG ? (g + half + 1) % C::NG * C::GP : g * C::GP;
-          const int rows = is_q ? kTile : rows16;
-          uint64_t* bar;
-          uint32_t to;
-          if (is_q) {
-            if (grp == first) { wait(&sm.emptyQ, par_e & 1 ^ 1); par_e ^= 1; }
-            bar = sm.fullQ + qg;
-            to = q_at + qg * C::GP * kPanel;
-          } else if (is_v) {
-            wait(&sm.emptyV[vb], (par_v >> vb & 1) ^ 1);
-            par_v ^= 1u << vb;
-            bar = sm.fullV + vb;
-            to = v_at + vb * C::VP * C::PB;
-            vb = vb + 1 == C::NVB ? 0 : vb + 1;
-          } else {
-            wait(&sm.emptyK[kb], (par_k >> kb & 1) ^ 1);
-            par_k ^= 1u << kb;
-            bar = sm.fullK + kb;
-            to = k_at + kb * C::GP * C::PB;
-            kb = kb + 1 == C::NKB * C::KG ? 0 : kb + 1;
-          }
-          to += off;
-          const bf16* ptr[PQ];                             // this thread's chunk in the group's first panel, of its rows (nullptr: nothing there)
+    // Four rows x 128 bytes go with an instruction; a lane knows where the rows lane, lane + 32, .. of the warp's share begin.
+    const int chunk = lane & 7, sub = lane >> 3, dch = a.s.d / 8, me = warp - kListWarp - 1;
+    const char* none = reinterpret_cast<const char*>(a.in.q);
+    // 32 rows from r0 on of a group of panels that begins at column 64 pan0; at: where row r0 + lane begins (0: nothing there)
+    auto rows32 = [&](uint32_t to, uint32_t stride, int r0, int pan0, unsigned long long at) {
 #pragma unroll
-          for (int i = 0; i < PQ; ++i) {
-            const unsigned long long x = __shfl_sync(0xffffffffu, mine, (lane & ~7) | i);
-            ptr[i] = x ? reinterpret_cast<const bf16*>(x) + pan0 * 64 + chunk * 8 : nullptr;
-          }
-          const int stride = is_q ? kPanel : C::PB;
-#pragma unroll 1
-          for (int p = 0; p < C::GP; ++p) {
-            const bool in = (pan0 + p) * 8 + chunk < dch;
+      for (int i = 0; i < 8; ++i) {
+        const unsigned long long b = __shfl_sync(0xffffffffu, at, 4 * i + sub);
+        const int r = r0 + 4 * i + sub;
+        const uint32_t dst = to + r * 128 + ((chunk ^ (r & 7)) << 4);
+        const char* src = reinterpret_cast<const char*>(b) + (pan0 * 8 + chunk) * 16;
 #pragma unroll
-            for (int i = 0; i < PQ; ++i) {
-              if (ROWS * i >= rows) break;
-              const bool live = in && ptr[i];
-              cp16(to + p * stride + i * ROWS * 128, live ? ptr[i] + p * 64 : reinterpret_cast<const bf16*>(a.in.q), live);
+        for (int p = 0; p < C::GP; ++p) {
+          const bool live = b && (pan0 + p) * 8 + chunk < dch;
+          cp16(dst + p * stride, live ? src + p * 128 : none, live);
+        }
+      }
+    };
+    // (in the order in which S takes them: the item's own output columns last where K is V)
+    auto first_panel = [&](int g, int half) { return SHARED && C::KG ? (g + half + 1) % C::NG * C::GP : g * C::GP; };
+    if (me == kCopyWarps - 1) {
+      uint32_t par = 1;
+      walk([&](const Item& w) {
+        if (w.nb == 0) return;
+        wait(&sm.emptyQ, par);
+        par ^= 1;
+#pragma unroll 1
+        for (int qg = 0; qg < w.nt * C::NG; ++qg) {        // (tile, group)
+          const int r0 = w.t.r0 + qg / C::NG * kTile, pan0 = first_panel(qg % C::NG, w.half), hk = w.t.hk;
+          const uint32_t to = q_at + qg * C::GP * kPanel;
+          if (g.q_box) {
+            if (lane == 0) {
+              const uint32_t bar = smem_u32(sm.fullQ + qg);
+              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::GP * kPanel) : "memory");
+              for (int p = 0; p < C::GP; ++p) tma_box3(to + p * kPanel, &g.q, (pan0 + p) * 64, hk * a.G + r0 % a.G, (int)(w.t.row0 + r0 / a.G), bar);
             }
-          }
-          if (mode == 2 && is_v) {                         // (what this thread has copied)
-            cp_commit();
-            cp_wait<0>();
-            for (int p = 0; p < C::GP; ++p)
-              for (int i = 0; ROWS * i < rows; ++i) make_finite<bf16>(smem_raw + (to + p * stride + i * ROWS * 128 - smem_u32(smem_raw)));
-            bar_arrive(bar);
+            __syncwarp();
           } else {
-            bar_arrive_copied(bar);
+#pragma unroll 1
+            for (int x = 0; x < kTile; x += 32) {
+              const int gr = r0 + x + lane;
+              unsigned long long at = 0;
+              if (gr - w.t.r0 < w.t.nr) at = reinterpret_cast<unsigned long long>(reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)hk * a.G + gr % a.G) * a.s.d);
+              rows32(to, kPanel, x, pan0, at);
+            }
+            bar_arrive_copied(sm.fullQ + qg);
           }
         }
-        if (j >= nb) break;
-      }
-    });
+      });
+    } else {
+      const bool is_v = !C::KG || me >= C::TEAM;
+      const int r0 = 32 * (me % C::TEAM);                  // of a block's rows, and every 32 TEAM rows on
+      uint64_t* full = is_v ? sm.fullV : sm.fullK;
+      uint64_t* room = is_v ? sm.emptyV : sm.emptyK;
+      const uint32_t base_at = is_v ? v_at : k_at;
+      const int nbuf = is_v ? C::NVB : C::NKB * C::KG;
+      uint32_t par = 0xffffffffu;                          // a bit per buffer
+      int buf = 0;
+      walk([&](const Item& w) {
+        const int nb = w.nb;
+        if (nb == 0) return;
+        const int half = w.half, hk = w.t.hk;
+        constexpr int X = C::BN / (32 * C::TEAM) > 0 ? C::BN / (32 * C::TEAM) : 1;
+        unsigned long long at[X];
+        auto find = [&](int j) {                           // where this lane's rows of block j begin
+#pragma unroll
+          for (int x = 0; x < X; ++x) {
+            const int r = r0 + 32 * C::TEAM * x + lane, kk = w.k0 + j * C::BN + r;
+            at[x] = 0;
+            if (r < C::BN && kk < w.k1) {
+              const int64_t code = list_row(a, w.t, kk);
+              if (code != -1) at[x] = reinterpret_cast<unsigned long long>(row_ptr<bf16>(a, hk, code, is_v));
+            }
+          }
+        };
+        find(0);
+#pragma unroll 1
+        for (int j = 0; j < nb; ++j) {
+          const int rows16 = (min(C::BN, w.k1 - w.k0 - j * C::BN) + 15) & ~15;
+#pragma unroll 1
+          for (int grp = 0; grp < (is_v ? 1 : C::KG); ++grp) {
+            const uint32_t to = base_at + buf * C::GP * C::PB;
+            const int pan0 = is_v ? half * C::VP : first_panel(grp, half);
+            wait(&room[buf], par >> buf & 1);
+#pragma unroll
+            for (int x = 0; x < X; ++x)
+              if (r0 + 32 * C::TEAM * x < rows16) rows32(to, C::PB, r0 + 32 * C::TEAM * x, pan0, at[x]);
+            if (w.mode == 2 && is_v) {                     // (what this thread has copied)
+              cp_commit();
+              cp_wait<0>();
+              for (int p = 0; p < C::GP; ++p)
+                for (int x = 0; x < X; ++x)
+                  for (int r = r0 + 32 * C::TEAM * x + sub, e = 0; e < 8 && r0 + 32 * C::TEAM * x < rows16; ++e, r += 4)
+                    make_finite<bf16>(smem_raw + (to + p * C::PB + r * 128 + ((chunk ^ (r & 7)) << 4) - smem_u32(smem_raw)));
+              bar_arrive(&full[buf]);
+            } else {
+              bar_arrive_copied(&full[buf]);
+            }
+            par ^= 1u << buf;
+            buf = buf + 1 == nbuf ? 0 : buf + 1;
+          }
+          if (j + 1 < nb) find(j + 1);
+        }
+      });
+    }
     cp_commit();
     cp_wait<0>();
   } else if (warp == kMmaWarp) {
@@ -580,31 +605,39 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             tmem_ld16x256b_x8_nowait(ocol + ((uint32_t)(16 * hh) << 16) + c, r);
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             tmem_regs_ready(r);
+            uint32_t x[4][4];                             // [2 h + k]: words of the 8-column groups 4 k .. 4 k + 3, columns 8 g + 2 qi, + 1
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t wd[8];                             // words of 8-column groups g = 0 .. 7: columns 8 g + 2 qi, + 1
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
               for (int gq = 0; gq < 8; ++gq) {
                 const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[4 * gq + 2 * h]) * iv[h], __uint_as_float(r[4 * gq + 2 * h + 1]) * iv[h]);
                 nz[h] = __hfma2(v, zero2, nz[h]);
-                wd[gq] = *reinterpret_cast<const uint32_t*>(&v);
+                x[2 * h + (gq >> 2)][gq & 3] = *reinterpret_cast<const uint32_t*>(&v);
               }
+            // lane qi gets all words of group 4 k + qi; eight exchanges at a time, which need not wait for one another
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {               // groups 4 k .. 4 k + 3: lane qi gets all words of group 4 k + qi
-                uint32_t x[4] = {wd[4 * k], wd[4 * k + 1], wd[4 * k + 2], wd[4 * k + 3]};
+            for (int m = 1; m <= 2; m <<= 1) {
+              const bool upper = (qi & m) != 0;
+              uint32_t got[4][2];
 #pragma unroll
-                for (int m = 1; m <= 2; m <<= 1) {
-                  const bool upper = (qi & m) != 0;
+              for (int y = 0; y < 4; ++y)
 #pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    if (!(i & m)) {
-                      const uint32_t send = upper ? x[i] : x[i | m], got = __shfl_xor_sync(FULL, send, m);
-                      if (upper) x[i] = got; else x[i | m] = got;
-                    }
+                for (int i = 0; i < 2; ++i) {
+                  const int lo = m == 1 ? 2 * i : i;
+                  got[y][i] = __shfl_xor_sync(FULL, upper ? x[y][lo] : x[y][lo | m], m);
                 }
-                const int col = c + (4 * k + qi) * 8;
-                if (okr[h] && w.half * C::OC + col < a.s.d) *reinterpret_cast<uint4*>(o[h] + col) = make_uint4(x[0], x[1], x[2], x[3]);
-              }
+#pragma unroll
+              for (int y = 0; y < 4; ++y)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  const int lo = m == 1 ? 2 * i : i;
+                  if (upper) x[y][lo] = got[y][i]; else x[y][lo | m] = got[y][i];
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int col = c + (4 * (y & 1) + qi) * 8;
+              if (okr[y >> 1] && w.half * C::OC + col < a.s.d) *reinterpret_cast<uint4*>(o[y >> 1] + col) = make_uint4(x[y][0], x[y][1], x[y][2], x[y][3]);
             }
           }
 #pragma unroll
@@ -681,24 +714,29 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             uint32_t sv[64];
             tmem_ld32_nowait(scol + 64 * i, sv);
             tmem_ld32_nowait(scol + 64 * i + 32, sv + 32);
-            const bool whole = !missing && c >= all0 && c + 64 <= all1;
-            uint32_t vis[2] = {FULL, FULL};
-            if (!whole) {
+            uint32_t vis[2];
+            bool whole[2];
 #pragma unroll
-              for (int v = 0; v < 2; ++v) {
-                const int cv = c + 32 * v, x = nc - cv;
+            for (int v = 0; v < 2; ++v) {
+              const int cv = c + 32 * v, x = nc - cv;
+              whole[v] = !missing && cv >= all0 && cv + 32 <= all1;
+              vis[v] = FULL;
+              if (!whole[v]) {
                 vis[v] = bits(kmin - cv, min(kmax + 1, nc) - cv) | bits(-cv, min(ksink, nc) - cv);
                 if (tree && x < 32 && x > -32) vis[v] |= x >= 0 ? nodes << x : nodes >> -x;
                 vis[v] &= bits(0, k1 - cv);
                 if (missing) vis[v] = have_pages(a, t, cv, vis[v]);
+                whole[v] = __all_sync(FULL, vis[v] == FULL);
               }
             }
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
             tmem_regs_ready(sv);
             tmem_regs_ready(sv + 32);
-            if (!whole) {
 #pragma unroll
-              for (int e = 0; e < 64; ++e) if (!(vis[e >> 5] >> (e & 31) & 1u)) sv[e] = 0xff800000u;
+            for (int v = 0; v < 2; ++v) {
+              if (whole[v]) continue;
+#pragma unroll
+              for (int e = 0; e < 32; ++e) if (!(vis[v] >> e & 1u)) sv[32 * v + e] = 0xff800000u;
             }
             float m8[8];
 #pragma unroll
@@ -761,11 +799,29 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
 }
 
+bool query_map(CUtensorMap* m, const AttnArgs& a) {
+  static PFN_cuTensorMapEncodeTiled fn = nullptr;
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled>(p);
+  }
+  if (!fn || a.bt.rows < 1) return false;
+  const cuuint64_t dim[3] = {(cuuint64_t)a.s.d, (cuuint64_t)a.s.H, (cuuint64_t)a.bt.rows};
+  const cuuint64_t stride[2] = {(cuuint64_t)a.s.d * 2, (cuuint64_t)a.in.q_ld * 2};
+  const cuuint32_t box[3] = {64u, (cuuint32_t)(a.G < 128 ? a.G : 128), (cuuint32_t)(a.G < 128 ? 128 / a.G : 1)}, one[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.in.q), dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DP, bool SHARED>
 int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
   typedef Cfg<DP, SHARED> C;
   TcArgs g;
   g.a = a;
+  // (heads that do not fill a box of 128 rows evenly, or rows beyond a tensor map's: by the copying warps' own loads)
+  g.q_box = (128 % a.G == 0 || a.G % 128 == 0) && a.bt.rows < (int64_t)1 << 31 && a.in.q_ld < (int64_t)1 << 38 && query_map(&g.q, a);
   const int64_t items = units * a.s.Hk * a.nsplit * C::HALVES;
   if (items > 0x7fffffff - 148) return TSV_ERR_LIMIT;
   g.items = (int32_t)items;

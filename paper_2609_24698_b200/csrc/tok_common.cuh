@@ -86,13 +86,21 @@ __device__ __forceinline__ int tok_tree(const tsv_tok_batch& bt, const TokUnit& 
   return TSV_OK;
 }
 
-// Row of the token cache that holds position pos of sequence b; -1: no such page.
+// Row of the token cache that holds position pos of sequence b; -1: no such page.  (Page sizes are powers of two nearly always, and a
+// ring's turn is a subtraction where the position is less than a window beyond: a division is some forty instructions.)
 __device__ __forceinline__ int64_t tok_cache_row(const tsv_tok_cache& c, int window, int n_sink, int b, int pos) {
-  if (!c.page_table) return (int64_t)b * ((int64_t)n_sink + window) + (pos < n_sink ? pos : n_sink + (pos - n_sink) % window);
-  const int lp = pos / c.page_tokens;
+  if (!c.page_table) {
+    if (pos < n_sink) return (int64_t)b * ((int64_t)n_sink + window) + pos;
+    int at = pos - n_sink;
+    if (at >= window) { at -= window; if (at >= window) at %= window; }
+    return (int64_t)b * ((int64_t)n_sink + window) + n_sink + at;
+  }
+  const int P = c.page_tokens;
+  const bool pow2 = (P & (P - 1)) == 0;
+  const int sh = 31 - __clz(P), lp = pow2 ? pos >> sh : pos / P, in = pow2 ? pos & (P - 1) : pos - lp * P;
   if (lp >= c.max_pages) return -1;
   const int page = __ldg(c.page_table + (size_t)b * c.max_pages + lp);
-  const int64_t row = (int64_t)page * c.page_tokens + pos % c.page_tokens;
+  const int64_t row = (int64_t)page * P + in;
   return page < 0 || row >= c.rows ? -1 : row;
 }
 
