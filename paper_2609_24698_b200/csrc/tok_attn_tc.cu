@@ -119,9 +119,17 @@ __device__ __forceinline__ void bar_arrive_copied(uint64_t* b) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
 }
 __device__ __forceinline__ void fence_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-               ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc) : "memory");
+// The products with the descriptors' low words apart: the high ones never change, and each word goes to a uniform register of its own
+// for every product.
+__device__ __forceinline__ void mma_ss2(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+               ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void mma_ts2(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+               ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(acc) : "memory");
 }
 // Bits [lo, hi) of a word, any lo and hi.
 __device__ __forceinline__ uint32_t bits(int lo, int hi) {
@@ -487,7 +495,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 #pragma unroll
             for (int k = 0; k < C::BN / 16; ++k) {
               if (16 * k >= left) break;
-              mma_ts(oc, pc + 8 * k, vd + k * (2048 >> 4), idesc_v, k ? 1u : (uint32_t)ob);
+              mma_ts2(oc, pc + 8 * k, (uint32_t)vd + k * (2048 >> 4), (uint32_t)(vd >> 32), idesc_v, k ? 1u : (uint32_t)ob);
             }
             if (last) { mma_commit(&sm.emptyV[vo]); par_vo ^= 1u << vo; vo = vo + 1 == C::NVB ? 0 : vo + 1; }
             mma_commit(&sm.pv_done[t]);
@@ -506,7 +514,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
               const uint64_t kd = make_desc(k_only ? k_at + at_k * C::GP * C::PB : v_at + vs * C::VP * C::PB, 16, 1024);
 #pragma unroll
               for (int i = 0; i < 4 * C::GP; ++i)
-                mma_ss(dst, qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), idesc, i ? 1u : (uint32_t)g);
+                mma_ss2(dst, (uint32_t)qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), (uint32_t)(qd >> 32), (uint32_t)kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), (uint32_t)(kd >> 32), idesc, i ? 1u : (uint32_t)g);
               if (k_only) {
                 if (last) { mma_commit(&sm.emptyK[at_k]); par_k ^= 1u << at_k; }
                 at_k = at_k + 1 == C::NKB * C::KG ? 0 : at_k + 1;
