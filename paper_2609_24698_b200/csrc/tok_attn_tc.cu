@@ -119,6 +119,16 @@ __device__ __forceinline__ void bar_arrive_copied(uint64_t* b) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
 }
 __device__ __forceinline__ void fence_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+// High word of the descriptors here (make_desc): 1024 bytes from eight rows to the next, descriptor version 1, 128-byte swizzle.  The low
+// one: address / 16, and the distance of 64-column panels / 16 where that counts.
+constexpr uint32_t kDescHi = 1024 >> 4 | 1u << 14 | 2u << 29;
+
 // The products with the descriptors' low words apart: the high ones never change, and each word goes to a uniform register of its own
 // for every product.
 __device__ __forceinline__ void mma_ss2(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc) {
@@ -261,29 +271,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 
   auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait(b, parity)) fail = 1; };
   // Calls body(item) for this CTA's items, as the list warp finds them, until it marks the end; then, where one has left a mark, for those.
-  // By a warp, or by its first thread alone.
-  auto walk_as = [&](auto&& body, bool alone) {
-    uint32_t c = 0;
+  auto walk = [&](auto&& body) {
+    uint32_t slot = 0, parity = 0;
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {
-      if (!alone || lane == 0) {
-        uint32_t slot = c % kItems, parity = c / kItems & 1;
 #pragma unroll 1
-        for (;;) {
-          wait(&sm.item_full[slot], parity);
-          if (!alone) fail = __any_sync(0xffffffffu, fail);
-          if (fail) break;                                 // (without its item a role has nothing to go by)
-          const Item& w = sm.item[slot];
-          const bool end = w.t.ok == 0;
-          if (!end) body(w);
-          if (!alone) __syncwarp();
-          if (lane == 0) bar_arrive(&sm.item_free[slot]);
-          ++c;
-          if (++slot == kItems) { slot = 0; parity ^= 1; }
-          if (end) break;
-        }
+      for (bool end = false; !end;) {
+        wait(&sm.item_full[slot], parity);
+        fail = __any_sync(0xffffffffu, fail);
+        if (fail) break;                                   // (without its item a role has nothing to go by)
+        const Item& w = sm.item[slot];
+        end = w.t.ok == 0;
+        if (!end) body(w);
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sm.item_free[slot]);
+        if (++slot == kItems) { slot = 0; parity ^= 1; }
       }
-      __syncwarp();
       if (round == 0) {
         __syncthreads();
         uint32_t any = 0;
@@ -292,8 +295,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       }
     }
   };
-  auto walk = [&](auto&& body) { walk_as(body, false); };
-  auto walk_one = [&](auto&& body) { walk_as(body, true); };
 
   if (warp == kListWarp) {
     // ------------------------------------------------------------------ items
@@ -461,11 +462,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     cp_commit();
     cp_wait<0>();
   } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------------ products (one thread)
+    // ------------------------------------------------------------------ products (issued by one thread of a converged warp)
     const uint32_t idesc_v = make_idesc(C::OC, 1);
     uint32_t par_q = 0, par_k = 0, par_vs = 0, par_vo = 0, par_p = 0, par_o = 3;     // parities: per tile, buffers (of V for S and for O), S buffer, tile
     int kb = 0, vs = 0, vo = 0, sx = 0;                    // next K buffer, V buffer (for S, for O), S buffer of one tile
-    walk_one([&](const Item& w) {
+    const bool one = elect_one();
+    walk([&](const Item& w) {
       const int nb = w.nb, nt = NT == 2 ? w.nt : 1, k_all = w.k1 - w.k0;
       if (nb == 0) return;
       // A step: scores of block sb (of tile t), output of the block before.  Two tiles: P V first, whose P lies where the scores will.
@@ -481,7 +483,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         const bool last = t == nt - 1;
 #pragma unroll 1
         for (uint32_t spins = 0; g < C::NG || !out; ++spins) {
-          if (!out && (NT == 2 || fail || g == C::NG || (bar_ready(&sm.p_ready[xo], par_p >> xo & 1) && (ob || bar_ready(&sm.o_free[0], par_o & 1))))) {
+          fail = __any_sync(0xffffffffu, fail);
+          if (!out && (NT == 2 || fail || g == C::NG ||
+                       __any_sync(0xffffffffu, bar_ready(&sm.p_ready[xo], par_p >> xo & 1) && (ob || bar_ready(&sm.o_free[0], par_o & 1))))) {
             // O (+)= P V of block ob
             if (!SHARED) wait(&sm.fullV[vo], par_vo >> vo & 1);
             if (ob == 0) { wait(&sm.o_free[t], par_o >> t & 1); par_o ^= 1u << t; }
@@ -489,40 +493,50 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             par_p ^= 1u << xo;
             fence_proxy();
             fence_after();
-            const uint64_t vd = make_desc(v_at + vo * C::VP * C::PB, C::PB, 1024);
-            const uint32_t pc = s_col + xo * kTile, oc = o_col + t * C::OC;
-            const int left = k_all - ob * C::BN;
+            // (values that the compiler knows to be the warp's: they go through uniform registers, one instruction each for a product)
+            const uint32_t vd = uniform((v_at + vo * C::VP * C::PB) >> 4 | C::PB >> 4 << 16), pc = uniform(s_col + xo * kTile), oc = uniform(o_col + t * C::OC);
+            const uint32_t left = uniform(k_all - ob * C::BN), more = uniform(ob);
+            if (one) {
 #pragma unroll
-            for (int k = 0; k < C::BN / 16; ++k) {
-              if (16 * k >= left) break;
-              mma_ts2(oc, pc + 8 * k, (uint32_t)vd + k * (2048 >> 4), (uint32_t)(vd >> 32), idesc_v, k ? 1u : (uint32_t)ob);
+              for (int k = 0; k < C::BN / 16; ++k) {
+                if (16 * k >= (int)left) break;
+                mma_ts2(oc, pc + 8 * k, vd + k * (2048 >> 4), kDescHi, idesc_v, k ? 1u : more);
+              }
+              if (last) mma_commit(&sm.emptyV[vo]);
+              mma_commit(&sm.pv_done[t]);
+              if (NT == 1 && ob == nb - 1) mma_commit(&sm.o_full);
             }
-            if (last) { mma_commit(&sm.emptyV[vo]); par_vo ^= 1u << vo; vo = vo + 1 == C::NVB ? 0 : vo + 1; }
-            mma_commit(&sm.pv_done[t]);
-            if (NT == 1 && ob == nb - 1) mma_commit(&sm.o_full);
+            __syncwarp();
+            if (last) { par_vo ^= 1u << vo; vo = vo + 1 == C::NVB ? 0 : vo + 1; }
             out = true;
           } else if (g < C::NG) {
             const bool k_only = g < C::KG;
             uint64_t* b = k_only ? &sm.fullK[at_k] : &sm.fullV[vs];
             const uint32_t parity = (k_only ? par_k >> at_k : par_vs >> vs) & 1;
-            if (out || fail || bar_ready(b, parity)) {
+            if (out || fail || __any_sync(0xffffffffu, bar_ready(b, parity))) {
               wait(b, parity);
               if (sb == 0) wait(&sm.fullQ[t * C::NG + g], par_q >> t & 1);
               fence_proxy();
               fence_after();
-              const uint64_t qd = make_desc(q_at + (t * C::NG + g) * C::GP * kPanel, 16, 1024);
-              const uint64_t kd = make_desc(k_only ? k_at + at_k * C::GP * C::PB : v_at + vs * C::VP * C::PB, 16, 1024);
+              const uint32_t qd = uniform((q_at + (t * C::NG + g) * C::GP * kPanel) >> 4 | 1u << 16);
+              const uint32_t kd = uniform((k_only ? k_at + at_k * C::GP * C::PB : v_at + vs * C::VP * C::PB) >> 4 | 1u << 16);
+              const uint32_t to = uniform(dst), id = uniform(idesc), more = uniform(g);
+              if (one) {
 #pragma unroll
-              for (int i = 0; i < 4 * C::GP; ++i)
-                mma_ss2(dst, (uint32_t)qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), (uint32_t)(qd >> 32), (uint32_t)kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), (uint32_t)(kd >> 32), idesc, i ? 1u : (uint32_t)g);
+                for (int i = 0; i < 4 * C::GP; ++i)
+                  mma_ss2(to, qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), kDescHi, kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), kDescHi, id, i ? 1u : more);
+                if (k_only && last) mma_commit(&sm.emptyK[at_k]);
+                if (g == C::NG - 1) {
+                  mma_commit(&sm.s_full[xs]);
+                  if (last && sb == nb - 1) mma_commit(&sm.emptyQ);
+                }
+              }
+              __syncwarp();
               if (k_only) {
-                if (last) { mma_commit(&sm.emptyK[at_k]); par_k ^= 1u << at_k; }
+                if (last) par_k ^= 1u << at_k;
                 at_k = at_k + 1 == C::NKB * C::KG ? 0 : at_k + 1;
               }
-              if (++g == C::NG) {
-                mma_commit(&sm.s_full[xs]);
-                if (last && sb == nb - 1) mma_commit(&sm.emptyQ);
-              }
+              ++g;
               spins = 0;
             }
           }
