@@ -169,6 +169,16 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return r;
 }
 
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 32 bytes at a 32-byte boundary
+__device__ __forceinline__ void store32(void* p, const uint32_t* r) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
 // 2^x for a whole x <= 0, exactly (below the smallest normal number: 0).
 __device__ __forceinline__ float power_of_two(float x) {
   const int e = (int)fmaxf(x, -127.f) + 127;
@@ -604,71 +614,36 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         odd |= !(nz == 0.f);
         if (live && lead && mode != 1) a.pml[part] = make_float2(ref, sum);
       } else {
-        // read out so that four lanes share a row: they transpose their words, and a warp stores whole 128-byte lines of eight rows
+        // a row per lane, 32 bytes of it at a time: whole sectors, no exchanges between lanes
         const float inv = 1.f / sum;
-        const int quad = lane >> 2, qi = lane & 3;
+        const uint64_t inv2 = pair2(inv, inv);
+        bf16* o = out_at(t, min(rt + row, t.nr - 1)) + w.half * C::OC;
+        const bool put = live && mode != 1, wide = (((uintptr_t)a.out | (uintptr_t)(a.s.d * 2)) & 31) == 0;
         const __nv_bfloat162 zero2 = __floats2bfloat162_rn(0.f, 0.f);
+        __nv_bfloat162 nz[2] = {zero2, zero2};             // 0 x each value: NaN where one is not finite
 #pragma unroll 1
-        for (int hh = 0; hh < 2; ++hh) {
-          float iv[2];
-          bf16* o[2];
-          bool okr[2];
-          __nv_bfloat162 nz[2] = {zero2, zero2};
+        for (int c = 0; c < C::OC; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(ocol + c, r);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = 16 * hh + 8 * h + quad;
-            iv[h] = __shfl_sync(FULL, inv, r);
-            okr[h] = r0 + r < t.nr && mode != 1;
-            o[h] = out_at(t, min(r0 + r, t.nr - 1)) + w.half * C::OC;
+          for (int e = 0; e < 32; e += 2) {
+            const float2 x = unpair(mul2(pair2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), inv2));
+            const __nv_bfloat162 v = __floats2bfloat162_rn(x.x, x.y);
+            nz[(e >> 1) & 1] = __hfma2(v, zero2, nz[(e >> 1) & 1]);
+            r[e >> 1] = *reinterpret_cast<const uint32_t*>(&v);
           }
-#pragma unroll 1
-          for (int c = 0; c < C::OC; c += 64) {
-            uint32_t r[32];
-            tmem_ld16x256b_x8_nowait(ocol + ((uint32_t)(16 * hh) << 16) + c, r);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            tmem_regs_ready(r);
-            uint32_t x[4][4];                             // [2 h + k]: words of the 8-column groups 4 k .. 4 k + 3, columns 8 g + 2 qi, + 1
+          const int left = a.s.d - w.half * C::OC - c;     // columns that there are
+          if (put && wide) {
+            if (left >= 16) store32(o + c, r);
+            if (left >= 32) store32(o + c + 16, r + 8);
+          } else if (put) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int gq = 0; gq < 8; ++gq) {
-                const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[4 * gq + 2 * h]) * iv[h], __uint_as_float(r[4 * gq + 2 * h + 1]) * iv[h]);
-                nz[h] = __hfma2(v, zero2, nz[h]);
-                x[2 * h + (gq >> 2)][gq & 3] = *reinterpret_cast<const uint32_t*>(&v);
-              }
-            // lane qi gets all words of group 4 k + qi; eight exchanges at a time, which need not wait for one another
-#pragma unroll
-            for (int m = 1; m <= 2; m <<= 1) {
-              const bool upper = (qi & m) != 0;
-              uint32_t got[4][2];
-#pragma unroll
-              for (int y = 0; y < 4; ++y)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                  const int lo = m == 1 ? 2 * i : i;
-                  got[y][i] = __shfl_xor_sync(FULL, upper ? x[y][lo] : x[y][lo | m], m);
-                }
-#pragma unroll
-              for (int y = 0; y < 4; ++y)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                  const int lo = m == 1 ? 2 * i : i;
-                  if (upper) x[y][lo] = got[y][i]; else x[y][lo | m] = got[y][i];
-                }
-            }
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const int col = c + (4 * (y & 1) + qi) * 8;
-              if (okr[y >> 1] && w.half * C::OC + col < a.s.d) *reinterpret_cast<uint4*>(o[y >> 1] + col) = make_uint4(x[y][0], x[y][1], x[y][2], x[y][3]);
-            }
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {                   // a row's four lanes to the row's thread
-            const float2 z = __bfloat1622float2(nz[h]);
-            const uint32_t b = __ballot_sync(FULL, !(z.x == 0.f && z.y == 0.f));
-            if (lane >= 16 * hh + 8 * h && lane < 16 * hh + 8 * h + 8) odd |= (b >> (4 * (lane & 7)) & 15u) != 0;
+            for (int e = 0; e < 4; ++e)
+              if (8 * e < left) *reinterpret_cast<uint4*>(o + c + 8 * e) = make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);
           }
         }
+        const float2 za = __bfloat1622float2(nz[0]), zb = __bfloat1622float2(nz[1]);
+        odd |= !(za.x == 0.f && za.y == 0.f && zb.x == 0.f && zb.y == 0.f);
       }
       fence_before();
       bar_arrive(&sm.o_free[tile]);
