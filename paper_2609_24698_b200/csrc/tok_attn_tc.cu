@@ -37,47 +37,57 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 128;            // query rows of a tile; columns of an S buffer
-constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 5, kTcThreads = 32 * (10 + kCopyWarps);
+constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 5, kOutWarp = 15;
 constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
 constexpr float kGap = 10.f;          // log2 units by which a maximum may exceed the row's reference
 constexpr int kCtl = 3072;
 
+template <int N> struct Int { static constexpr int value = N; };
+
 template <int DP, bool SHARED>
 struct Cfg {
+  static constexpr int PAIR = DP == 512 ? 2 : 1;             // CTAs of an item, 256 columns each
   static constexpr int NT = DP <= 128 ? 2 : 1;               // tiles of an item
-  static constexpr int OC = DP < 256 ? DP : 256;             // output columns of an item
-  static constexpr int HALVES = DP / OC;
-  static constexpr int NP = DP / 64, VP = OC / 64;           // panels of all of d, of the output columns
-  static constexpr int KP = SHARED ? NP - VP : NP;           // panels that only S reads
-  static constexpr int GP = VP;                              // panels of a group: copied, announced and multiplied together
-  static constexpr int NG = NP / GP, KG = KP / GP;           // groups of all of d, of those that only S reads
-  static constexpr int BN = DP == 512 ? 64 : 128;            // keys of a block
+  static constexpr int OC = DP / PAIR;                       // columns of a CTA
+  static constexpr int NP = OC / 64;                         // panels of them: copied, announced and multiplied together
+  static constexpr int KP = SHARED ? 0 : NP;                 // panels of K where V has its own
+  static constexpr int QB = PAIR == 2 ? 2 : NT;              // tiles of Q in shared memory
+  static constexpr int BN = PAIR == 2 ? 48 : 128;            // keys of a block
+  static constexpr int SL = BN < 64 ? BN : 64;               // columns of a slab of S
   static constexpr int PB = BN * 128;                        // bytes of a panel of keys
-  static constexpr int NKB = KP == 0 ? 0 : DP == 64 ? 4 : DP == 128 ? 2 : 1;          // buffers of a block's K groups
-  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : SHARED ? 2 : 1;   // of its V group
-  static constexpr int TEAM = KG ? 2 : 4;                    // warps that copy a group of K or V
-  static constexpr int SMEM = kCtl + NT * NP * kPanel + (NKB * KP + NVB * VP) * PB;
+  static constexpr int NKB = KP == 0 ? 0 : DP == 64 ? 4 : DP == 128 ? 2 : 1;          // buffers of a block's K
+  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : DP == 256 ? (SHARED ? 2 : 1) : SHARED ? 3 : 2;   // of its V
+  static constexpr int SB = PAIR == 2 ? 4 : 2, SW = 2 * kTile / SB;  // buffers of S, their columns
+  static constexpr int WARPS = NT == 1 ? 16 : 15;
+  static constexpr int TEAM = KP ? 2 : 4;                    // warps that copy a block of K or V
+  static constexpr int RW = BN % (32 * TEAM) ? BN / TEAM : 32;       // rows that a warp copies at a time
+  static constexpr int XB = PAIR == 2 ? kTile * BN * 4 : 0;  // the other CTA's part of S
+  static constexpr int SMEM = kCtl + QB * NP * kPanel + (NKB + NVB) * NP * PB + XB;
 };
 
 // An item: tile, output columns, keys.  mode: 0 the first time; of those that left a mark then, 1 as before (which rows are not finite?)
 // and 2 with values that are not finite taken as zero.
 struct Item {
   TileList t;
-  int unit, half, split, k0, k1, nb, nt, mode, li;
+  int unit, split, k0, k1, nb, nt, mode, li;
   int missing;                        // a page of the list is not there
   int depth[TSV_MAX_D];
   uint32_t anc[TSV_MAX_D];
 };
 
 struct TcCtl {
-  uint64_t fullQ[4], emptyQ;                  // groups of panels: Q (tile, group), K (buffer, group), V (buffer)
+  uint64_t fullQ[2], emptyQ[2];               // by buffer
   uint64_t fullK[4], emptyK[4];
   uint64_t fullV[4], emptyV[4];
-  uint64_t s_full[2], p_ready[2], pv_done[2], o_free[2];
+  uint64_t s_full[4], p_ready[4], s_free[4], pv_done[2], o_free[2];      // (s_free: of one tile)
   uint64_t o_full, stat_full, stat_free;      // one tile: O is complete; reference and sum of its rows, for the epilogue
+  uint64_t x_full[4], x_free[4];              // a warp's rows of the other CTA's part of S: there; taken there, of this one's
+  uint64_t bad_full[2][4];                    // the other CTA's word of `bad`, by turns
+  uint32_t bad[2][4];                         // rows with a result that is not finite there, a bit each
   uint64_t item_full[kItems], item_free[kItems];
   uint32_t tmem_base;
+  uint32_t limit;                     // of a wait: polls
   uint32_t redo[32];                  // items with a result that is not finite, a bit each
   float2 stat[kTile];
   Item item[kItems];
@@ -90,10 +100,15 @@ __device__ __forceinline__ void bar_init(uint64_t* b, int count) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
 }
+__device__ __forceinline__ TcCtl& control() {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  return *reinterpret_cast<TcCtl*>(smem_raw);
+}
 // One bounded try in line, the others (to the limit) in a function: a wait is in the code of some thirty places.
 __device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
+  const uint32_t limit = control().limit;
 #pragma unroll 1
-  for (uint32_t it = 0; it < WAIT_LIMIT; ++it) {
+  for (uint32_t it = 0; it < limit; ++it) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
@@ -107,6 +122,27 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
   return ok || bar_wait_on(addr, parity);
+}
+// The same for what the other CTA of a pair sends.
+__device__ __noinline__ bool bar_wait_pair(uint64_t* bar, uint32_t parity) {
+  const uint32_t addr = smem_u32(bar), limit = control().limit;
+#pragma unroll 1
+  for (uint32_t it = 0; it < limit; ++it) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+__device__ __forceinline__ uint32_t other_cta(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Whether the phase is complete.
 __device__ __forceinline__ bool bar_ready(uint64_t* b, uint32_t parity) {
@@ -128,6 +164,8 @@ __device__ __forceinline__ bool elect_one() {
 // High word of the descriptors here (make_desc): 1024 bytes from eight rows to the next, descriptor version 1, 128-byte swizzle.  The low
 // one: address / 16, and the distance of 64-column panels / 16 where that counts.
 constexpr uint32_t kDescHi = 1024 >> 4 | 1u << 14 | 2u << 29;
+// (a CTA of a cluster has its rank in the address's upper bits)
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t far) { return (addr >> 4 & 0x3fff) | far << 16; }
 
 // The products with the descriptors' low words apart: the high ones never change, and each word goes to a uniform register of its own
 // for every product.
@@ -185,6 +223,17 @@ __device__ __forceinline__ float power_of_two(float x) {
   return __int_as_float(max(e, 0) << 23);
 }
 
+__device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_regs_ready16(uint32_t* r) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+
 struct TcArgs {
   alignas(64) CUtensorMap q;    // [rows][H][d]; a box is 128 rows of a tile (G heads of 128 / G tokens, or 128 heads of one) x 64 columns
   AttnArgs a;
@@ -207,20 +256,20 @@ __device__ __noinline__ uint32_t have_pages(const AttnArgs& a, const TileList& t
   }
   return m;
 }
-// Multiplies the first `slabs` slabs of P at p_col, and `cols` columns of O, by f (a power of two).
-__device__ __noinline__ void rescale(uint32_t p_col, int slabs, uint32_t o_col, int cols, float f) {
+// Multiplies the first `words` words (a multiple of 16) of P at p_col, and `cols` columns of O, by f (a power of two).
+__device__ __noinline__ void rescale(uint32_t p_col, int words, uint32_t o_col, int cols, float f) {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 #pragma unroll 1
-  for (int v = 0; v < slabs; ++v) {
+  for (int v = 0; v < words; v += 16) {
     uint32_t r[16];
-    tmem_ld16(p_col + 16 * v, r);
+    tmem_ld16(p_col + v, r);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const float2 pv = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r[e]));
       const __nv_bfloat162 h = __floats2bfloat162_rn(pv.x * f, pv.y * f);
       r[e] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    tmem_st16(p_col + 16 * v, r);
+    tmem_st16(p_col + v, r);
   }
 #pragma unroll 1
   for (int v = 0; v < cols; v += 16) {
@@ -252,34 +301,55 @@ __device__ __noinline__ void exact_output(const AttnArgs& a, const TileList& t, 
 }
 
 template <int DP, bool SHARED>
-__global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_constant__ TcArgs g) {
+__global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel(const __grid_constant__ TcArgs g) {
   typedef Cfg<DP, SHARED> C;
   constexpr int NT = C::NT;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const AttnArgs& a = g.a;
   TcCtl& sm = *reinterpret_cast<TcCtl*>(smem_raw);
   const uint32_t base = smem_u32(smem_raw) + kCtl;
-  const uint32_t q_at = base, k_at = q_at + NT * C::NP * kPanel, v_at = k_at + C::NKB * C::KP * C::PB;
+  const uint32_t q_at = base, k_at = q_at + C::QB * C::NP * kPanel, v_at = k_at + C::NKB * C::NP * C::PB, x_at = v_at + C::NVB * C::NP * C::PB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = C::PAIR == 2 ? (int)(blockIdx.x & 1) : 0, col0 = rank * C::OC;      // its columns: from col0 on
   int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
   if (tid == 0) {
-    for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], 9 + kCopyWarps); }
-    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.fullV[i], 32 * C::TEAM); bar_init(&sm.fullK[i], 32 * C::TEAM); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); }
-    for (int i = 0; i < 2; ++i) { bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.pv_done[i], 1); bar_init(&sm.o_free[i], kTile); }
-    bar_init(&sm.emptyQ, 1); bar_init(&sm.o_full, 1); bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
+    for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], C::WARPS - 1); }
+    for (int i = 0; i < 4; ++i) { bar_init(&sm.fullV[i], 32 * C::TEAM); bar_init(&sm.fullK[i], 32 * C::TEAM); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.s_free[i], 1); bar_init(&sm.x_full[i], 1); bar_init(&sm.x_free[i], 1); bar_init(&sm.bad_full[0][i], 1); bar_init(&sm.bad_full[1][i], 1); }
+    for (int i = 0; i < 2; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.emptyQ[i], 1); bar_init(&sm.pv_done[i], 1); bar_init(&sm.o_free[i], kTile); }
+    bar_init(&sm.o_full, 1); bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (tid == 0) sm.limit = WAIT_LIMIT;
   if (tid < 32) sm.redo[tid] = 0;
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  auto all_sync = [&]() { __syncwarp(); if (C::PAIR == 2) pair_sync(); else __syncthreads(); };
   fence_before();
-  __syncthreads();
+  all_sync();                                                   // (a pair: each has its barriers before the other reaches for them)
   fence_after();
   const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + 2 * kTile;
 
   auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait(b, parity)) fail = 1; };
+  // After the first round: whether there is a second (alike in all threads of a CTA or a pair).  It computes rows one by one, and its waits
+  // have 256 times the limit.
+  auto marks = [&](int i) {
+    uint32_t m = sm.redo[i & 31];
+    if (C::PAIR == 2) {
+      uint32_t v;
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(other_cta(&sm.redo[i & 31], rank ^ 1)) : "memory");
+      m |= v;
+    }
+    return m;
+  };
+  auto again = [&]() {
+    all_sync();
+    uint32_t any = 0;
+    for (int i = 0; i < 32; ++i) any |= marks(i);
+    if (tid == 0) sm.limit = WAIT_LIMIT << 8;
+    return any != 0;
+  };
   // Calls body(item) for this CTA's items, as the list warp finds them, until it marks the end; then, where one has left a mark, for those.
   auto walk = [&](auto&& body) {
     uint32_t slot = 0, parity = 0;
@@ -297,12 +367,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         if (lane == 0) bar_arrive(&sm.item_free[slot]);
         if (++slot == kItems) { slot = 0; parity ^= 1; }
       }
-      if (round == 0) {
-        __syncthreads();
-        uint32_t any = 0;
-        for (int i = 0; i < 32; ++i) any |= sm.redo[i];
-        if (!any) break;                                   // (alike in all threads)
-      }
+      if (round == 0 && !again()) break;
     }
   };
 
@@ -312,11 +377,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {
       int li = 0;
-      int idx = blockIdx.x;
+      int idx = blockIdx.x / C::PAIR;
 #pragma unroll 1
-      for (bool more = true; more; idx += gridDim.x, ++li) {
-        if (idx < g.items && round && !(sm.redo[(li >> 5) & 31] >> (li & 31) & 1u)) continue;
-        const int half = idx % C::HALVES, i1 = idx / C::HALVES, i2 = i1 / a.s.Hk, hk = i1 - i2 * a.s.Hk, unit = i2 / a.nsplit, split = i2 - unit * a.nsplit;
+      for (bool more = true; more; idx += gridDim.x / C::PAIR, ++li) {
+        if (idx < g.items && round && !(marks(li >> 5) >> (li & 31) & 1u)) continue;
+        const int i2 = idx / a.s.Hk, hk = idx - i2 * a.s.Hk, unit = i2 / a.nsplit, split = i2 - unit * a.nsplit;
 #pragma unroll 1
         for (int mode = round; more && mode <= 2 * round; ++mode, ++c) {
           wait(&sm.item_free[c % kItems], (c / kItems & 1) ^ 1);
@@ -342,63 +407,57 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           missing = __any_sync(0xffffffffu, missing);
           // The queries into L2, two items before they are copied: those copies all come at once, when Q is free, and left to them HBM would
           // idle in between.
-          if (nb && mode == 0 && half == 0) {
+          if (nb && mode == 0 && rank == 0) {
             const int t0 = t.r0 / a.G, t1 = (t.r0 + t.nr - 1) / a.G;
             for (int tok = t0 + lane; tok <= t1; tok += 32)
               asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const bf16*>(a.in.q) + (t.row0 + tok) * a.in.q_ld + (size_t)hk * a.G * a.s.d), "r"(a.G * a.s.d * 2) : "memory");
           }
           if (lane == 0) {
-            w.t = t; w.unit = unit; w.half = half; w.split = split; w.k0 = k0; w.k1 = k1; w.nb = nb; w.nt = t.ok && t.nr > kTile ? 2 : 1; w.mode = mode; w.li = li; w.missing = missing;
-            if (missing) atomicOr(a.status + t.b, TSV_ST_PAGE);
+            w.t = t; w.unit = unit; w.split = split; w.k0 = k0; w.k1 = k1; w.nb = nb; w.nt = t.ok && t.nr > kTile ? 2 : 1; w.mode = mode; w.li = li; w.missing = missing;
+            if (missing && rank == 0) atomicOr(a.status + t.b, TSV_ST_PAGE);
           }
           __syncwarp();
           if (lane == 0) bar_arrive(&sm.item_full[c % kItems]);
         }
       }
-      if (round == 0) {
-        __syncthreads();
-        uint32_t any = 0;
-        for (int i = 0; i < 32; ++i) any |= sm.redo[i];
-        if (!any || fail) break;
-      }
+      if (round == 0 && (!again() || fail)) break;
     }
-  } else if (warp > kListWarp) {
+  } else if (warp > kListWarp && warp < kOutWarp) {
     // ------------------------------------------------------------------ producers
     // Four rows x 128 bytes go with an instruction; a lane knows where the rows lane, lane + 32, .. of the warp's share begin.
     const int chunk = lane & 7, sub = lane >> 3, dch = a.s.d / 8, me = warp - kListWarp - 1;
     const char* none = reinterpret_cast<const char*>(a.in.q);
-    // 32 rows from r0 on of a group of panels that begins at column 64 pan0; at: where row r0 + lane begins (0: nothing there)
-    auto rows32 = [&](uint32_t to, uint32_t stride, int r0, int pan0, unsigned long long at) {
+    // Rows r0 .. r0 + n.value - 1 of this CTA's columns; at: where row r0 + lane begins (0: nothing there)
+    auto copy_rows = [&](auto n, uint32_t to, uint32_t stride, int r0, unsigned long long at) {
+      const int pan0 = rank * C::NP;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < decltype(n)::value / 4; ++i) {
         const unsigned long long b = __shfl_sync(0xffffffffu, at, 4 * i + sub);
         const int r = r0 + 4 * i + sub;
         const uint32_t dst = to + r * 128 + ((chunk ^ (r & 7)) << 4);
         const char* src = reinterpret_cast<const char*>(b) + (pan0 * 8 + chunk) * 16;
 #pragma unroll
-        for (int p = 0; p < C::GP; ++p) {
+        for (int p = 0; p < C::NP; ++p) {
           const bool live = b && (pan0 + p) * 8 + chunk < dch;
           cp16(dst + p * stride, live ? src + p * 128 : none, live);
         }
       }
     };
-    // (in the order in which S takes them: the item's own output columns last where K is V)
-    auto first_panel = [&](int g, int half) { return SHARED && C::KG ? (g + half + 1) % C::NG * C::GP : g * C::GP; };
     if (me == kCopyWarps - 1) {
-      uint32_t par = 1;
+      uint32_t par = 3, qb = 0;                            // a bit per buffer
       walk([&](const Item& w) {
         if (w.nb == 0) return;
-        wait(&sm.emptyQ, par);
-        par ^= 1;
+        if (C::PAIR == 1) { wait(&sm.emptyQ[0], par & 1); par ^= 1u; }
 #pragma unroll 1
-        for (int qg = 0; qg < w.nt * C::NG; ++qg) {        // (tile, group)
-          const int r0 = w.t.r0 + qg / C::NG * kTile, pan0 = first_panel(qg % C::NG, w.half), hk = w.t.hk;
-          const uint32_t to = q_at + qg * C::GP * kPanel;
+        for (int tile = 0; tile < w.nt; ++tile) {
+          const int r0 = w.t.r0 + tile * kTile, hk = w.t.hk;
+          if (C::PAIR == 1) qb = tile; else { wait(&sm.emptyQ[qb], par >> qb & 1); par ^= 1u << qb; }
+          const uint32_t to = q_at + qb * C::NP * kPanel;
           if (g.q_box) {
             if (lane == 0) {
-              const uint32_t bar = smem_u32(sm.fullQ + qg);
-              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::GP * kPanel) : "memory");
-              for (int p = 0; p < C::GP; ++p) tma_box3(to + p * kPanel, &g.q, (pan0 + p) * 64, hk * a.G + r0 % a.G, (int)(w.t.row0 + r0 / a.G), bar);
+              const uint32_t bar = smem_u32(sm.fullQ + qb);
+              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(C::NP * kPanel) : "memory");
+              for (int p = 0; p < C::NP; ++p) tma_box3(to + p * kPanel, &g.q, (rank * C::NP + p) * 64, hk * a.G + r0 % a.G, (int)(w.t.row0 + r0 / a.G), bar);
             }
             __syncwarp();
           } else {
@@ -407,33 +466,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
               const int gr = r0 + x + lane;
               unsigned long long at = 0;
               if (gr - w.t.r0 < w.t.nr) at = reinterpret_cast<unsigned long long>(reinterpret_cast<const bf16*>(a.in.q) + (w.t.row0 + gr / a.G) * a.in.q_ld + ((size_t)hk * a.G + gr % a.G) * a.s.d);
-              rows32(to, kPanel, x, pan0, at);
+              copy_rows(Int<32>{}, to, kPanel, x, at);
             }
-            bar_arrive_copied(sm.fullQ + qg);
+            bar_arrive_copied(sm.fullQ + qb);
           }
+          if (C::PAIR == 2) qb ^= 1;
         }
       });
     } else {
-      const bool is_v = !C::KG || me >= C::TEAM;
-      const int r0 = 32 * (me % C::TEAM);                  // of a block's rows, and every 32 TEAM rows on
+      const bool is_v = !C::KP || me >= C::TEAM;
+      const int r0 = C::RW * (me % C::TEAM);               // of a block's rows, and every RW TEAM rows on
       uint64_t* full = is_v ? sm.fullV : sm.fullK;
       uint64_t* room = is_v ? sm.emptyV : sm.emptyK;
       const uint32_t base_at = is_v ? v_at : k_at;
-      const int nbuf = is_v ? C::NVB : C::NKB * C::KG;
+      const int nbuf = is_v ? C::NVB : C::NKB;
       uint32_t par = 0xffffffffu;                          // a bit per buffer
       int buf = 0;
       walk([&](const Item& w) {
         const int nb = w.nb;
         if (nb == 0) return;
-        const int half = w.half, hk = w.t.hk;
-        constexpr int X = C::BN / (32 * C::TEAM) > 0 ? C::BN / (32 * C::TEAM) : 1;
+        const int hk = w.t.hk;
+        constexpr int X = C::BN / (C::RW * C::TEAM), STEP = C::RW * C::TEAM;
         unsigned long long at[X];
         auto find = [&](int j) {                           // where this lane's rows of block j begin
 #pragma unroll
           for (int x = 0; x < X; ++x) {
-            const int r = r0 + 32 * C::TEAM * x + lane, kk = w.k0 + j * C::BN + r;
+            const int r = r0 + STEP * x + lane, kk = w.k0 + j * C::BN + r;
             at[x] = 0;
-            if (r < C::BN && kk < w.k1) {
+            if (lane < C::RW && kk < w.k1) {
               const int64_t code = list_row(a, w.t, kk);
               if (code != -1) at[x] = reinterpret_cast<unsigned long long>(row_ptr<bf16>(a, hk, code, is_v));
             }
@@ -443,123 +503,158 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 #pragma unroll 1
         for (int j = 0; j < nb; ++j) {
           const int rows16 = (min(C::BN, w.k1 - w.k0 - j * C::BN) + 15) & ~15;
-#pragma unroll 1
-          for (int grp = 0; grp < (is_v ? 1 : C::KG); ++grp) {
-            const uint32_t to = base_at + buf * C::GP * C::PB;
-            const int pan0 = is_v ? half * C::VP : first_panel(grp, half);
-            wait(&room[buf], par >> buf & 1);
+          const uint32_t to = base_at + buf * C::NP * C::PB;
+          wait(&room[buf], par >> buf & 1);
 #pragma unroll
-            for (int x = 0; x < X; ++x)
-              if (r0 + 32 * C::TEAM * x < rows16) rows32(to, C::PB, r0 + 32 * C::TEAM * x, pan0, at[x]);
-            if (w.mode == 2 && is_v) {                     // (what this thread has copied)
-              cp_commit();
-              cp_wait<0>();
-              for (int p = 0; p < C::GP; ++p)
-                for (int x = 0; x < X; ++x)
-                  for (int r = r0 + 32 * C::TEAM * x + sub, e = 0; e < 8 && r0 + 32 * C::TEAM * x < rows16; ++e, r += 4)
-                    make_finite<bf16>(smem_raw + (to + p * C::PB + r * 128 + ((chunk ^ (r & 7)) << 4) - smem_u32(smem_raw)));
-              bar_arrive(&full[buf]);
-            } else {
-              bar_arrive_copied(&full[buf]);
-            }
-            par ^= 1u << buf;
-            buf = buf + 1 == nbuf ? 0 : buf + 1;
+          for (int x = 0; x < X; ++x)
+            if (r0 + STEP * x < rows16) copy_rows(Int<C::RW>{}, to, C::PB, r0 + STEP * x, at[x]);
+          if (w.mode == 2 && is_v) {                       // (what this thread has copied)
+            cp_commit();
+            cp_wait<0>();
+            for (int p = 0; p < C::NP; ++p)
+              for (int x = 0; x < X; ++x)
+                for (int r = r0 + STEP * x + sub, e = 0; e < C::RW / 4 && r0 + STEP * x < rows16; ++e, r += 4)
+                  make_finite<bf16>(smem_raw + (to + p * C::PB + r * 128 + ((chunk ^ (r & 7)) << 4) - smem_u32(smem_raw)));
+            bar_arrive(&full[buf]);
+          } else {
+            bar_arrive_copied(&full[buf]);
           }
+          par ^= 1u << buf;
+          buf = buf + 1 == nbuf ? 0 : buf + 1;
           if (j + 1 < nb) find(j + 1);
         }
       });
     }
     cp_commit();
     cp_wait<0>();
-  } else if (warp == kMmaWarp) {
+  } else if (warp == kMmaWarp || warp == kOutWarp) {
     // ------------------------------------------------------------------ products (issued by one thread of a converged warp)
     const uint32_t idesc_v = make_idesc(C::OC, 1);
-    uint32_t par_q = 0, par_k = 0, par_vs = 0, par_vo = 0, par_p = 0, par_o = 3;     // parities: per tile, buffers (of V for S and for O), S buffer, tile
-    int kb = 0, vs = 0, vo = 0, sx = 0;                    // next K buffer, V buffer (for S, for O), S buffer of one tile
     const bool one = elect_one();
-    walk([&](const Item& w) {
-      const int nb = w.nb, nt = NT == 2 ? w.nt : 1, k_all = w.k1 - w.k0;
-      if (nb == 0) return;
-      // A step: scores of block sb (of tile t), output of the block before.  Two tiles: P V first, whose P lies where the scores will.
-      // One tile: the scores go to the other buffer, and P V as soon as P is there (with the scores first, P V waited for copies
-      // whose buffers it was to free).
-      int sb = 0, ob = -1, t = 0;
+    // S buffer xs = Q (buffer qb) K^T (buffer kb, of K or V), `keys` of them
+    auto scores = [&](int xs, int qb, int kb, int keys) {
+      fence_proxy();
+      fence_after();
+      // (values that the compiler knows to be the warp's: they go through uniform registers, one instruction each for a product)
+      const uint32_t qd = uniform(desc_lo(q_at + qb * C::NP * kPanel, 1)), kd = uniform(desc_lo((C::KP ? k_at : v_at) + kb * C::NP * C::PB, 1));
+      const uint32_t to = uniform(s_col + xs * C::SW), id = uniform(make_idesc((min(C::BN, keys) + 15) & ~15, 0));
+      if (one) {
+#pragma unroll
+        for (int i = 0; i < 4 * C::NP; ++i)
+          mma_ss2(to, qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), kDescHi, kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), kDescHi, id, i != 0);
+      }
+    };
+    // O of tile t (+)= P (S buffer xo) V (buffer vo)
+    auto output = [&](int t, int xo, int vo, int keys, int acc) {
+      fence_proxy();
+      fence_after();
+      const uint32_t vd = uniform(desc_lo(v_at + vo * C::NP * C::PB, C::PB >> 4)), pc = uniform(s_col + xo * C::SW), oc = uniform(o_col + t * C::OC);
+      const uint32_t left = uniform(keys), more = uniform(acc);
+      if (one) {
+#pragma unroll
+        for (int k = 0; k < C::BN / 16; ++k) {
+          if (16 * k >= (int)left) break;
+          mma_ts2(oc, pc + 8 * k, vd + k * (2048 >> 4), kDescHi, idesc_v, k ? 1u : more);
+        }
+      }
+    };
+    if (NT == 2) {
+      // One warp: scores of block sb of tile t after the output of the block before, whose P lies where the scores will (the products of a
+      // thread are carried out in order).
+      uint32_t par_q = 0, par_k = 0, par_vs = 0, par_vo = 0, par_p = 0, par_o = 3;   // parities: buffers (of V for S and for O), tile
+      int kb = 0, vs = 0, vo = 0;                          // next K buffer, V buffer (for S, for O)
+      walk([&](const Item& w) {
+        const int nb = w.nb, nt = w.nt, k_all = w.k1 - w.k0;
 #pragma unroll 1
-      while (ob < nb) {
-        int g = sb < nb ? 0 : C::NG, at_k = kb;
-        bool out = ob < 0;
-        const int xs = NT == 2 ? t : sx, xo = NT == 2 ? t : sx ^ 1;
-        const uint32_t idesc = make_idesc((min(C::BN, k_all - sb * C::BN) + 15) & ~15, 0), dst = s_col + xs * kTile;
-        const bool last = t == nt - 1;
-#pragma unroll 1
-        for (uint32_t spins = 0; g < C::NG || !out; ++spins) {
-          fail = __any_sync(0xffffffffu, fail);
-          if (!out && (NT == 2 || fail || g == C::NG ||
-                       __any_sync(0xffffffffu, bar_ready(&sm.p_ready[xo], par_p >> xo & 1) && (ob || bar_ready(&sm.o_free[0], par_o & 1))))) {
-            // O (+)= P V of block ob
+        for (int sb = 0, t = 0; nb && sb <= nb;) {
+          const int ob = sb - 1;
+          const bool last = t == nt - 1;
+          if (ob >= 0) {
             if (!SHARED) wait(&sm.fullV[vo], par_vo >> vo & 1);
             if (ob == 0) { wait(&sm.o_free[t], par_o >> t & 1); par_o ^= 1u << t; }
-            wait(&sm.p_ready[xo], par_p >> xo & 1);
-            par_p ^= 1u << xo;
-            fence_proxy();
-            fence_after();
-            // (values that the compiler knows to be the warp's: they go through uniform registers, one instruction each for a product)
-            const uint32_t vd = uniform((v_at + vo * C::VP * C::PB) >> 4 | C::PB >> 4 << 16), pc = uniform(s_col + xo * kTile), oc = uniform(o_col + t * C::OC);
-            const uint32_t left = uniform(k_all - ob * C::BN), more = uniform(ob);
+            wait(&sm.p_ready[t], par_p >> t & 1);
+            par_p ^= 1u << t;
+            fail = __any_sync(0xffffffffu, fail);
+            output(t, t, vo, k_all - ob * C::BN, ob);
             if (one) {
-#pragma unroll
-              for (int k = 0; k < C::BN / 16; ++k) {
-                if (16 * k >= (int)left) break;
-                mma_ts2(oc, pc + 8 * k, vd + k * (2048 >> 4), kDescHi, idesc_v, k ? 1u : more);
-              }
               if (last) mma_commit(&sm.emptyV[vo]);
               mma_commit(&sm.pv_done[t]);
-              if (NT == 1 && ob == nb - 1) mma_commit(&sm.o_full);
             }
             __syncwarp();
             if (last) { par_vo ^= 1u << vo; vo = vo + 1 == C::NVB ? 0 : vo + 1; }
-            out = true;
-          } else if (g < C::NG) {
-            const bool k_only = g < C::KG;
-            uint64_t* b = k_only ? &sm.fullK[at_k] : &sm.fullV[vs];
-            const uint32_t parity = (k_only ? par_k >> at_k : par_vs >> vs) & 1;
-            if (out || fail || __any_sync(0xffffffffu, bar_ready(b, parity))) {
-              wait(b, parity);
-              if (sb == 0) wait(&sm.fullQ[t * C::NG + g], par_q >> t & 1);
-              fence_proxy();
-              fence_after();
-              const uint32_t qd = uniform((q_at + (t * C::NG + g) * C::GP * kPanel) >> 4 | 1u << 16);
-              const uint32_t kd = uniform((k_only ? k_at + at_k * C::GP * C::PB : v_at + vs * C::VP * C::PB) >> 4 | 1u << 16);
-              const uint32_t to = uniform(dst), id = uniform(idesc), more = uniform(g);
-              if (one) {
-#pragma unroll
-                for (int i = 0; i < 4 * C::GP; ++i)
-                  mma_ss2(to, qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), kDescHi, kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), kDescHi, id, i ? 1u : more);
-                if (k_only && last) mma_commit(&sm.emptyK[at_k]);
-                if (g == C::NG - 1) {
-                  mma_commit(&sm.s_full[xs]);
-                  if (last && sb == nb - 1) mma_commit(&sm.emptyQ);
-                }
-              }
-              __syncwarp();
-              if (k_only) {
-                if (last) par_k ^= 1u << at_k;
-                at_k = at_k + 1 == C::NKB * C::KG ? 0 : at_k + 1;
-              }
-              ++g;
-              spins = 0;
-            }
           }
-          if (spins > (WAIT_LIMIT << 8)) fail = 1;          // (some 30 cycles each)
+          if (sb < nb) {
+            if (C::KP) wait(&sm.fullK[kb], par_k >> kb & 1); else wait(&sm.fullV[vs], par_vs >> vs & 1);
+            if (sb == 0) { wait(&sm.fullQ[t], par_q >> t & 1); par_q ^= 1u << t; }
+            fail = __any_sync(0xffffffffu, fail);
+            scores(t, t, C::KP ? kb : vs, k_all - sb * C::BN);
+            if (one) {
+              if (C::KP && last) mma_commit(&sm.emptyK[kb]);
+              mma_commit(&sm.s_full[t]);
+              if (last && sb == nb - 1) mma_commit(&sm.emptyQ[0]);
+            }
+            __syncwarp();
+            if (C::KP && last) { par_k ^= 1u << kb; kb = kb + 1 == C::NKB ? 0 : kb + 1; }
+            if (!C::KP && last) { par_vs ^= 1u << vs; vs = vs + 1 == C::NVB ? 0 : vs + 1; }
+          }
+          if (last) { t = 0; ++sb; } else ++t;
         }
-        if (sb < nb) {
-          if (last) { kb = at_k; par_vs ^= 1u << vs; vs = vs + 1 == C::NVB ? 0 : vs + 1; }
-          if (NT == 1) sx ^= 1;
+      });
+    } else if (warp == kMmaWarp) {
+      // Scores, as far ahead as buffers allow, into the next item too
+      constexpr int NB = C::KP ? C::NKB : C::NVB;
+      uint64_t* full = C::KP ? sm.fullK : sm.fullV;
+      uint32_t par_q = 0, par_k = 0, par_s = 0xfu;
+      int kb = 0, x = 0, qb = 0;
+      walk([&](const Item& w) {
+        const int nb = w.nb, k_all = w.k1 - w.k0;
+#pragma unroll 1
+        for (int j = 0; j < nb; ++j) {
+          wait(&full[kb], par_k >> kb & 1);
+          par_k ^= 1u << kb;
+          if (j == 0) { wait(&sm.fullQ[qb], par_q >> qb & 1); par_q ^= 1u << qb; }
+          wait(&sm.s_free[x], par_s >> x & 1);
+          par_s ^= 1u << x;
+          fail = __any_sync(0xffffffffu, fail);
+          scores(x, qb, kb, k_all - j * C::BN);
+          if (one) {
+            if (C::KP) mma_commit(&sm.emptyK[kb]);
+            mma_commit(&sm.s_full[x]);
+            if (j == nb - 1) mma_commit(&sm.emptyQ[qb]);
+          }
+          __syncwarp();
+          kb = kb + 1 == NB ? 0 : kb + 1;
+          x = (x + 1) % C::SB;
         }
-        if (last) { t = 0; ++sb; ++ob; } else ++t;
-      }
-      par_q ^= nt == 2 ? 3u : 1u;                          // (an item of one tile does not use the other's)
-    });
+        if (nb) qb = (qb + 1) % C::QB;
+      });
+    } else {
+      // Outputs
+      uint32_t par_v = 0, par_p = 0, par_o = 1;
+      int vb = 0, x = 0;
+      walk([&](const Item& w) {
+        const int nb = w.nb, k_all = w.k1 - w.k0;
+#pragma unroll 1
+        for (int j = 0; j < nb; ++j) {
+          wait(&sm.fullV[vb], par_v >> vb & 1);
+          par_v ^= 1u << vb;
+          if (j == 0) { wait(&sm.o_free[0], par_o); par_o ^= 1u; }
+          wait(&sm.p_ready[x], par_p >> x & 1);
+          par_p ^= 1u << x;
+          fail = __any_sync(0xffffffffu, fail);
+          output(0, x, vb, k_all - j * C::BN, j);
+          if (one) {
+            mma_commit(&sm.emptyV[vb]);
+            mma_commit(&sm.s_free[x]);
+            mma_commit(&sm.pv_done[0]);
+            if (j == nb - 1) mma_commit(&sm.o_full);
+          }
+          __syncwarp();
+          vb = vb + 1 == C::NVB ? 0 : vb + 1;
+          x = (x + 1) % C::SB;
+        }
+      });
+    }
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
     const int grp = warp >> 2, q4 = warp & 3;              // (a warp reaches the 32 lanes of tensor memory of its number modulo 4)
@@ -583,22 +678,35 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       if (w.t.ok == 2) {                                   // (with the keys split: the join's)
         uint4* o = reinterpret_cast<uint4*>(out_at(w.t, r));
         if (a.nsplit == 1)
-          for (int c = w.half * (C::OC / 8); c < min(a.s.d / 8, (w.half + 1) * (C::OC / 8)); ++c) o[c] = make_uint4(0, 0, 0, 0);
-      } else if (w.half == 0) {
+          for (int c = col0 / 8; c < min(a.s.d, col0 + C::OC) / 8; ++c) o[c] = make_uint4(0, 0, 0, 0);
+      } else if (col0 == 0) {
         a.pml[part_at(w, r)] = make_float2(-INFINITY, 0.f);
       }
     };
     // O out of tensor memory; its rows' reference and sum are ref and sum.  bad: of mode 1, for mode 2.
     bool bad = false;
+    uint32_t turn = 0;
+    // A row that is bad in one CTA of a pair is so in both: its columns are to come from the same scores.
+    auto bad_in_pair = [&](bool odd) {
+      const uint32_t mine = __ballot_sync(FULL, odd), k = turn & 1;
+      if (lane == 0) {
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other_cta(&sm.bad[k][q4], rank ^ 1)), "r"(mine) : "memory");
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(other_cta(&sm.bad_full[k][q4], rank ^ 1)) : "memory");
+      }
+      if (!fail && !bar_wait_pair(&sm.bad_full[k][q4], turn >> 1 & 1)) fail = 1;
+      ++turn;
+      return ((mine | *(volatile uint32_t*)&sm.bad[k][q4]) >> lane & 1u) != 0;
+    };
     auto epilogue = [&](const Item& w, float ref, float sum) {
       const TileList& t = w.t;
       const int mode = w.mode, rt = tile * kTile, r0 = rt + q4 * 32;
-      const bool live = rt + row < t.nr, lead = w.half == 0;
+      // (mode 2 writes the marked rows only: the others' results of the first round are right)
+      const bool live = rt + row < t.nr, put = live && (mode == 0 || (mode == 2 && bad));
       const uint32_t ocol = o_col + tile * C::OC + lane_at;
       bool odd = !is_finite(sum) || (ref == -INFINITY && a.nsplit == 1);
       if (a.nsplit > 1) {
         const size_t part = part_at(w, rt + row);
-        float* po = a.po + part * a.s.d + w.half * C::OC;
+        float* po = a.po + part * a.s.d + col0;
         float nz = 0.f;                                    // 0 x each value: NaN where one is not finite
 #pragma unroll 1
         for (int c = 0; c < C::OC; c += 32) {
@@ -608,17 +716,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           for (int e = 0; e < 32; e += 4) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) nz = fmaf(__uint_as_float(r[e + i]), 0.f, nz);
-            if (live && mode != 1 && w.half * C::OC + c + e < a.s.d) *reinterpret_cast<uint4*>(po + c + e) = make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]);
+            if (put && col0 + c + e < a.s.d) *reinterpret_cast<uint4*>(po + c + e) = make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]);
           }
         }
         odd |= !(nz == 0.f);
-        if (live && lead && mode != 1) a.pml[part] = make_float2(ref, sum);
+        if (put && col0 == 0) a.pml[part] = make_float2(ref, sum);
       } else {
         // a row per lane, 32 bytes of it at a time: whole sectors, no exchanges between lanes
         const float inv = 1.f / sum;
         const uint64_t inv2 = pair2(inv, inv);
-        bf16* o = out_at(t, min(rt + row, t.nr - 1)) + w.half * C::OC;
-        const bool put = live && mode != 1, wide = (((uintptr_t)a.out | (uintptr_t)(a.s.d * 2)) & 31) == 0;
+        bf16* o = out_at(t, min(rt + row, t.nr - 1)) + col0;
+        const bool wide = (((uintptr_t)a.out | (uintptr_t)(a.s.d * 2)) & 31) == 0;
         const __nv_bfloat162 zero2 = __floats2bfloat162_rn(0.f, 0.f);
         __nv_bfloat162 nz[2] = {zero2, zero2};             // 0 x each value: NaN where one is not finite
 #pragma unroll 1
@@ -632,7 +740,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             nz[(e >> 1) & 1] = __hfma2(v, zero2, nz[(e >> 1) & 1]);
             r[e >> 1] = *reinterpret_cast<const uint32_t*>(&v);
           }
-          const int left = a.s.d - w.half * C::OC - c;     // columns that there are
+          const int left = a.s.d - col0 - c;     // columns that there are
           if (put && wide) {
             if (left >= 16) store32(o + c, r);
             if (left >= 32) store32(o + c + 16, r + 8);
@@ -649,14 +757,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       bar_arrive(&sm.o_free[tile]);
       odd = odd && live;
       if (mode == 0 && odd) atomicOr(&sm.redo[(w.li >> 5) & 31], 1u << (w.li & 31));
-      if (mode == 1) bad = odd;
+      if (mode == 1) bad = C::PAIR == 2 ? bad_in_pair(odd) : odd;
       if (mode == 2) {
         uint32_t an;
         const int p = position(w, rt + row, an);
         for (uint32_t todo = __ballot_sync(FULL, bad); todo; todo &= todo - 1) {
           const int x = __ffs(todo) - 1;
-          exact_output(a, t, w.depth, t.r0 + r0 + x, __shfl_sync(FULL, p, x), __shfl_sync(FULL, an, x), w.k0, w.k1, w.half * C::OC,
-                       min(a.s.d, (w.half + 1) * C::OC), part_at(w, r0 + x));
+          exact_output(a, t, w.depth, t.r0 + r0 + x, __shfl_sync(FULL, p, x), __shfl_sync(FULL, an, x), w.k0, w.k1, col0,
+                       min(a.s.d, col0 + C::OC), part_at(w, r0 + x));
         }
       }
     };
@@ -678,6 +786,53 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       uint32_t cS = 0, par_s = 0, cW = 0, n = 0;           // blocks so far, parity of s_full; blocks whose P V is known to be complete; items
       // (one by one, each before the P of the block after the next is announced: a parity says no more than the last phase)
       auto wait_pv = [&](uint32_t blocks) { for (; cW != blocks; ++cW) wait(&sm.pv_done[tile], cW & 1); fence_after(); };
+      // A pair: this row's part of the scores goes to the other CTA, and that one's part is added (the sum is the same bits in both).
+      uint32_t sv[C::SL], par_x = 0;
+      const uint32_t x_mine = x_at + row * 16, x_to = C::PAIR == 2 ? other_cta(smem_raw + (x_mine - smem_u32(smem_raw)), rank ^ 1) : 0;
+      const uint32_t x_full_to = C::PAIR == 2 ? other_cta(&sm.x_full[q4], rank ^ 1) : 0, x_free_to = C::PAIR == 2 ? other_cta(&sm.x_free[q4], rank ^ 1) : 0;
+      auto load = [&](uint32_t col) {                      // (to be followed by a wait and `loaded`)
+        tmem_ld32_nowait(col, sv);
+        if (C::SL == 64) tmem_ld32_nowait(col + 32, sv + 32); else tmem_ld16_nowait(col + 32, sv + 32);
+      };
+      auto loaded = [&]() {
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        tmem_regs_ready(sv);
+        if (C::SL == 64) tmem_regs_ready(sv + 32); else tmem_regs_ready16(sv + 32);
+      };
+      auto send = [&](int x) {                             // the scores of buffer x, which stay in sv
+        wait(&sm.s_full[x], par_s >> x & 1);
+        par_s ^= 1u << x;
+        fence_after();
+        load(s_col + x * C::SW + lane_at);
+        wait(&sm.x_free[q4], par_x ^ 1);
+        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(&sm.x_full[q4])), "r"(32 * C::SL * 4) : "memory");
+        loaded();
+#pragma unroll
+        for (int e = 0; e < C::SL; e += 4)
+          asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                       ::"r"(x_to + e * (kTile * 4)), "r"(sv[e]), "r"(sv[e + 1]), "r"(sv[e + 2]), "r"(sv[e + 3]), "r"(x_full_to) : "memory");
+      };
+      auto receive = [&]() {
+        wait(&sm.x_full[q4], par_x);
+#pragma unroll
+        for (int h = 0; h < C::SL; h += 24) {
+          float v[24];
+#pragma unroll
+          for (int e = 0; e < 24; e += 4)
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[e]), "=f"(v[e + 1]), "=f"(v[e + 2]), "=f"(v[e + 3]) : "r"(x_mine + (h + e) * (kTile * 4)) : "memory");
+#pragma unroll
+          for (int e = 0; e < 24; e += 2) {
+            const float2 y = unpair(add2(pair2(__uint_as_float(sv[(h + e) % C::SL]), __uint_as_float(sv[(h + e + 1) % C::SL])), pair2(v[e], v[e + 1])));
+            sv[(h + e) % C::SL] = __float_as_uint(y.x); sv[(h + e + 1) % C::SL] = __float_as_uint(y.y);
+          }
+        }
+        par_x ^= 1;
+      };
+      // What was received has been used by the whole warp: the other CTA may send again (nothing else is to be ordered before this; with
+      // a release, which waits for all of the thread's memory accesses, it took 1 to 2 thousand cycles).
+      auto taken = [&]() {
+        if (lane == 0) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(x_free_to) : "memory");
+      };
       walk([&](const Item& w) {
         const TileList& t = w.t;
         if (w.nb == 0) { if (NT == 2) no_keys(w); return; }
@@ -698,55 +853,57 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         float ref = -INFINITY;
         uint64_t l2[4] = {0, 0, 0, 0};                     // (four sums of two)
         const uint64_t scale2 = pair2(a.scale2, a.scale2);
+        if (C::PAIR == 2) send(cS % C::SB);
 #pragma unroll 1
         for (int j = 0; j < nb; ++j) {
-          const int x = NT == 2 ? tile : (int)(cS & 1), c0 = k0 + j * C::BN, slabs = (min(C::BN, k1 - c0) + 63) / 64;
-          const uint32_t scol = s_col + x * kTile + lane_at;
-          wait(&sm.s_full[x], par_s >> x & 1);
-          par_s ^= 1u << x;
-          fence_after();
+          const int x = NT == 2 ? tile : (int)(cS % C::SB), c0 = k0 + j * C::BN, slabs = (min(C::BN, k1 - c0) + C::SL - 1) / C::SL;
+          const uint32_t scol = s_col + x * C::SW + lane_at;
+          if (C::PAIR == 1) {
+            wait(&sm.s_full[x], par_s >> x & 1);
+            par_s ^= 1u << x;
+            fence_after();
+          }
 #pragma unroll 1
           for (int i = 0; i < slabs; ++i) {
-            const int c = c0 + 64 * i;
-            uint32_t sv[64];
-            tmem_ld32_nowait(scol + 64 * i, sv);
-            tmem_ld32_nowait(scol + 64 * i + 32, sv + 32);
+            const int c = c0 + C::SL * i;
+            if (C::PAIR == 1) load(scol + C::SL * i);
             uint32_t vis[2];
             bool whole[2];
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-              const int cv = c + 32 * v, x = nc - cv;
-              whole[v] = !missing && cv >= all0 && cv + 32 <= all1;
-              vis[v] = FULL;
+              const int wide = v ? C::SL - 32 : 32, cv = c + 32 * v, x = nc - cv;
+              const uint32_t every = FULL >> (32 - wide);
+              whole[v] = !missing && cv >= all0 && cv + wide <= all1;
+              vis[v] = every;
               if (!whole[v]) {
                 vis[v] = bits(kmin - cv, min(kmax + 1, nc) - cv) | bits(-cv, min(ksink, nc) - cv);
                 if (tree && x < 32 && x > -32) vis[v] |= x >= 0 ? nodes << x : nodes >> -x;
-                vis[v] &= bits(0, k1 - cv);
+                vis[v] &= bits(0, min(wide, k1 - cv));
                 if (missing) vis[v] = have_pages(a, t, cv, vis[v]);
-                whole[v] = __all_sync(FULL, vis[v] == FULL);
+                whole[v] = __all_sync(FULL, vis[v] == every);
               }
             }
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            tmem_regs_ready(sv);
-            tmem_regs_ready(sv + 32);
+            if (C::PAIR == 1) loaded(); else receive();
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
               if (whole[v]) continue;
 #pragma unroll
-              for (int e = 0; e < 32; ++e) if (!(vis[v] >> e & 1u)) sv[32 * v + e] = 0xff800000u;
+              for (int e = 0; e < (v ? C::SL - 32 : 32); ++e) if (!(vis[v] >> e & 1u)) sv[32 * v + e] = 0xff800000u;
             }
             float m8[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) m8[e] = fmaxf(fmaxf(__uint_as_float(sv[e]), __uint_as_float(sv[e + 8])), __uint_as_float(sv[e + 16]));
 #pragma unroll
-            for (int e = 24; e < 56; e += 16)
+            for (int e = 24; e < C::SL - 8; e += 16)
 #pragma unroll
               for (int x = 0; x < 8; ++x) m8[x] = fmaxf(fmaxf(m8[x], __uint_as_float(sv[e + x])), __uint_as_float(sv[e + 8 + x]));
 #pragma unroll
-            for (int x = 0; x < 8; ++x) m8[x] = fmaxf(m8[x], __uint_as_float(sv[56 + x]));
+            for (int x = 0; x < 8; ++x) m8[x] = fmaxf(m8[x], __uint_as_float(sv[C::SL - 8 + x]));
             const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])), fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * a.scale2;
             const bool up = mx > ref + kGap || (ref == -INFINITY && mx > ref);
-            if (__any_sync(FULL, up)) {                    // (alike in the warp: accesses to tensor memory are the whole warp's)
+            const bool any_up = __any_sync(FULL, up);
+            if (C::PAIR == 2) taken();
+            if (any_up) {                                  // (alike in the warp: accesses to tensor memory are the whole warp's)
               const float to = up ? ceilf(mx) : ref, f = up && ref != -INFINITY ? power_of_two(ref - to) : 1.f;
               ref = to;
               if (__any_sync(FULL, f != 1.f)) {
@@ -754,27 +911,28 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 #pragma unroll
                 for (int x = 0; x < 4; ++x) l2[x] = fma2(l2[x], f2, 0);
                 if (j) wait_pv(cS);
-                rescale(scol, 2 * i, o_col + tile * C::OC + lane_at, j ? C::OC : 0, f);
+                rescale(scol, C::SL / 2 * i, o_col + tile * C::OC + lane_at, j ? C::OC : 0, f);
               }
             }
             const float neg = ref == -INFINITY ? 0.f : -ref;
             const uint64_t neg2 = pair2(neg, neg);
 #pragma unroll
-            for (int e = 0; e < 64; e += 2) {
+            for (int e = 0; e < C::SL; e += 2) {
               const float2 y = unpair(fma2(pair2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), scale2, neg2));
               const float p0 = ex2(y.x), p1 = ex2(y.y);
               l2[(e >> 1) & 3] = add2(l2[(e >> 1) & 3], pair2(p0, p1));
               const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
               sv[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            tmem_st16(scol + 32 * i, sv);
-            tmem_st16(scol + 32 * i + 16, sv + 16);
+            tmem_st16(scol + C::SL / 2 * i, sv);
+            tmem_st16(scol + C::SL / 2 * i + 16, sv + 16);     // (48: its last eight words lie behind P)
           }
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           fence_before();
           wait_pv(cS);
           bar_arrive(&sm.p_ready[x]);
           ++cS;
+          if (C::PAIR == 2 && j + 1 < nb) send(cS % C::SB);
         }
         const float2 la = unpair(add2(l2[0], l2[1])), lb = unpair(add2(l2[2], l2[3]));
         const float sum = (la.x + la.y) + (lb.x + lb.y);
@@ -792,7 +950,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   }
   if (__any_sync(0xffffffffu, fail)) for (int b = lane; b < a.s.B; b += 32) atomicOr(a.status + b, TSV_ST_INTERNAL);   // (an internal error: every sequence is flagged)
   fence_before();
-  __syncthreads();
+  all_sync();                                                   // (a pair: nobody reaches for the other's memory any more)
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
 }
 
@@ -819,13 +977,24 @@ int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
   g.a = a;
   // (heads that do not fill a box of 128 rows evenly, or rows beyond a tensor map's: by the copying warps' own loads)
   g.q_box = (128 % a.G == 0 || a.G % 128 == 0) && a.bt.rows < (int64_t)1 << 31 && a.in.q_ld < (int64_t)1 << 38 && query_map(&g.q, a);
-  const int64_t items = units * a.s.Hk * a.nsplit * C::HALVES;
+  const int64_t items = units * a.s.Hk * a.nsplit;
   if (items > 0x7fffffff - 148) return TSV_ERR_LIMIT;
   g.items = (int32_t)items;
   if (!ensure_smem((const void*)attn_tc_kernel<DP, SHARED>, C::SMEM)) return TSV_ERR_CUDA;
   TSV_PREP((attn_tc_kernel<DP, SHARED>));
-  const int grid = g.items < 148 ? g.items : 148;
-  attn_tc_kernel<DP, SHARED><<<(unsigned)grid, kTcThreads, C::SMEM, st>>>(g);
+  const int most = 148 / C::PAIR, grid = g.items < most ? g.items : most;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(grid * C::PAIR));
+  cfg.blockDim = dim3(32 * C::WARPS);
+  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = C::PAIR;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = C::PAIR == 2;
+  if (cudaLaunchKernelEx(&cfg, attn_tc_kernel<DP, SHARED>, g) != cudaSuccess) return TSV_ERR_CUDA;
   count_launch();
   return TSV_OK;
 }
