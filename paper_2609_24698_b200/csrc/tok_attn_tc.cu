@@ -80,8 +80,8 @@ struct TcCtl {
   uint64_t fullQ[2], emptyQ[2];               // by buffer
   uint64_t fullK[4], emptyK[4];
   uint64_t fullV[4], emptyV[4];
-  uint64_t s_full[4], p_ready[4], s_free[4], pv_done[2], o_free[2];      // (s_free: of one tile)
-  uint64_t o_full, stat_full, stat_free;      // one tile: O is complete; reference and sum of its rows, for the epilogue
+  uint64_t s_full[4], p_ready[4], s_free[4], o_full[2], o_free[2];       // (s_free: of one tile)
+  uint64_t stat_full, stat_free;              // one tile: reference and sum of its rows, for the epilogue
   uint64_t x_full[4], x_free[4];              // a warp's rows of the other CTA's part of S: there; taken there, of this one's
   uint64_t bad_full[2][4];                    // the other CTA's word of `bad`, by turns
   uint32_t bad[2][4];                         // rows with a result that is not finite there, a bit each
@@ -104,7 +104,9 @@ __device__ __forceinline__ TcCtl& control() {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   return *reinterpret_cast<TcCtl*>(smem_raw);
 }
-// One bounded try in line, the others (to the limit) in a function: a wait is in the code of some thirty places.
+// A first look in line, then tries to the limit in a function: a wait is in the code of some thirty places.  A test is back sooner than a try
+// that may suspend, a try leaves the other warps more; pairs of CTAs, whose softmax hardly ever finds a phase incomplete, take the test
+// (prompts of 64 heads x 512: 672 against 691 us; 32 heads x 128 the other way about, 606 and 582).
 __device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
   const uint32_t limit = control().limit;
 #pragma unroll 1
@@ -116,11 +118,15 @@ __device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
   }
   return false;
 }
+template <bool TEST>
 __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
   const uint32_t addr = smem_u32(bar);
   uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
+  if (TEST)
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(addr), "r"(parity) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
   return ok || bar_wait_on(addr, parity);
 }
 // The same for what the other CTA of a pair sends.
@@ -143,12 +149,6 @@ __device__ __forceinline__ uint32_t other_cta(const void* p, uint32_t rank) {
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Whether the phase is complete.
-__device__ __forceinline__ bool bar_ready(uint64_t* b, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
-  return ok != 0;
 }
 // An arrival of this thread when its copies so far have landed.
 __device__ __forceinline__ void bar_arrive_copied(uint64_t* b) {
@@ -315,8 +315,8 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
   if (tid == 0) {
     for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], C::WARPS - 1); }
     for (int i = 0; i < 4; ++i) { bar_init(&sm.fullV[i], 32 * C::TEAM); bar_init(&sm.fullK[i], 32 * C::TEAM); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.s_free[i], 1); bar_init(&sm.x_full[i], 1); bar_init(&sm.x_free[i], 1); bar_init(&sm.bad_full[0][i], 1); bar_init(&sm.bad_full[1][i], 1); }
-    for (int i = 0; i < 2; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.emptyQ[i], 1); bar_init(&sm.pv_done[i], 1); bar_init(&sm.o_free[i], kTile); }
-    bar_init(&sm.o_full, 1); bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
+    for (int i = 0; i < 2; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.emptyQ[i], 1); bar_init(&sm.o_full[i], 1); bar_init(&sm.o_free[i], kTile); }
+    bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid == 0) sm.limit = WAIT_LIMIT;
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
   fence_after();
   const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + 2 * kTile;
 
-  auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait(b, parity)) fail = 1; };
+  auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait<C::PAIR == 2>(b, parity)) fail = 1; };
   // After the first round: whether there is a second (alike in all threads of a CTA or a pair).  It computes rows one by one, and its waits
   // have 256 times the limit.
   auto marks = [&](int i) {
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
             output(t, t, vo, k_all - ob * C::BN, ob);
             if (one) {
               if (last) mma_commit(&sm.emptyV[vo]);
-              mma_commit(&sm.pv_done[t]);
+              if (ob == nb - 1) mma_commit(&sm.o_full[t]);
             }
             __syncwarp();
             if (last) { par_vo ^= 1u << vo; vo = vo + 1 == C::NVB ? 0 : vo + 1; }
@@ -646,8 +646,7 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
           if (one) {
             mma_commit(&sm.emptyV[vb]);
             mma_commit(&sm.s_free[x]);
-            mma_commit(&sm.pv_done[0]);
-            if (j == nb - 1) mma_commit(&sm.o_full);
+            if (j == nb - 1) mma_commit(&sm.o_full[0]);
           }
           __syncwarp();
           vb = vb + 1 == C::NVB ? 0 : vb + 1;
@@ -776,16 +775,19 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
         wait(&sm.stat_full, n & 1);
         const float2 st = sm.stat[row];
         bar_arrive(&sm.stat_free);
-        wait(&sm.o_full, n & 1);
+        wait(&sm.o_full[0], n & 1);
         ++n;
         fence_after();
         epilogue(w, st.x, st.y);
       });
     } else {
       // ---------------------------------------------------------------- softmax
-      uint32_t cS = 0, par_s = 0, cW = 0, n = 0;           // blocks so far, parity of s_full; blocks whose P V is known to be complete; items
-      // (one by one, each before the P of the block after the next is announced: a parity says no more than the last phase)
-      auto wait_pv = [&](uint32_t blocks) { for (; cW != blocks; ++cW) wait(&sm.pv_done[tile], cW & 1); fence_after(); };
+      uint32_t cS = 0, par_s = 0, n = 0;                   // blocks so far, parities of s_full; items
+      // O holds the blocks before this one.  Of two tiles: there are this block's scores, products of the same thread.
+      auto wait_o = [&]() {
+        if (NT == 1) wait(&sm.s_free[(cS - 1) % C::SB], (cS - 1) / C::SB & 1);
+        fence_after();
+      };
       // A pair: this row's part of the scores goes to the other CTA, and that one's part is added (the sum is the same bits in both).
       uint32_t sv[C::SL], par_x = 0;
       const uint32_t x_mine = x_at + row * 16, x_to = C::PAIR == 2 ? other_cta(smem_raw + (x_mine - smem_u32(smem_raw)), rank ^ 1) : 0;
@@ -910,7 +912,7 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
                 const uint64_t f2 = pair2(f, f);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) l2[x] = fma2(l2[x], f2, 0);
-                if (j) wait_pv(cS);
+                if (j) wait_o();
                 rescale(scol, C::SL / 2 * i, o_col + tile * C::OC + lane_at, j ? C::OC : 0, f);
               }
             }
@@ -929,7 +931,6 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
           }
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           fence_before();
-          wait_pv(cS);
           bar_arrive(&sm.p_ready[x]);
           ++cS;
           if (C::PAIR == 2 && j + 1 < nb) send(cS % C::SB);
@@ -942,7 +943,9 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
           bar_arrive(&sm.stat_full);
           ++n;
         } else {
-          wait_pv(cS);
+          wait(&sm.o_full[tile], n & 1);
+          ++n;
+          fence_after();
           epilogue(w, ref, sum);
         }
       });
