@@ -53,11 +53,11 @@ struct Cfg {
   static constexpr int NP = OC / 64;                         // panels of them: copied, announced and multiplied together
   static constexpr int KP = SHARED ? 0 : NP;                 // panels of K where V has its own
   static constexpr int QB = PAIR == 2 ? 2 : NT;              // tiles of Q in shared memory
-  static constexpr int BN = PAIR == 2 ? 48 : 128;            // keys of a block
+  static constexpr int BN = PAIR == 2 ? 48 : DP == 256 && !SHARED ? 64 : 128;            // keys of a block
   static constexpr int SL = BN < 64 ? BN : 64;               // columns of a slab of S
   static constexpr int PB = BN * 128;                        // bytes of a panel of keys
-  static constexpr int NKB = KP == 0 ? 0 : DP == 64 ? 4 : DP == 128 ? 2 : 1;          // buffers of a block's K
-  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : DP == 256 ? (SHARED ? 2 : 1) : SHARED ? 3 : 2;   // of its V
+  static constexpr int NKB = KP == 0 ? 0 : DP == 64 ? 4 : DP == 512 ? 1 : 2;           // buffers of a block's K
+  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : DP == 256 ? 2 : SHARED ? 3 : 2;   // of its V
   static constexpr int SB = PAIR == 2 ? 4 : 2, SW = 2 * kTile / SB;  // buffers of S, their columns
   static constexpr int WARPS = NT == 1 ? 16 : 15;
   static constexpr int TEAM = KP ? 2 : 4;                    // warps that copy a block of K or V
