@@ -657,8 +657,10 @@ struct AttnPlan {
   size_t off_pml;
 };
 
-// bf16 tiles of 128 rows where a sequence may have enough rows for a key head to fill a good part of one.
-bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s.max_n * (s.H / s.Hk) >= 48; }
+// bf16 in tiles of 128 rows where a sequence may have more rows for a key head than one tile of 16.  us, tiles of 128 / of 16 rows, 32 heads
+// on 8 of 128: 64 sequences, window 1024: 16 rows 95 / 112, 32 rows 97 / 209, 64 rows 98 / 362; 4 sequences, window 128: 17 / 14, 17 / 15,
+// 17 / 18; window 2048: 32 / 29, 32 / 38, 36 / 59.
+bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s.max_n * (s.H / s.Hk) > kRows; }
 
 // Tiles and CTAs that splitting the keys aims at: those that run at a time.
 int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? 148 / tc_halves(s.d) : s.d <= 128 ? 2 * 148 : 148; }

@@ -3,27 +3,38 @@
 // A persistent CTA per SM walks over work items (one or two tiles, key head, columns, share of the keys), warps by role:
 //   warps 0-3    softmax of the first tile, a row per thread
 //   warps 4-7    softmax of the second tile; where there is one tile, its epilogue, under the next item's scores and softmax
-//   warp 8       issues the products: S = Q K^T, then O += P V with P as the A operand straight from tensor memory
+//   warp 8       issues the products: S = Q K^T; with two tiles also O += P V, P as the A operand straight from tensor memory
 //   warp 9       finds the items ahead of the others: tile, keys, tree
-//   warps 10-13  copy groups of panels of K and V into shared memory, 32 rows each: two for what only S reads, two for the output columns, or
-//                all four for these where K is V (a wait for a barrier's phase is only good for a thread that sees all of them).  Rows come by 16-byte asynchronous copies: from pages, a ring or the call's own tensors, any of
-//                them with strides of their own, which no tensor map describes; a barrier counts a group's copies as they land, and the
-//                thread that issues the products orders them before its reads (fence.proxy.async)
+//   warps 10-13  copy blocks of K and V into shared memory: two warps K, two V, or all four where K is V (a wait for a barrier's phase is
+//                only good for a thread that sees all of them).  Rows come by 16-byte asynchronous copies: from pages, a ring or the call's
+//                own tensors, any of them with strides of their own, which no tensor map describes; a barrier counts a block's copies as
+//                they land, and the thread that issues the products orders them before its reads (fence.proxy.async)
 //   warp 14      Q, by TMA where the heads of a key head fill a box evenly, else like K and V
-// K and V live in panels of 128 rows (64 at d = 512) x 64 columns (128-byte swizzle): K row-major is the K-major operand of S, and the same
-// layout read MN-major the operand of P V, so that where the keys are the values one copy serves both products.  Two tiles share a
-// block of K and V: copies (half of the shared-memory traffic of a tile) and their instructions per product halve, and one tile's
-// softmax runs under the other's products.
+//   warp 15      where there is one tile, issues O += P V: the scores run ahead of it, into the next item too
 //
-// Tensor memory: two buffers of S (128 columns; of the two tiles, or of two blocks of the one) and O.  P (bf16) overlays the S it came
-// from.  d = 512 has no room for S beside all of O (512 columns): two CTAs take 256 output columns each and compute S and the softmax
-// alike.  There, where Q takes 128 KiB, blocks of 64 keys leave room for two of them: with one of 128 keys the next block's copies waited
-// for this one's P V, and lists of a few more than 128 keys paid for a second block 6.6 of 20 thousand cycles.
+// K and V live in panels of a block's rows x 64 columns (128-byte swizzle): K row-major is the K-major operand of S, and the same layout
+// read MN-major the operand of P V, so that where the keys are the values one copy serves both products.  Two tiles share a block of K
+// and V: copies (half of the shared-memory traffic of a tile) and their instructions per product halve, and one tile's softmax runs
+// under the other's products.
 //
-// Softmax: S is read once, in slabs of 64 keys.  The row's reference is its first maximum, rounded up to a whole power of two; it moves
-// where a later slab exceeds it by more than 2^10 (bf16 and fp32 have the range for weights above one), and then what is there of
-// P, the sum and O are multiplied by a power of two, exactly.  Nearly never after the first slab.
+// Tensor memory: buffers of S (two of 128 columns, of the two tiles or of two blocks of the one; four of 64 at d = 512) and O.  P (bf16)
+// overlays the S it came from.
+//
+// d = 512: Q of a tile (128 KiB) leaves no room for blocks of keys ahead, and tensor memory none for S beside all of O (512 columns).  So
+// an item belongs to the two CTAs of a cluster, each with half of the columns of Q, K, V and O: it multiplies its halves of Q and K, sends
+// its part of S to the other through distributed shared memory, adds what comes from there, and both do the same softmax.  Nothing is
+// read or multiplied twice, Q fits twice (the next tile's comes under this one's work) and so do three blocks of 48 keys.  Prompts of 64
+// heads x 512: 644 us; with all of Q and K in both CTAs, which was the form before, 755 with blocks of 48 keys and 828 of 64.
+//
+// Softmax: S is read once, in slabs of 64 keys (48 at d = 512).  The row's reference is its first maximum, rounded up to a whole power of
+// two; it moves where a later slab exceeds it by more than 2^10 (bf16 and fp32 have the range for weights above one), and then what is
+// there of P, the sum and O are multiplied by a power of two, exactly.  Nearly never after the first slab.
 // P is rounded to bf16 for the product (2^-9 of a weight); scores, sums and O are fp32.
+//
+// What bounds it (prompts of 32 heads on 8 x 128, window 1024, 17 k tokens: 547 us, 35 % of the tensor pipe's cycles, 37 % of the special
+// function units'): the products take 2.7 k cycles of a block of 128 keys (K = 16 of P V from tensor memory costs 103 cycles for 128
+// columns, of S from shared memory 64), a tile's softmax 1.3 k for 64 keys, mostly latencies of dependent instructions of the one warp
+// that a scheduler has for it.  At d = 512 a block's softmax and exchange (2.5 k cycles for 48 keys, of which 0.5 wait for the other CTA).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -206,7 +217,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -245,8 +255,7 @@ __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, i
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
-// What is rare stays out of the loops' code: at some 150 KB of it, the warp that issues the products took a thousand cycles for the forty
-// instructions of a panel.
+// What is rare stays out of the loops' code.
 
 // Of keys c0 .. (bits of m) those that have a page.
 __device__ __noinline__ uint32_t have_pages(const AttnArgs& a, const TileList& t, int c0, uint32_t m) {

@@ -213,6 +213,43 @@ def test_what_is_not_seen_has_no_influence(api, heads, n):
         assert np.abs(got[r0:r0 + n] - ref)[ok].max() < 0.1
 
 
+@pytest.mark.parametrize("heads", [("bf16", 64, 1, 512, True), ("bf16", 8, 1, 512, False), ("bf16", 32, 1, 128, True)], ids=lambda h: "_".join(map(str, h)))
+def test_infinite_scores_in_split_keys(api, heads):
+    """A key with an infinite value: some rows' score of it is -infinity (no weight), others' is +infinity, and all shares of a row's keys agree."""
+    _, tk, _ = api
+    for bad in (float("inf"), -float("inf")):
+        lay = Layer(tk, *heads, window=3000, sinks=1, L=[3100], n=[8], seed=5)
+        lay.k[lay.row0[0] + 2, -1, 1] = bad
+        got = f64(lay.run(tk))[lay.row0[0]:lay.row0[0] + 8]
+        ref, mag, _ = lay.ref(0)
+        ok = np.isfinite(ref)
+        assert (ok == np.isfinite(got)).all()
+        assert not ok[2:].all() and ok[2:].any()
+        # (a rounding of each weight, of the result, and of fp32 sums of 3 k terms)
+        assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -8 * mag + 1e-3 * mag)[ok].all()
+        assert not lay.status.any()
+
+
+# rows computed one by one, some tenths of a second of them in front of a CTA's next tile
+@pytest.mark.parametrize("heads,L,n", [(("bf16", 16, 1, 64, False), 0, 4900), (("bf16", 64, 1, 512, True), 7000, 310)], ids=str)
+def test_nan_that_all_rows_of_a_long_window_see(api, heads, L, n):
+    _, tk, _ = api
+    lay = Layer(tk, *heads, window=20000, sinks=0, L=[L], n=[n], seed=1)
+    clean = lay.run(tk).clone()
+    (lay.k if lay.v is None else lay.v)[lay.row0[0], 0, 3] = float("nan")
+    out = lay.run(tk)
+    r = slice(lay.row0[0], lay.row0[0] + n)
+    assert not lay.status.any()
+    got, was = out[r].float(), clean[r].float()
+    assert got[..., 3].isnan().all()
+    if lay.v is None:
+        assert got.isnan().all()                          # (every score of that key)
+    else:
+        got[..., 3] = was[..., 3]
+        # two results, each within a rounding of the weights and of itself (values of up to 6)
+        assert ((got - was).abs() <= 2 * (2.0 ** -8 * 6 + 2.0 ** -8 * was.abs())).all()
+
+
 def test_large_scores(api):
     """Scores far apart: one key decides, and the reference of the softmax moves from block to block."""
     _, tk, _ = api
