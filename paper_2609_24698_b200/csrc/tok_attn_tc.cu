@@ -48,7 +48,7 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 128;            // query rows of a tile; columns of an S buffer
-constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 5, kOutWarp = 15;
+constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 5, kOutWarp = 15, kWarps = 16;
 constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
 constexpr float kGap = 10.f;          // log2 units by which a maximum may exceed the row's reference
@@ -64,13 +64,12 @@ struct Cfg {
   static constexpr int NP = OC / 64;                         // panels of them: copied, announced and multiplied together
   static constexpr int KP = SHARED ? 0 : NP;                 // panels of K where V has its own
   static constexpr int QB = PAIR == 2 ? 2 : NT;              // tiles of Q in shared memory
-  static constexpr int BN = PAIR == 2 ? 48 : DP == 256 && !SHARED ? 64 : 128;            // keys of a block
+  static constexpr int BN = PAIR == 2 ? 48 : DP == 256 && SHARED ? 128 : 64;            // keys of a block
   static constexpr int SL = BN < 64 ? BN : 64;               // columns of a slab of S
   static constexpr int PB = BN * 128;                        // bytes of a panel of keys
-  static constexpr int NKB = KP == 0 ? 0 : DP == 64 ? 4 : DP == 512 ? 1 : 2;           // buffers of a block's K
-  static constexpr int NVB = DP == 64 ? 4 : DP == 128 ? (SHARED ? 4 : 2) : DP == 256 ? 2 : SHARED ? 3 : 2;   // of its V
-  static constexpr int SB = PAIR == 2 ? 4 : 2, SW = 2 * kTile / SB;  // buffers of S, their columns
-  static constexpr int WARPS = NT == 1 ? 16 : 15;
+  static constexpr int NKB = KP == 0 ? 0 : DP == 512 ? 1 : DP == 256 ? 2 : 4;          // buffers of a block's K
+  static constexpr int NVB = DP <= 128 ? 4 : DP == 512 && SHARED ? 3 : 2;   // of its V
+  static constexpr int SB = (BN > 64 || PAIR == 1 && NT == 1 ? 2 : 4) / NT, SW = 2 * kTile / (NT * SB);     // a tile's buffers of S, their columns
   static constexpr int TEAM = KP ? 2 : 4;                    // warps that copy a block of K or V
   static constexpr int RW = BN % (32 * TEAM) ? BN / TEAM : 32;       // rows that a warp copies at a time
   static constexpr int XB = PAIR == 2 ? kTile * BN * 4 : 0;  // the other CTA's part of S
@@ -91,7 +90,7 @@ struct TcCtl {
   uint64_t fullQ[2], emptyQ[2];               // by buffer
   uint64_t fullK[4], emptyK[4];
   uint64_t fullV[4], emptyV[4];
-  uint64_t s_full[4], p_ready[4], s_free[4], o_full[2], o_free[2];       // (s_free: of one tile)
+  uint64_t s_full[4], p_ready[4], s_free[4], o_full[2], o_free[2];
   uint64_t stat_full, stat_free;              // one tile: reference and sum of its rows, for the epilogue
   uint64_t x_full[4], x_free[4];              // a warp's rows of the other CTA's part of S: there; taken there, of this one's
   uint64_t bad_full[2][4];                    // the other CTA's word of `bad`, by turns
@@ -310,7 +309,7 @@ __device__ __noinline__ void exact_output(const AttnArgs& a, const TileList& t, 
 }
 
 template <int DP, bool SHARED>
-__global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel(const __grid_constant__ TcArgs g) {
+__global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_constant__ TcArgs g) {
   typedef Cfg<DP, SHARED> C;
   constexpr int NT = C::NT;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -322,7 +321,7 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
   const int rank = C::PAIR == 2 ? (int)(blockIdx.x & 1) : 0, col0 = rank * C::OC;      // its columns: from col0 on
   int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
   if (tid == 0) {
-    for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], C::WARPS - 1); }
+    for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], kWarps - 1); }
     for (int i = 0; i < 4; ++i) { bar_init(&sm.fullV[i], 32 * C::TEAM); bar_init(&sm.fullK[i], 32 * C::TEAM); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.s_free[i], 1); bar_init(&sm.x_full[i], 1); bar_init(&sm.x_free[i], 1); bar_init(&sm.bad_full[0][i], 1); bar_init(&sm.bad_full[1][i], 1); }
     for (int i = 0; i < 2; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.emptyQ[i], 1); bar_init(&sm.o_full[i], 1); bar_init(&sm.o_free[i], kTile); }
     bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
@@ -540,6 +539,8 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
     // ------------------------------------------------------------------ products (issued by one thread of a converged warp)
     const uint32_t idesc_v = make_idesc(C::OC, 1);
     const bool one = elect_one();
+    // the next S buffer of each tile, in a byte of its own (an item of one tile does not use the other's)
+    auto next = [&](uint32_t x, int t) { return (x >> 8 * t & 255u) + 1 == C::SB ? x & ~(255u << 8 * t) : x + (1u << 8 * t); };
     // S buffer xs = Q (buffer qb) K^T (buffer kb, of K or V), `keys` of them
     auto scores = [&](int xs, int qb, int kb, int keys) {
       fence_proxy();
@@ -567,99 +568,67 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
         }
       }
     };
-    if (NT == 2) {
-      // One warp: scores of block sb of tile t after the output of the block before, whose P lies where the scores will (the products of a
-      // thread are carried out in order).
-      uint32_t par_q = 0, par_k = 0, par_vs = 0, par_vo = 0, par_p = 0, par_o = 3;   // parities: buffers (of V for S and for O), tile
-      int kb = 0, vs = 0, vo = 0;                          // next K buffer, V buffer (for S, for O)
-      walk([&](const Item& w) {
-        const int nb = w.nb, nt = w.nt, k_all = w.k1 - w.k0;
-#pragma unroll 1
-        for (int sb = 0, t = 0; nb && sb <= nb;) {
-          const int ob = sb - 1;
-          const bool last = t == nt - 1;
-          if (ob >= 0) {
-            if (!SHARED) wait(&sm.fullV[vo], par_vo >> vo & 1);
-            if (ob == 0) { wait(&sm.o_free[t], par_o >> t & 1); par_o ^= 1u << t; }
-            wait(&sm.p_ready[t], par_p >> t & 1);
-            par_p ^= 1u << t;
-            fail = __any_sync(0xffffffffu, fail);
-            output(t, t, vo, k_all - ob * C::BN, ob);
-            if (one) {
-              if (last) mma_commit(&sm.emptyV[vo]);
-              if (ob == nb - 1) mma_commit(&sm.o_full[t]);
-            }
-            __syncwarp();
-            if (last) { par_vo ^= 1u << vo; vo = vo + 1 == C::NVB ? 0 : vo + 1; }
-          }
-          if (sb < nb) {
-            if (C::KP) wait(&sm.fullK[kb], par_k >> kb & 1); else wait(&sm.fullV[vs], par_vs >> vs & 1);
-            if (sb == 0) { wait(&sm.fullQ[t], par_q >> t & 1); par_q ^= 1u << t; }
-            fail = __any_sync(0xffffffffu, fail);
-            scores(t, t, C::KP ? kb : vs, k_all - sb * C::BN);
-            if (one) {
-              if (C::KP && last) mma_commit(&sm.emptyK[kb]);
-              mma_commit(&sm.s_full[t]);
-              if (last && sb == nb - 1) mma_commit(&sm.emptyQ[0]);
-            }
-            __syncwarp();
-            if (C::KP && last) { par_k ^= 1u << kb; kb = kb + 1 == C::NKB ? 0 : kb + 1; }
-            if (!C::KP && last) { par_vs ^= 1u << vs; vs = vs + 1 == C::NVB ? 0 : vs + 1; }
-          }
-          if (last) { t = 0; ++sb; } else ++t;
-        }
-      });
-    } else if (warp == kMmaWarp) {
+    if (warp == kMmaWarp) {
       // Scores, as far ahead as buffers allow, into the next item too
       constexpr int NB = C::KP ? C::NKB : C::NVB;
       uint64_t* full = C::KP ? sm.fullK : sm.fullV;
-      uint32_t par_q = 0, par_k = 0, par_s = 0xfu;
-      int kb = 0, x = 0, qb = 0;
+      uint32_t par_q = 0, par_k = 0, par_s = 0xfu;         // parities: a bit per buffer
+      uint32_t x = 0;
+      int kb = 0, qx = 0;                                  // next buffer of K, of a pair's Q
       walk([&](const Item& w) {
-        const int nb = w.nb, k_all = w.k1 - w.k0;
+        const int nb = w.nb, nt = NT == 2 ? w.nt : 1, k_all = w.k1 - w.k0;
+        if (nb == 0) return;
 #pragma unroll 1
         for (int j = 0; j < nb; ++j) {
           wait(&full[kb], par_k >> kb & 1);
           par_k ^= 1u << kb;
-          if (j == 0) { wait(&sm.fullQ[qb], par_q >> qb & 1); par_q ^= 1u << qb; }
-          wait(&sm.s_free[x], par_s >> x & 1);
-          par_s ^= 1u << x;
-          fail = __any_sync(0xffffffffu, fail);
-          scores(x, qb, kb, k_all - j * C::BN);
-          if (one) {
-            if (C::KP) mma_commit(&sm.emptyK[kb]);
-            mma_commit(&sm.s_full[x]);
-            if (j == nb - 1) mma_commit(&sm.emptyQ[qb]);
+#pragma unroll 1
+          for (int t = 0; t < nt; ++t) {
+            const int xs = t * C::SB + (int)(x >> 8 * t & 255u), qb = C::PAIR == 2 ? qx : t;
+            if (j == 0) { wait(&sm.fullQ[qb], par_q >> qb & 1); par_q ^= 1u << qb; }
+            wait(&sm.s_free[xs], par_s >> xs & 1);
+            par_s ^= 1u << xs;
+            fail = __any_sync(0xffffffffu, fail);
+            scores(xs, qb, kb, k_all - j * C::BN);
+            if (one) {
+              if (C::KP && t == nt - 1) mma_commit(&sm.emptyK[kb]);
+              mma_commit(&sm.s_full[xs]);
+              if (j == nb - 1 && t == nt - 1) mma_commit(&sm.emptyQ[C::PAIR == 2 ? qb : 0]);
+            }
+            __syncwarp();
+            x = next(x, t);
           }
-          __syncwarp();
           kb = kb + 1 == NB ? 0 : kb + 1;
-          x = (x + 1) % C::SB;
         }
-        if (nb) qb = (qb + 1) % C::QB;
+        qx ^= 1;
       });
     } else {
       // Outputs
-      uint32_t par_v = 0, par_p = 0, par_o = 1;
-      int vb = 0, x = 0;
+      uint32_t par_v = 0, par_p = 0, par_o = 3, x = 0;
+      int vb = 0;
       walk([&](const Item& w) {
-        const int nb = w.nb, k_all = w.k1 - w.k0;
+        const int nb = w.nb, nt = NT == 2 ? w.nt : 1, k_all = w.k1 - w.k0;
 #pragma unroll 1
         for (int j = 0; j < nb; ++j) {
           wait(&sm.fullV[vb], par_v >> vb & 1);
           par_v ^= 1u << vb;
-          if (j == 0) { wait(&sm.o_free[0], par_o); par_o ^= 1u; }
-          wait(&sm.p_ready[x], par_p >> x & 1);
-          par_p ^= 1u << x;
-          fail = __any_sync(0xffffffffu, fail);
-          output(0, x, vb, k_all - j * C::BN, j);
-          if (one) {
-            mma_commit(&sm.emptyV[vb]);
-            mma_commit(&sm.s_free[x]);
-            if (j == nb - 1) mma_commit(&sm.o_full[0]);
+#pragma unroll 1
+          for (int t = 0; t < nt; ++t) {
+            const int xo = t * C::SB + (int)(x >> 8 * t & 255u);
+            if (j == 0) { wait(&sm.o_free[t], par_o >> t & 1); par_o ^= 1u << t; }
+            wait(&sm.p_ready[xo], par_p >> xo & 1);
+            par_p ^= 1u << xo;
+            fail = __any_sync(0xffffffffu, fail);
+            output(t, xo, vb, k_all - j * C::BN, j);
+            if (one) {
+              if (t == nt - 1) mma_commit(&sm.emptyV[vb]);
+              mma_commit(&sm.s_free[xo]);
+              if (j == nb - 1) mma_commit(&sm.o_full[t]);
+            }
+            __syncwarp();
+            x = next(x, t);
           }
-          __syncwarp();
           vb = vb + 1 == C::NVB ? 0 : vb + 1;
-          x = (x + 1) % C::SB;
         }
       });
     }
@@ -792,9 +761,9 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
     } else {
       // ---------------------------------------------------------------- softmax
       uint32_t cS = 0, par_s = 0, n = 0;                   // blocks so far, parities of s_full; items
-      // O holds the blocks before this one.  Of two tiles: there are this block's scores, products of the same thread.
+      // O holds the blocks before this one.
       auto wait_o = [&]() {
-        if (NT == 1) wait(&sm.s_free[(cS - 1) % C::SB], (cS - 1) / C::SB & 1);
+        wait(&sm.s_free[tile * C::SB + (cS - 1) % C::SB], (cS - 1) / C::SB & 1);
         fence_after();
       };
       // A pair: this row's part of the scores goes to the other CTA, and that one's part is added (the sum is the same bits in both).
@@ -867,7 +836,7 @@ __global__ void __launch_bounds__(32 * Cfg<DP, SHARED>::WARPS, 1) attn_tc_kernel
         if (C::PAIR == 2) send(cS % C::SB);
 #pragma unroll 1
         for (int j = 0; j < nb; ++j) {
-          const int x = NT == 2 ? tile : (int)(cS % C::SB), c0 = k0 + j * C::BN, slabs = (min(C::BN, k1 - c0) + C::SL - 1) / C::SL;
+          const int x = tile * C::SB + (int)(cS % C::SB), c0 = k0 + j * C::BN, slabs = (min(C::BN, k1 - c0) + C::SL - 1) / C::SL;
           const uint32_t scol = s_col + x * C::SW + lane_at;
           if (C::PAIR == 1) {
             wait(&sm.s_full[x], par_s >> x & 1);
@@ -997,7 +966,7 @@ int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
   const int most = 148 / C::PAIR, grid = g.items < most ? g.items : most;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(grid * C::PAIR));
-  cfg.blockDim = dim3(32 * C::WARPS);
+  cfg.blockDim = dim3(32 * kWarps);
   cfg.dynamicSmemBytes = C::SMEM;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
