@@ -240,7 +240,7 @@ struct CopyArgs {
 
 // Thread 0 moves the planes' chunks: a load into the next stage once the store out of it has been read, a store three chunks behind the
 // loads.  The other warps copy the row arrays, which may be of 4-byte alignment, and renumber the table.
-// (Loads and stores through registers, 8 vectors of a thread: 289 MB of scattered pages 124 us instead of @.)
+// (Loads and stores through registers, 8 vectors of a thread: 289 MB of scattered pages 124 us instead of 111.)
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyArgs a) {
   extern __shared__ __align__(128) unsigned char stage[];
   __shared__ __align__(8) uint64_t bars[kStages];

@@ -3,22 +3,23 @@
 // A persistent CTA per SM walks over work items (one or two tiles, key head, columns, share of the keys), warps by role:
 //   warps 0-3    softmax of the first tile, a row per thread
 //   warps 4-7    softmax of the second tile; where there is one tile, its epilogue, under the next item's scores and softmax
-//   warp 8       issues the products: S = Q K^T; with two tiles also O += P V, P as the A operand straight from tensor memory
+//   warp 8       issues S = Q K^T, as far ahead as buffers allow, into the next item too
 //   warp 9       finds the items ahead of the others: tile, keys, tree
 //   warps 10-13  copy blocks of K and V into shared memory: two warps K, two V, or all four where K is V (a wait for a barrier's phase is
 //                only good for a thread that sees all of them).  Rows come by 16-byte asynchronous copies: from pages, a ring or the call's
 //                own tensors, any of them with strides of their own, which no tensor map describes; a barrier counts a block's copies as
 //                they land, and the thread that issues the products orders them before its reads (fence.proxy.async)
 //   warp 14      Q, by TMA where the heads of a key head fill a box evenly, else like K and V
-//   warp 15      where there is one tile, issues O += P V: the scores run ahead of it, into the next item too
+//   warp 15      issues O += P V, P as the A operand straight from tensor memory
 //
 // K and V live in panels of a block's rows x 64 columns (128-byte swizzle): K row-major is the K-major operand of S, and the same layout
 // read MN-major the operand of P V, so that where the keys are the values one copy serves both products.  Two tiles share a block of K
 // and V: copies (half of the shared-memory traffic of a tile) and their instructions per product halve, and one tile's softmax runs
 // under the other's products.
 //
-// Tensor memory: buffers of S (two of 128 columns, of the two tiles or of two blocks of the one; four of 64 at d = 512) and O.  P (bf16)
-// overlays the S it came from.
+// Tensor memory: O, and beside it at most 256 columns of S: two blocks' scores for each tile (four at d = 512), so that the next block's are
+// there when a softmax is done.  P (bf16) overlays the S it came from.  (Two tiles with one buffer of 128 columns each, scores after the
+// P V of the block before: 16 heads x 64 125 us instead of 117.)
 //
 // d = 512: Q of a tile (128 KiB) leaves no room for blocks of keys ahead, and tensor memory none for S beside all of O (512 columns).  So
 // an item belongs to the two CTAs of a cluster, each with half of the columns of Q, K, V and O: it multiplies its halves of Q and K, sends
@@ -31,10 +32,10 @@
 // there of P, the sum and O are multiplied by a power of two, exactly.  Nearly never after the first slab.
 // P is rounded to bf16 for the product (2^-9 of a weight); scores, sums and O are fp32.
 //
-// What bounds it (prompts of 32 heads on 8 x 128, window 1024, 17 k tokens: 547 us, 35 % of the tensor pipe's cycles, 37 % of the special
-// function units'): the products take 2.7 k cycles of a block of 128 keys (K = 16 of P V from tensor memory costs 103 cycles for 128
-// columns, of S from shared memory 64), a tile's softmax 1.3 k for 64 keys, mostly latencies of dependent instructions of the one warp
-// that a scheduler has for it.  At d = 512 a block's softmax and exchange (2.5 k cycles for 48 keys, of which 0.5 wait for the other CTA).
+// What bounds it (prompts of 32 heads on 8 x 128, window 1024, 17 k tokens: 540 us, 35 % of the tensor pipe's cycles, 37 % of the special
+// function units'): a tile's softmax of 64 keys takes 2.2 k cycles, a third of it the exponentials, which two warps of a scheduler share
+// the unit for, the rest latencies of dependent instructions; the products of both tiles 1.6 k (K = 16 of P V from tensor memory costs
+// 103 cycles for 128 columns, of S from shared memory 50 up to 64 keys).  At d = 512 a block's softmax and exchange (2.5 k cycles for 48 keys, of which 0.5 wait for the other CTA).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -47,7 +48,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = 128;            // query rows of a tile; columns of an S buffer
+constexpr int kTile = 128;            // query rows of a tile
 constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 5, kOutWarp = 15, kWarps = 16;
 constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
@@ -69,7 +70,7 @@ struct Cfg {
   static constexpr int PB = BN * 128;                        // bytes of a panel of keys
   static constexpr int NKB = KP == 0 ? 0 : DP == 512 ? 1 : DP == 256 ? 2 : 4;          // buffers of a block's K
   static constexpr int NVB = DP <= 128 ? 4 : DP == 512 && SHARED ? 3 : 2;   // of its V
-  static constexpr int SB = (BN > 64 || PAIR == 1 && NT == 1 ? 2 : 4) / NT, SW = 2 * kTile / (NT * SB);     // a tile's buffers of S, their columns
+  static constexpr int SB = (NT == 1 && PAIR == 1 ? 2 : 4) / NT, SW = 2 * kTile / (NT * SB);     // a tile's buffers of S, their columns
   static constexpr int TEAM = KP ? 2 : 4;                    // warps that copy a block of K or V
   static constexpr int RW = BN % (32 * TEAM) ? BN / TEAM : 32;       // rows that a warp copies at a time
   static constexpr int XB = PAIR == 2 ? kTile * BN * 4 : 0;  // the other CTA's part of S
@@ -116,7 +117,7 @@ __device__ __forceinline__ TcCtl& control() {
 }
 // A first look in line, then tries to the limit in a function: a wait is in the code of some thirty places.  A test is back sooner than a try
 // that may suspend, a try leaves the other warps more; pairs of CTAs, whose softmax hardly ever finds a phase incomplete, take the test
-// (prompts of 64 heads x 512: 672 against 691 us; 32 heads x 128 the other way about, 606 and 582).
+// (prompts of 64 heads x 512: 672 against 691 us; 32 heads x 128 the other way about, 565 and 540).
 __device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
   const uint32_t limit = control().limit;
 #pragma unroll 1
