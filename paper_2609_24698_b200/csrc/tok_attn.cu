@@ -194,10 +194,12 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 }
 
 // ---------------------------------------------------------------- bf16, 16 rows
-// Four warps: of a block of KB keys each computes the scores of a quarter (16 rows x KB / 4 keys over all of d), the row maxima go
-// through shared memory, then each adds the whole block's P V to its quarter of the output columns (d / 4: 16 rows x 128 columns are
-// 64 registers at d = 512).  P is rounded to bf16 for the product (half a step, 2^-9, of a weight; the sum of the weights is of the
-// unrounded ones); scores, maxima, sums and the output are fp32.  Rows of K and V come by 16-byte asynchronous copies, ST - 1 blocks
+// Four warps, blocks of KB keys.  d <= 128: a quarter of a block's keys is a warp's own from the scores to the output (16 rows x 128 columns
+// are 64 registers), with its own maxima and sums; the warps are joined at the end, and a block has one barrier.  (Through shared memory, as
+// below: 8 sequences of 32 heads on 8 x 128, 32 k keys, 365 us instead of @.)  Beyond, where one warp's registers do not hold all of d:
+// each computes the scores of a quarter of the keys, the row maxima go through shared memory, then each adds the whole block's P V to
+// its quarter of the output columns.  P is rounded to bf16 for the product (half a step, 2^-9, of a weight; the sum of the weights is of
+// the unrounded ones); scores, maxima, sums and the output are fp32.  Rows of K and V come by 16-byte asynchronous copies, ST - 1 blocks
 // ahead of the arithmetic (a window of 32 k tokens streams from HBM: that much has to be under way), through the page table or from the
 // new rows, whose addresses are worked out a block before their copies: 16-byte chunks of a row are stored at chunk ^ (row & 7), which
 // keeps every ldmatrix free of bank conflicts.  DP: d rounded up to 64, 128, 256 or 512, the rest zero.
@@ -216,7 +218,7 @@ struct MmaSmem {
   const bf16* row[ST + 1][SHARED ? 1 : 2][KB];      // where a block's rows begin (nullptr: nothing there)
   float red[4][kRows], sum[4][kRows];
   TileCtl c;
-  int missing[ST + 1];                // a key of the block has no page
+  int missing[ST + 1][2];             // a key of the block has no page (32 keys each)
 };
 
 template <int DP, bool SHARED>
@@ -226,10 +228,10 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
   Sm& sm = *reinterpret_cast<Sm*>(smem_raw);
   constexpr int KB = Sm::KB, ST = Sm::ST;
   constexpr int CH = DP / 8, KW = KB / 4, NT = KW / 8;    // 16-byte chunks of a row; keys of a warp, in tiles of 8
-  constexpr int CW = DP / 4, CT = CW / 8;                 // output columns of a warp, in tiles of 8
-  static_assert(sizeof(float) * kRows * DP <= sizeof(sm.k), "the output lies in the blocks' place");
+  constexpr bool OWN = DP <= 128;                         // a warp's keys are its own to the end
+  constexpr int CW = OWN ? DP : DP / 4, CT = CW / 8;      // output columns of a warp, in tiles of 8
+  static_assert(sizeof(float) * kRows * DP * (OWN ? 4 : 1) <= sizeof(sm.k), "the output lies in the blocks' place");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid <= ST) sm.missing[tid] = 0;
   if (!begin_tile<bf16>(a, sm.c)) return;
   const TileList& t = sm.c.t;
   int k0, k1;
@@ -241,8 +243,10 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
     int64_t code = -1;
     if (kk < k1) {
       code = list_row(a, t, kk);
-      if (code == -1) { sm.missing[slot] = 1; atomicOr(a.status + t.b, TSV_ST_PAGE); }
+      if (code == -1) atomicOr(a.status + t.b, TSV_ST_PAGE);
     }
+    const bool none = __any_sync(0xffffffffu, kk < k1 && code == -1);
+    if (lane == 0) sm.missing[slot][warp] = none;
     sm.row[slot][0][tid] = code == -1 ? nullptr : row_ptr<bf16>(a, t.hk, code, false);
     if (!SHARED) sm.row[slot][SHARED ? 0 : 1][tid] = code == -1 ? nullptr : row_ptr<bf16>(a, t.hk, code, true);
   };
@@ -282,6 +286,13 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
   uint32_t ra[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) { rp[h] = sm.c.pos[g + 8 * h]; ra[h] = sm.c.row_anc[g + 8 * h]; }
+  // Positions of the window part that every row sees.
+  int seen0 = 0, seen1 = -1;
+  {
+    const int p0 = __reduce_min_sync(0xffffffffu, lane < t.nr ? sm.c.pos[lane & (kRows - 1)] : 0x7fffffff), p1 = __reduce_max_sync(0xffffffffu, lane < t.nr ? sm.c.pos[lane & (kRows - 1)] : 0);
+    seen0 = max(t.lo, p1 - a.s.window + 1);
+    seen1 = min(t.lo + t.nc - t.ns - 1, p0);
+  }
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
   float o[CT][4];
 #pragma unroll
@@ -322,8 +333,16 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
       }
     }
     // masks, row maxima over the block
-    const bool missing = sm.missing[slot] != 0;
+    const bool missing = sm.missing[slot][0] || (KB > 32 && sm.missing[slot][1]);
     float mx[2] = {-INFINITY, -INFINITY};
+    const int kk0 = k0 + j * KB + warp * KW, at0 = t.lo + kk0 - t.ns;
+    const bool whole = !missing && kk0 >= t.ns && kk0 + KW <= k1 && at0 >= seen0 && at0 + KW - 1 <= seen1;
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { s[i][e] *= a.scale2; mx[e >> 1] = fmaxf(mx[e >> 1], s[i][e]); }
+    } else {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -334,10 +353,48 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
         s[i][e] = see ? s[i][e] * a.scale2 : -INFINITY;
         mx[h] = fmaxf(mx[h], s[i][e]);
       }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
       mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
+    }
+    if (OWN) {
+      float alpha[2], ref[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float mn = fmaxf(m[h], mx[h]);
+        ref[h] = mn == -INFINITY ? 0.f : mn;
+        alpha[h] = ex2(m[h] - ref[h]);
+        m[h] = mn;
+        l[h] *= alpha[h];
+      }
+      if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+        for (int i = 0; i < CT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][e] *= alpha[e >> 1];
+      }
+      uint32_t af[4];                                     // (the scores' places in the registers are those of the product's operand)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { float& x = s[i % NT][e]; x = ex2(x - ref[e >> 1]); l[e >> 1] += x; }
+        af[2 * i] = pack2(s[i % NT][0], s[i % NT][1]);
+        af[2 * i + 1] = pack2(s[i % NT][2], s[i % NT][3]);
+      }
+#pragma unroll
+      for (int i = 0; i < CT; i += 2) {
+        uint32_t bf[4];
+        const int r = warp * KW + (lane & 7) + ((lane >> 3) & 1) * 8, c = i + (lane >> 4);
+        ldsm4t(bf, vs + (uint32_t)(r * CH + (c ^ (r & 7))) * 16);
+        mma16816(o[i], af, bf);
+        mma16816(o[i + 1], af, bf + 2);
+      }
+      continue;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
       if (tc == 0) sm.red[warp][g + 8 * h] = mx[h];
     }
     __syncthreads();
@@ -367,7 +424,6 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
     for (int i = 0; i < CT; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] *= alpha[e >> 1];
-    if (tid == 0) sm.missing[slot] = 0;                   // (the block's after next, set behind the next barrier)
     __syncthreads();
     // P V, this warp's columns
 #pragma unroll
@@ -390,11 +446,46 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
   for (int h = 0; h < 2; ++h) {
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+    if (OWN && tc == 0) sm.red[warp][g + 8 * h] = m[h];
     if (tc == 0) sm.sum[warp][g + 8 * h] = l[h];
   }
   cp_wait<0>();
   __syncthreads();                                        // (and everyone is done with the blocks)
   float* os = reinterpret_cast<float*>(sm.k);
+  if (OWN) {
+    // the warps' shares at the rows' maxima, then added up in order
+    float part[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = g + 8 * h;
+      float mn = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) mn = fmaxf(mn, sm.red[w][r]);
+      const float to = mn == -INFINITY ? 0.f : mn;
+      part[h] = ex2(m[h] - to);
+      l[h] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) l[h] = fmaf(sm.sum[w][r], ex2(sm.red[w][r] - to), l[h]);
+      m[h] = mn;
+      if (warp == 0 && tc == 0) sm.c.ml[r] = make_float2(m[h], l[h]);
+      const bool bad = !is_finite(l[h]) || (m[h] == -INFINITY && a.nsplit == 1);
+      if (bad && pass == 0 && r < t.nr) atomicOr(&sm.c.bad, 1u << r);
+#pragma unroll
+      for (int i = 0; i < CT; ++i) *reinterpret_cast<float2*>(os + (warp * kRows + r) * DP + i * 8 + 2 * tc) = make_float2(o[i][2 * h] * part[h], o[i][2 * h + 1] * part[h]);
+    }
+    __syncthreads();
+    for (int i = tid; i < kRows * DP / 4; i += kThreads) {
+      float4 x = *reinterpret_cast<const float4*>(os + 4 * i);
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        const float4 y = *reinterpret_cast<const float4*>(os + w * kRows * DP + 4 * i);
+        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+      }
+      const int r = 4 * i / DP;
+      if (pass == 0 && r < t.nr && !(is_finite(x.x) && is_finite(x.y) && is_finite(x.z) && is_finite(x.w))) atomicOr(&sm.c.bad, 1u << r);
+      *reinterpret_cast<float4*>(os + 4 * i) = x;
+    }
+  } else
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int r = g + 8 * h;
