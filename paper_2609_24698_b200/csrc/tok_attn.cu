@@ -4,6 +4,8 @@
 //
 // Kernels here: attn_mma_kernel (bf16, few rows per sequence: 16 query rows, mma.sync), attn_fp32_kernel (fp32: 16 query rows, FMAs), and
 // attn_join_kernel, which joins the partial outputs of tiles whose keys were split over CTAs.  Calls with more rows: tok_attn_tc.cu.
+#include <algorithm>
+
 #include "tok_attn.cuh"
 #include "tc_common.cuh"
 
@@ -196,7 +198,7 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 // ---------------------------------------------------------------- bf16, 16 rows
 // Four warps, blocks of KB keys.  d <= 128: a quarter of a block's keys is a warp's own from the scores to the output (16 rows x 128 columns
 // are 64 registers), with its own maxima and sums; the warps are joined at the end, and a block has one barrier.  (Through shared memory, as
-// below: 8 sequences of 32 heads on 8 x 128, 32 k keys, 365 us instead of @.)  Beyond, where one warp's registers do not hold all of d:
+// below: 8 sequences of 32 heads on 8 x 128, 32 k keys, 366 us instead of 277.)  Beyond, where one warp's registers do not hold all of d:
 // each computes the scores of a quarter of the keys, the row maxima go through shared memory, then each adds the whole block's P V to
 // its quarter of the output columns.  P is rounded to bf16 for the product (half a step, 2^-9, of a weight; the sum of the weights is of
 // the unrounded ones); scores, maxima, sums and the output are fp32.  Rows of K and V come by 16-byte asynchronous copies, ST - 1 blocks
@@ -756,8 +758,9 @@ bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s
 // Tiles and CTAs that splitting the keys aims at: those that run at a time.
 int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? 148 / tc_halves(s.d) : s.d <= 128 ? 2 * 148 : 148; }
 
-// Keys are split where the tiles alone would leave SMs without work.  16-row tiles: into up to eight shares of 32 keys and more, a
-// cluster's CTAs, which join them; into more only where a share of eight would still be longer than 512 keys, through partial outputs.
+// Keys are split where the tiles alone would leave SMs without work.  Tiles of 16 rows: into shares of 32 keys and more, up to eight as a
+// cluster's CTAs, which join them; into more, of 512 keys and more, through partial outputs.  (8 sequences of 8 key heads x 128, 32 k keys:
+// 9 shares, nearly two rounds of CTAs, 262 us; 4, not all of one, 278.)
 AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   AttnPlan p;
   p.tc = takes_tc(s);
@@ -767,17 +770,20 @@ AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   int64_t reach = (int64_t)s.window + s.max_n;
   if (reach > s.max_L) reach = s.max_L;
   const int64_t keys = reach + (s.n_sink < s.max_L ? s.n_sink : s.max_L);
-  auto shares = [&](int64_t least) {
-    int64_t ns = slots_of(s) / ctas;                      // (no more CTAs than run at a time)
-    if (ns > (keys + least - 1) / least) ns = (keys + least - 1) / least;
-    return (int)(ns < 1 ? 1 : ns > 64 ? 64 : ns);
-  };
   p.cluster = 0;
-  p.nsplit = shares(512);
-  if (!p.tc && p.nsplit <= 8) {
-    p.nsplit = shares(32);
-    if (p.nsplit > 8) p.nsplit = 8;
-    p.cluster = p.nsplit > 1;
+  if (p.tc) {                                             // 512 keys and more, and no more CTAs than run at a time
+    const int64_t ns = std::min(slots_of(s) / ctas, (keys + 511) / 512);
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(ns, 64));
+  } else {
+    // The time in keys: rounds of CTAs, of a share and what a CTA takes without keys; more than eight shares, which another kernel joins.
+    int64_t best = INT64_MAX;
+    for (int ns = 1; ns <= 64; ++ns) {
+      const int64_t share = ((keys + ns - 1) / ns + 15) & ~15, all = ctas * ns;
+      if (ns > 1 && ((ns - 1) * (ns > 8 ? 512 : 32) >= keys || (ns > 8 && all > 2 * slots_of(s)))) break;
+      const int64_t time = (all + slots_of(s) - 1) / slots_of(s) * (share + 128) + (ns > 8 ? 200 : 0);
+      if (time < best) { best = time; p.nsplit = ns; }
+    }
+    p.cluster = p.nsplit > 1 && p.nsplit <= 8;
   }
   p.off_pml = up256((size_t)2 * slots_of(s) * p.per * s.d * sizeof(float));
   return p;
