@@ -751,8 +751,9 @@ struct AttnPlan {
 };
 
 // bf16 in tiles of 128 rows where a sequence may have more rows for a key head than one tile of 16.  us, tiles of 128 / of 16 rows, 32 heads
-// on 8 of 128: 64 sequences, window 1024: 16 rows 95 / 112, 32 rows 97 / 209, 64 rows 98 / 362; 4 sequences, window 128: 17 / 14, 17 / 15,
-// 17 / 18; window 2048: 32 / 29, 32 / 38, 36 / 59.
+// on 8 of 128: 64 sequences, window 1024: 16 rows 80 / 99, 32 rows 81 / 205, 64 rows 82 / 315; 4 sequences, window 128: 16 / 16, 15 / 17,
+// 16 / 21; 8 heads of 64, 64 sequences, window 1024: 74 / 70, 76 / 119, 82 / 168.  Single tokens (1 to 256 sequences, windows of 128 to
+// 32 k): d = 64 and 128 shared 17 / 15 to 97 / 72, the larger ones of 32 on 8 x 128 and of d above 128 the other way about, 135 / 160, 73 / 101.
 bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s.max_n * (s.H / s.Hk) > kRows; }
 
 // Tiles and CTAs that splitting the keys aims at: those that run at a time.
