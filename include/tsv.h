@@ -390,7 +390,8 @@ size_t tsv_tok_workspace_bytes(const tsv_tok_shape *shape, int64_t rows);
  * cache->v is: the keys are the values).  In a tree a node sees, of the new tokens, itself and its ancestors, under the same
  * window.  The cache is not written.  What a query may not see has no influence on its result, also if it is not finite.
  * A page that a query needs and that is not one of the pool's (-1, beyond `rows`, or a position beyond max_pages) is left
- * out, and the sequence flagged TSV_ST_PAGE.
+ * out, and the sequence flagged TSV_ST_PAGE.  `out` must not overlap the rows of `in` (TSV_ERR_SHAPE): a result that is not
+ * finite has them read once more.
  */
 int window_sink_attn(const tsv_tok_shape *shape, const tsv_tok_cache *cache, const tsv_tok_batch *batch, const tsv_tok_rows *in,
                      void *out, void *workspace, size_t workspace_bytes, int32_t *status, void *stream);

@@ -34,6 +34,13 @@ static int check_rows(const tsv_tok_shape* s, const void* p, int64_t ld, int hea
   return ld % ve ? TSV_ERR_ALIGN : TSV_OK;
 }
 
+// Do heads of rows rows, ld elements apart, share bytes with [out, out + bytes)?
+static bool meets(const tsv_tok_shape* s, const void* out, int64_t bytes, const void* p, int64_t ld, int heads, int64_t rows) {
+  const int64_t es = s->dtype == TSV_BF16 ? 2 : 4, span = ((rows - 1) * ld + (int64_t)heads * s->d) * es;
+  const char *a = (const char*)out, *b = (const char*)p;
+  return p && a < b + span && b < a + bytes;
+}
+
 static int check_tok_cache(const tsv_tok_cache* c, const tsv_tok_shape* s) {
   if (!c || !c->L || !c->k) return TSV_ERR_NULL;
   if (!al(c->k, 16) || !al(c->v, 16)) return TSV_ERR_ALIGN;
@@ -118,6 +125,11 @@ int window_sink_attn(const tsv_tok_shape* shape, const tsv_tok_cache* cache, con
   if (batch->rows && (r = check_rows(shape, in->q, in->q_ld, shape->H))) return r;
   if (!al(out, 16)) return TSV_ERR_ALIGN;
   if ((r = check_ws(workspace, workspace_bytes, tok_attn_workspace(*shape, batch->rows)))) return r;
+  if (const int64_t n = batch->rows) {
+    const int64_t bytes = n * shape->H * shape->d * (shape->dtype == TSV_BF16 ? 2 : 4);
+    if (meets(shape, out, bytes, in->q, in->q_ld, shape->H, n) || meets(shape, out, bytes, in->k, in->k_ld, shape->Hk, n) ||
+        meets(shape, out, bytes, in->v, in->v_ld, shape->Hk, n)) return TSV_ERR_SHAPE;
+  }
   return launch_tok_attn(resolved(shape), *cache, *batch, *in, out, (char*)workspace, status, (cudaStream_t)stream);
 }
 

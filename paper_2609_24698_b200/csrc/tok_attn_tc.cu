@@ -54,6 +54,8 @@ constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
 constexpr float kGap = 10.f;          // log2 units by which a maximum may exceed the row's reference
 constexpr int kCtl = 3072;
+// Polls of up to 4 us before a wait gives up: a role may wait for a whole item, and that may be millions of keys, or rows computed one by one.
+constexpr uint32_t kWaitLimit = WAIT_LIMIT << 8;
 
 template <int N> struct Int { static constexpr int value = N; };
 
@@ -98,7 +100,6 @@ struct TcCtl {
   uint32_t bad[2][4];                         // rows with a result that is not finite there, a bit each
   uint64_t item_full[kItems], item_free[kItems];
   uint32_t tmem_base;
-  uint32_t limit;                     // of a wait: polls
   uint32_t redo[32];                  // items with a result that is not finite, a bit each
   float2 stat[kTile];
   Item item[kItems];
@@ -111,17 +112,12 @@ __device__ __forceinline__ void bar_init(uint64_t* b, int count) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
 }
-__device__ __forceinline__ TcCtl& control() {
-  extern __shared__ __align__(1024) unsigned char smem_raw[];
-  return *reinterpret_cast<TcCtl*>(smem_raw);
-}
 // A first look in line, then tries to the limit in a function: a wait is in the code of some thirty places.  A test is back sooner than a try
 // that may suspend, a try leaves the other warps more; pairs of CTAs, whose softmax hardly ever finds a phase incomplete, take the test
 // (prompts of 64 heads x 512: 672 against 691 us; 32 heads x 128 the other way about, 565 and 540).
 __device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
-  const uint32_t limit = control().limit;
 #pragma unroll 1
-  for (uint32_t it = 0; it < limit; ++it) {
+  for (uint32_t it = 0; it < kWaitLimit; ++it) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
@@ -142,9 +138,9 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
 }
 // The same for what the other CTA of a pair sends.
 __device__ __noinline__ bool bar_wait_pair(uint64_t* bar, uint32_t parity) {
-  const uint32_t addr = smem_u32(bar), limit = control().limit;
+  const uint32_t addr = smem_u32(bar);
 #pragma unroll 1
-  for (uint32_t it = 0; it < limit; ++it) {
+  for (uint32_t it = 0; it < kWaitLimit; ++it) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
@@ -328,7 +324,6 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
     bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (tid == 0) sm.limit = WAIT_LIMIT;
   if (tid < 32) sm.redo[tid] = 0;
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
@@ -341,8 +336,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
   const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + 2 * kTile;
 
   auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait<C::PAIR == 2>(b, parity)) fail = 1; };
-  // After the first round: whether there is a second (alike in all threads of a CTA or a pair).  It computes rows one by one, and its waits
-  // have 256 times the limit.
+  // After the first round: whether there is a second (alike in all threads of a CTA or a pair).
   auto marks = [&](int i) {
     uint32_t m = sm.redo[i & 31];
     if (C::PAIR == 2) {
@@ -356,7 +350,6 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
     all_sync();
     uint32_t any = 0;
     for (int i = 0; i < 32; ++i) any |= marks(i);
-    if (tid == 0) sm.limit = WAIT_LIMIT << 8;
     return any != 0;
   };
   // Calls body(item) for this CTA's items, as the list warp finds them, until it marks the end; then, where one has left a mark, for those.

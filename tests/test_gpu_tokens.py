@@ -144,6 +144,15 @@ def test_head_layouts(api, heads, tree):
     lay.check(lay.run(tk))
 
 
+# the same heads with more rows for a key head than a small tile has
+@pytest.mark.parametrize("heads", [h for h in HEADS + ODD_HEADS if h[0] == "bf16"], ids=lambda h: "_".join(map(str, h)))
+@pytest.mark.parametrize("tree", [False, True])
+def test_head_layouts_with_more_rows(api, heads, tree):
+    _, tk, _ = api
+    lay = Layer(tk, *heads, window=37, sinks=3, L=[0, 1, 36, 90], n=[18, 1, 32 if tree else 47, 0], tree=tree, page=0 if tree else 24, seed=hash(heads) % 1000)
+    lay.check(lay.run(tk))
+
+
 # window, sinks: one position; no sinks; sinks that reach into the window, into the new tokens, beyond everything; a window beyond everything
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 2), (5, 0), (16, 40), (33, 4), (64, 1), (500, 0), (500, 600), (2 ** 30, 0)])
 @pytest.mark.parametrize("heads", [("bf16", 8, 2, 64, False), ("bf16", 4, 1, 512, True), ("fp32", 4, 1, 64, True)], ids=lambda h: "_".join(map(str, h)))

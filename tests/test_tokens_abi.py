@@ -92,6 +92,19 @@ def test_more_attention_refusals(api):
     assert f(a(s), a(cache), a(batch), a(rows), FAKE, FAKE, 1 << 40, FAKE, None) == tsv.ERR_SHAPE
 
 
+def test_output_over_inputs_is_refused(api):
+    tsv, tk, _ = api
+    cache, batch, rows = _structs(tk)
+    f, a, s = tsv._lib.window_sink_attn, C.addressof, _shape(tk)
+    es, n = 2 if s.dtype == tsv.TSV_BF16 else 4, batch.rows
+    out_bytes = n * s.H * s.d * es
+    rows.q, rows.k, rows.v = 1 << 30, 2 << 30, 3 << 30
+    for base, ld, heads in ((rows.q, rows.q_ld, s.H), (rows.k, rows.k_ld, s.Hk), (rows.v, rows.v_ld, s.Hk)):
+        span = ((n - 1) * ld + heads * s.d) * es
+        for out in (base, base + 16, base + span - 16, base - out_bytes + 16):
+            assert f(a(s), a(cache), a(batch), a(rows), out, FAKE, 1 << 40, FAKE, None) == tsv.ERR_SHAPE
+
+
 def test_rope_refusals(api):
     tsv, tk, _ = api
     _, batch, rows = _structs(tk)
