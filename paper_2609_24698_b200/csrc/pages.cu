@@ -40,6 +40,27 @@ inline Work work_of(char* ws, int n_pages) {
   return w;
 }
 
+// The sum over the warps before this one of a number that a warp's lanes have alike; the sum of all in s_warp[kPlanWarps].  By the whole CTA.
+__device__ __forceinline__ int warps_before(int mine, int* s_warp /* [kPlanWarps + 1] */) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncthreads();
+  if (lane == 0) s_warp[warp] = mine;
+  __syncthreads();
+  if (warp == 0) {
+    const int v = s_warp[lane];
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    s_warp[lane] = x - v;
+    if (lane == 31) s_warp[kPlanWarps] = x;
+  }
+  __syncthreads();
+  return s_warp[warp];
+}
+
 // Goes over pages p0 .. p1 - 1 in rounds of kPlanThreads * kScan and calls emit(page, rank) for those with `want(page)`, rank counted from
 // the lowest; stops behind the round that reaches `enough`.  Returns their number (of the rounds gone over).  By the whole CTA.
 template <typename Want, typename Emit>
@@ -54,22 +75,7 @@ __device__ __forceinline__ int scan_pages(int p0, int p1, int enough, int* s_war
     for (int k = 0; k < kScan; ++k) hit[k] = at + 32 * k < p1 && want((int)(at + 32 * k)) ? 1u : 0u;
 #pragma unroll
     for (int k = 0; k < kScan; ++k) { hit[k] = __ballot_sync(0xffffffffu, hit[k]); mine += __popc(hit[k]); }
-    __syncthreads();
-    if (lane == 0) s_warp[warp] = mine;
-    __syncthreads();
-    if (warp == 0) {
-      const int v = s_warp[lane];
-      int x = v;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      s_warp[lane] = x - v;
-      if (lane == 31) s_warp[kPlanWarps] = x;
-    }
-    __syncthreads();
-    int rank = total + s_warp[warp];
+    int rank = total + warps_before(mine, s_warp);
 #pragma unroll
     for (int k = 0; k < kScan; ++k) {
       if (hit[k] >> lane & 1u) emit((int)(at + 32 * k), rank + __popc(hit[k] & ((1u << lane) - 1u)));
@@ -212,10 +218,44 @@ __global__ void __launch_bounds__(kCopyThreads) free_kernel(const Pool p, const 
 
 __global__ void __launch_bounds__(kPlanThreads) compact_kernel(const Pool p, const Work w, int32_t* n_used) {
   __shared__ int s_warp[kPlanWarps + 1];
-  const int used = scan_pages(0, p.n_pages, p.n_pages + 1, s_warp, [&](int pg) { return p.ref[pg] != 0; }, [](int, int) {});
-  scan_pages(0, used, p.n_pages + 1, s_warp, [&](int pg) { return p.ref[pg] == 0; }, [&](int pg, int rank) { w.pages[rank].y = pg; });
-  const int moves = scan_pages(used, p.n_pages, p.n_pages + 1, s_warp, [&](int pg) { w.list[pg] = pg; return p.ref[pg] != 0; },
-                               [&](int pg, int rank) { w.pages[rank].x = pg; });
+  int used, moves;
+  if (p.n_pages <= kPlanThreads * kScan) {                // the counts stay in registers (three scans of them: a call of few pages 27.6 us instead of 23.5)
+    const int lane = threadIdx.x & 31, at = (threadIdx.x >> 5) * 32 * kScan + lane;
+    unsigned held = 0;
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < kScan; ++k) held |= (at + 32 * k < p.n_pages && p.ref[at + 32 * k] != 0 ? 1u : 0u) << k;
+#pragma unroll
+    for (int k = 0; k < kScan; ++k) mine += __popc(__ballot_sync(0xffffffffu, held >> k & 1u));
+    warps_before(mine, s_warp);
+    used = s_warp[kPlanWarps];
+    unsigned hole[kScan], far[kScan];
+    mine = 0;                                             // holes below, pages beyond: 16 bits each (at most 8192 of each)
+#pragma unroll
+    for (int k = 0; k < kScan; ++k) {
+      const int pg = at + 32 * k;
+      hole[k] = __ballot_sync(0xffffffffu, pg < used && !(held >> k & 1u));
+      far[k] = __ballot_sync(0xffffffffu, pg >= used && (held >> k & 1u));
+      mine += __popc(hole[k]) + (__popc(far[k]) << 16);
+    }
+    int rank = warps_before(mine, s_warp);
+    moves = s_warp[kPlanWarps] & 0xffff;
+#pragma unroll
+    for (int k = 0; k < kScan; ++k) {
+      const int pg = at + 32 * k;
+      const unsigned below = (1u << lane) - 1u;
+      if (hole[k] >> lane & 1u) w.pages[(rank & 0xffff) + __popc(hole[k] & below)].y = pg;
+      if (far[k] >> lane & 1u) w.pages[(rank >> 16) + __popc(far[k] & below)].x = pg;
+      if (pg >= used && pg < p.n_pages) w.list[pg] = pg;
+      rank += __popc(hole[k]) + (__popc(far[k]) << 16);
+    }
+    __syncthreads();
+  } else {
+    used = scan_pages(0, p.n_pages, p.n_pages + 1, s_warp, [&](int pg) { return p.ref[pg] != 0; }, [](int, int) {});
+    scan_pages(0, used, p.n_pages + 1, s_warp, [&](int pg) { return p.ref[pg] == 0; }, [&](int pg, int rank) { w.pages[rank].y = pg; });
+    moves = scan_pages(used, p.n_pages, p.n_pages + 1, s_warp, [&](int pg) { w.list[pg] = pg; return p.ref[pg] != 0; },
+                       [&](int pg, int rank) { w.pages[rank].x = pg; });
+  }
   for (int i = threadIdx.x; i < moves; i += kPlanThreads) {
     const int2 m = w.pages[i];
     w.list[m.x] = m.y;

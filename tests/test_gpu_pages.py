@@ -128,6 +128,18 @@ def test_the_largest_list_and_none(api):
     assert e.value.code == tsv.ERR_LIMIT
 
 
+@pytest.mark.parametrize("n_pages", [16384, 16385])       # (as many as stay in one CTA's registers, and one more)
+def test_compaction_of_a_large_pool(api, n_pages):
+    _, _, pg = api
+    x = Both(pg, 256, 64, n_pages, 4, [4], [], 9)
+    for half in (0, 1):
+        x.call("assign", list(range(128 * half, 128 * half + 128)), [0] * 128, [64] * 128)
+    gone = [int(v) for v in x.rng.permutation(256)[:150]]
+    x.call("free", gone, [int(v) for v in x.rng.integers(0, 30, 150)], [int(v) for v in x.rng.integers(30, 65, 150)])
+    x.compact()
+    x.compact()                                           # (nothing moves)
+
+
 def test_many_planes(api):
     """More arrays than one launch's parameters hold."""
     _, _, pg = api
