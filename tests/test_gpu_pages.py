@@ -140,6 +140,30 @@ def test_compaction_of_a_large_pool(api, n_pages):
     x.compact()                                           # (nothing moves)
 
 
+def test_pages_beyond_32_bits(api):
+    """A fork's copy and a compaction's move between pages that lie 6 GB apart."""
+    _, _, pg = api
+    n_pages, words = 6000, 1 << 18
+    plane = torch.empty(n_pages, words, dtype=torch.int32, device="cuda")
+    L = i32(5, 0, 0)
+    pool = pg.PagePool(torch.full((3, 2), -1, dtype=torch.int32, device="cuda"), torch.ones(n_pages, dtype=torch.int32, device="cuda"), 4, [plane], [L])
+    pool.page_table[0] = i32(7, 5990)
+    pool.ref[5995] = 0
+    plane[7], plane[5990] = 7, torch.arange(words, dtype=torch.int32, device="cuda")
+    ws, status = pg.alloc_workspace(pool), i32(0)
+    pg.pages_fork(pool, i32(0), i32(2), L, ws, status)
+    assert not status.any() and pool.page_table[2].tolist() == [7, 5995] and torch.equal(plane[5995], plane[5990]) and L.tolist() == [5, 0, 5]
+    pool.ref.zero_()
+    pool.ref[7], pool.ref[5990], pool.ref[5995] = 2, 1, 1
+    plane[5995] += 1
+    n = i32(0)
+    pg.pages_compact(pool, n, ws)
+    assert n.tolist() == [3] and pool.ref[:3].tolist() == [2, 1, 1] and not pool.ref[3:].any()
+    a, b = pool.page_table[0].tolist(), pool.page_table[2].tolist()
+    assert a[0] == b[0] and sorted({a[0], a[1], b[1]}) == [0, 1, 2]
+    assert (plane[a[0]] == 7).all() and torch.equal(plane[a[1]], torch.arange(words, dtype=torch.int32, device="cuda")) and torch.equal(plane[b[1]], plane[a[1]] + 1)
+
+
 def test_many_planes(api):
     """More arrays than one launch's parameters hold."""
     _, _, pg = api

@@ -173,6 +173,35 @@ def test_pages(api, page, heads):
     lay.check(lay.run(tk))
 
 
+# the same pages at the end of a pool of more than 2^32 elements
+@pytest.mark.parametrize("heads", [("bf16", 64, 1, 512, True), ("bf16", 8, 2, 128, False), ("fp32", 4, 1, 256, True)], ids=lambda h: "_".join(map(str, h)))
+@pytest.mark.parametrize("n", [[1, 1], [40, 90]])
+def test_pages_beyond_32_bits(api, heads, n):
+    _, tk, _ = api
+    page = 32
+    lay = Layer(tk, *heads, window=50, sinks=2, L=[300, 45], n=n, page=page, seed=6)
+    want = lay.run(tk)
+    small = [t for t in (lay.cache.k, lay.cache.v) if t is not None]
+    rows, row = small[0].shape[0], lay.shape.Hk * lay.shape.d
+    first = ((1 << 32) // row // page + 1) * page
+    big = []
+    for t in small:
+        x = torch.empty(first + rows, *t.shape[1:], dtype=t.dtype, device="cuda")
+        x[first:] = t
+        big.append(x)
+    assert first * row >= 1 << 32
+    table = torch.where(lay.cache.page_table >= 0, lay.cache.page_table + first // page, -1).int()
+    lay.cache = tk.TokenCache(lay.cache.L, big[0], big[1] if len(big) > 1 else None, table, page)
+    assert torch.equal(lay.run(tk).nan_to_num(9), want.nan_to_num(9))
+    tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, lay.status)
+    assert not lay.status.any()
+    for b, L in enumerate(lay.L):
+        pos = torch.arange(L, L + n[b])
+        at = (table[b].cpu()[pos // page].long() * page + pos % page).cuda()
+        for x, src in zip(big, (lay.k, lay.v)):
+            assert torch.equal(x[at], src[lay.row0[b]:lay.row0[b] + n[b]])
+
+
 # many tokens: tiles of queries that begin and end inside tokens, prompts with and without history
 @pytest.mark.parametrize("heads,window,L,n", [
     (("bf16", 6, 2, 64, False), 70, [0, 45, 200], [333, 130, 257]), (("bf16", 5, 1, 128, True), 129, [0, 5], [300, 201]),
