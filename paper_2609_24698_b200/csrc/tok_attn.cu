@@ -753,8 +753,18 @@ struct AttnPlan {
 // bf16 in tiles of 128 rows where a sequence may have more rows for a key head than one tile of 16.  us, tiles of 128 / of 16 rows, 32 heads
 // on 8 of 128: 64 sequences, window 1024: 16 rows 80 / 99, 32 rows 81 / 205, 64 rows 82 / 315; 4 sequences, window 128: 16 / 16, 15 / 17,
 // 16 / 21; 8 heads of 64, 64 sequences, window 1024: 74 / 70, 76 / 119, 82 / 168.  Single tokens (1 to 256 sequences, windows of 128 to
-// 32 k): d = 64 and 128 shared 17 / 15 to 97 / 72, the larger ones of 32 on 8 x 128 and of d above 128 the other way about, 135 / 160, 73 / 101.
-bool takes_tc(const tsv_tok_shape& s) { return s.dtype == TSV_BF16 && (int64_t)s.max_n * (s.H / s.Hk) > kRows; }
+// 32 k): d = 64 and 128 shared 17 / 15 to 97 / 72, the larger ones of 32 on 8 x 128 and of d above 128 the other way about, 135 / 160.
+// Above d = 128 also where there are 64 tiles and more, or lists of 16 k keys: 16 heads x 512, 256 sequences, window 128 42 / 55, 64 of 2048
+// 81 / 91, one of 32 k 56 / 60, but eight of 2048 38 / 34; 8 heads on 8 x 256, 64 of 2048 201 / 296, eight of 32 k 364 / 932; the worst found
+// was 2 heads x 512 with values of their own, eight of 32 k 216 / 185.
+int64_t keys_of(const tsv_tok_shape& s) {                 // of a list, at most
+  const int64_t reach = std::min<int64_t>((int64_t)s.window + s.max_n, s.max_L);
+  return reach + std::min<int64_t>(s.n_sink, s.max_L);
+}
+bool takes_tc(const tsv_tok_shape& s) {
+  if (s.dtype != TSV_BF16) return false;
+  return (int64_t)s.max_n * (s.H / s.Hk) > kRows || (s.d > 128 && ((int64_t)s.B * s.Hk >= 64 || keys_of(s) >= 16384));
+}
 
 // Tiles and CTAs that splitting the keys aims at: those that run at a time.
 int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? 148 / tc_halves(s.d) : s.d <= 128 ? 2 * 148 : 148; }
@@ -768,9 +778,7 @@ AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   p.per = p.tc ? tc_tile(s.d) : kRows;
   p.tiles = tok_units_bound(s, rows, s.H / s.Hk, p.per);
   const int64_t ctas = p.tiles * s.Hk;
-  int64_t reach = (int64_t)s.window + s.max_n;
-  if (reach > s.max_L) reach = s.max_L;
-  const int64_t keys = reach + (s.n_sink < s.max_L ? s.n_sink : s.max_L);
+  const int64_t keys = keys_of(s);
   p.cluster = 0;
   if (p.tc) {                                             // 512 keys and more, and no more CTAs than run at a time
     const int64_t ns = std::min(slots_of(s) / ctas, (keys + 511) / 512);

@@ -173,6 +173,19 @@ def test_pages(api, page, heads):
     lay.check(lay.run(tk))
 
 
+# a token or two of many sequences, some of them of none; lists of many keys
+@pytest.mark.parametrize("heads,L,n,window", [
+    (("bf16", 16, 1, 512, True), [3 * i for i in range(70)], [(1, 2, 1, 0)[i % 4] for i in range(70)], 60),
+    (("bf16", 6, 2, 264, False), [5 * i % 97 for i in range(40)], [1] * 40, 33),
+    (("bf16", 3, 1, 256, True), [i for i in range(66)], [(1, 4)[i % 2] for i in range(66)], 128), (("bf16", 2, 1, 200, True), [17000, 50], [1, 2], 16900),
+    (("bf16", 4, 1, 512, False), [16700], [1], 16500)], ids=lambda x: "" if isinstance(x, list) else str(x))
+@pytest.mark.parametrize("page", [0, 16])
+def test_single_tokens(api, heads, L, n, window, page):
+    _, tk, _ = api
+    lay = Layer(tk, *heads, window=window, sinks=4, L=L, n=n, page=page, seed=len(L))
+    lay.check(lay.run(tk))
+
+
 # the same pages at the end of a pool of more than 2^32 elements
 @pytest.mark.parametrize("heads", [("bf16", 64, 1, 512, True), ("bf16", 8, 2, 128, False), ("fp32", 4, 1, 256, True)], ids=lambda h: "_".join(map(str, h)))
 @pytest.mark.parametrize("n", [[1, 1], [40, 90]])
