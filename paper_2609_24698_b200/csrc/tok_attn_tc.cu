@@ -53,7 +53,7 @@ constexpr int kMmaWarp = 8, kListWarp = 9, kCopyWarps = 5, kOutWarp = 15, kWarps
 constexpr int kPanel = 16384;
 constexpr int kItems = 3;             // items found ahead
 constexpr float kGap = 10.f;          // log2 units by which a maximum may exceed the row's reference
-constexpr int kCtl = 3072;
+constexpr int kCtl = 3 * 1024;            // bytes in front of the panels (a multiple of 1024)
 // Polls of up to 4 us before a wait gives up: a role may wait for a whole item, and that may be millions of keys, or rows computed one by one.
 constexpr uint32_t kWaitLimit = WAIT_LIMIT << 8;
 
