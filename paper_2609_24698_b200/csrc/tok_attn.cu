@@ -83,7 +83,7 @@ struct TileCtl {
   int pos[kRows];
   uint32_t row_anc[kRows];
   TileList t;
-  uint32_t bad;
+  uint32_t bad, still;                // rows with a result that is not finite, after the first pass and after the second
 };
 
 // The tile of this CTA; false (alike in all CTAs of a cluster) where there is nothing to attend to.
@@ -91,7 +91,7 @@ template <typename T>
 __device__ __forceinline__ bool begin_tile(const AttnArgs& a, TileCtl& sm) {
   if (threadIdx.x < 32) {
     const TileList t = make_list(a, blockIdx.x, blockIdx.y, kRows, sm.depth, sm.anc);
-    if (threadIdx.x == 0) { sm.t = t; sm.bad = 0; }
+    if (threadIdx.x == 0) { sm.t = t; sm.bad = 0; sm.still = 0; }
   }
   __syncthreads();
   const TileList& t = sm.t;
@@ -109,7 +109,21 @@ __device__ __forceinline__ bool begin_tile(const AttnArgs& a, TileCtl& sm) {
 }
 
 // From o [16][ld] and sm.ml in shared memory, written by this CTA before, to the output: through the partial outputs, or at once, the
-// shares of a cluster's CTAs joined in order.  Rows of sm.bad that see something not finite are computed by definition first.
+// shares of a cluster's CTAs joined in order.  Rows of sm.bad that see something not finite, and those of sm.still, are computed by
+// definition first.
+__device__ __forceinline__ bool all_finite(const float4& x) { return is_finite(x.x) && is_finite(x.y) && is_finite(x.z) && is_finite(x.w); }
+// Four values joined from a cluster's shares whose sum is not finite: with weights that add up to one what is finite stays so.  l becomes 1.
+__device__ __noinline__ void join_again(float4& x, float& l, float m, int shares, uint32_t ml_at, uint32_t o_at) {
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < shares; ++s) {
+    const float2 ml = ld_rank2(at_rank(ml_at, s));
+    const float4 v = ld_rank4(at_rank(o_at, s));
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;
+    const float w = exp2f(ml.x - m) / l * (ml.y < 0.f ? -ml.y : 1.f);
+    y.x = fmaf(v.x, w, y.x); y.y = fmaf(v.y, w, y.y); y.z = fmaf(v.z, w, y.z); y.w = fmaf(v.w, w, y.w);
+  }
+  if (all_finite(y)) { x = y; l = 1.f; }
+}
 template <typename T>
 __device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* o, int ld, int k0, int k1) {
   const TileList& t = sm.t;
@@ -119,7 +133,7 @@ __device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* 
     for (int r = warp; r < t.nr; r += kThreads / 32) {
       if (!(sm.bad >> r & 1u)) continue;
       float m, l, x[16];
-      if (!exact_row<T>(a, t, sm.depth, query_row<T>(a, t, r), sm.pos[r], sm.row_anc[r], k0, k1, m, l, x)) continue;
+      if (!exact_row<T>(a, t, sm.depth, query_row<T>(a, t, r), sm.pos[r], sm.row_anc[r], k0, k1, m, l, x) && !(sm.still >> r & 1u)) continue;
 #pragma unroll
       for (int i = 0; i < 16; ++i) if (lane + 32 * i < d) o[r * ld + lane + 32 * i] = x[i];
       if (lane == 0) sm.ml[r] = make_float2(m, l);
@@ -145,7 +159,7 @@ __device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* 
     float l = 0.f;
     if (shares == 1) {
       x = *reinterpret_cast<const float4*>(o + r * ld + c);
-      l = sm.ml[r].y;
+      l = sm.ml[r].y < 0.f ? 1.f : sm.ml[r].y;
     } else {
       float2 ml[8];
       float4 v[8];
@@ -160,10 +174,12 @@ __device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* 
 #pragma unroll
       for (int s = 0; s < 8; ++s)
         if (s < shares && !(ml[s].x == -INFINITY && ml[s].y == 0.f)) {           // (else nothing seen)
-          const float w = exp2f(ml[s].x - m);
-          l = fmaf(ml[s].y, w, l);
+          float w = exp2f(ml[s].x - m);
+          l = fmaf(fabsf(ml[s].y), w, l);
+          if (ml[s].y < 0.f) w *= -ml[s].y;
           x.x = fmaf(v[s].x, w, x.x); x.y = fmaf(v[s].y, w, x.y); x.z = fmaf(v[s].z, w, x.z); x.w = fmaf(v[s].w, w, x.w);
         }
+      if (!all_finite(x) && l > 0.f && is_finite(l)) join_again(x, l, m, shares, ml_at + r * 8, o_at + (r * ld + c) * 4);
     }
     const float inv = 1.f / l;
     T* out = out_row<T>(a, t, r) + c;
@@ -471,7 +487,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
       m[h] = mn;
       if (warp == 0 && tc == 0) sm.c.ml[r] = make_float2(m[h], l[h]);
       const bool bad = !is_finite(l[h]) || (m[h] == -INFINITY && a.nsplit == 1);
-      if (bad && pass == 0 && r < t.nr) atomicOr(&sm.c.bad, 1u << r);
+      if (bad && r < t.nr) atomicOr(pass ? &sm.c.still : &sm.c.bad, 1u << r);
 #pragma unroll
       for (int i = 0; i < CT; ++i) *reinterpret_cast<float2*>(os + (warp * kRows + r) * DP + i * 8 + 2 * tc) = make_float2(o[i][2 * h] * part[h], o[i][2 * h + 1] * part[h]);
     }
@@ -484,7 +500,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
         x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
       }
       const int r = 4 * i / DP;
-      if (pass == 0 && r < t.nr && !(is_finite(x.x) && is_finite(x.y) && is_finite(x.z) && is_finite(x.w))) atomicOr(&sm.c.bad, 1u << r);
+      if (r < t.nr && !all_finite(x)) atomicOr(pass ? &sm.c.still : &sm.c.bad, 1u << r);
       *reinterpret_cast<float4*>(os + 4 * i) = x;
     }
   } else
@@ -499,7 +515,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
       bad |= !is_finite(o[i][2 * h]) || !is_finite(o[i][2 * h + 1]);
       *reinterpret_cast<float2*>(os + r * DP + warp * CW + i * 8 + 2 * tc) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
     }
-    if (bad && pass == 0 && r < t.nr) atomicOr(&sm.c.bad, 1u << r);
+    if (bad && r < t.nr) atomicOr(pass ? &sm.c.still : &sm.c.bad, 1u << r);
     if (warp == 0 && tc == 0) sm.c.ml[r] = make_float2(m[h], l[h]);
   }
   __syncthreads();
@@ -640,7 +656,7 @@ __global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a, c
 #pragma unroll
     for (int c = 0; c < NC; ++c) bad |= !is_finite(o[c][r]);
     if (tid == 0) sm.c.ml[r] = make_float2(sm.m[r], l);
-    if (bad && again) atomicOr(&sm.c.bad, 1u << r);
+    if (bad) atomicOr(again ? &sm.c.bad : &sm.c.still, 1u << r);
   }
   __syncthreads();
   if (!sm.c.bad || !again) {                              // (Q's place: it is not read any more)
@@ -689,24 +705,43 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a, c
     for (int h = 0; h < 2; ++h) w[h] = ml[h].x == -INFINITY && ml[h].y == 0.f ? -1.f : exp2f(ml[h].x - m);      // (-1: nothing seen)
     float l = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
-      float4 v[8];
+    // (a second time where a sum is not finite, with weights that add up to one: what is finite stays so)
+    float by = 1.f, div = 1.f;
+    float4 first = x;
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+      l = 0.f;
+      x = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
+        float4 v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (s0 + k < a.nsplit && col < d) v[k] = *reinterpret_cast<const float4*>(a.po + (base + (size_t)(s0 + k) * per) * d + col);
-      }
+        for (int k = 0; k < 8; ++k) {
+          v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (s0 + k < a.nsplit && col < d) v[k] = *reinterpret_cast<const float4*>(a.po + (base + (size_t)(s0 + k) * per) * d + col);
+        }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float ws = __shfl_sync(0xffffffffu, s0 + k < 32 ? w[0] : w[1], (s0 + k) & 31), ls = __shfl_sync(0xffffffffu, s0 + k < 32 ? ml[0].y : ml[1].y, (s0 + k) & 31);
-        if (s0 + k >= a.nsplit || ws == -1.f) continue;
-        l = fmaf(ls, ws, l);
-        x.x = fmaf(v[k].x, ws, x.x); x.y = fmaf(v[k].y, ws, x.y); x.z = fmaf(v[k].z, ws, x.z); x.w = fmaf(v[k].w, ws, x.w);
+        for (int k = 0; k < 8; ++k) {
+          float ws = __shfl_sync(0xffffffffu, s0 + k < 32 ? w[0] : w[1], (s0 + k) & 31);
+          const float ls = __shfl_sync(0xffffffffu, s0 + k < 32 ? ml[0].y : ml[1].y, (s0 + k) & 31);
+          if (s0 + k >= a.nsplit || ws == -1.f) continue;
+          ws *= by;
+          l = fmaf(fabsf(ls), ws, l);
+          if (ls < 0.f) ws *= -ls;
+          x.x = fmaf(v[k].x, ws, x.x); x.y = fmaf(v[k].y, ws, x.y); x.z = fmaf(v[k].z, ws, x.z); x.w = fmaf(v[k].w, ws, x.w);
+        }
       }
+      if (again) {
+        if (all_finite(first) || !all_finite(x)) x = first; else div = 1.f;
+        break;
+      }
+      div = l;                                            // (the same in all lanes)
+      if (!(l > 0.f && is_finite(l) && __any_sync(0xffffffffu, !all_finite(x)))) break;
+      first = x;
+      by = 1.f / l;
     }
     if (col < d) {
       T* out = out_row<T>(a, t, r) + col;
-      out[0] = from_f<T>(x.x / l); out[1] = from_f<T>(x.y / l); out[2] = from_f<T>(x.z / l); out[3] = from_f<T>(x.w / l);
+      out[0] = from_f<T>(x.x / div); out[1] = from_f<T>(x.y / div); out[2] = from_f<T>(x.z / div); out[3] = from_f<T>(x.w / div);
     }
   }
 }

@@ -97,11 +97,13 @@ __device__ __forceinline__ TileList make_list(const AttnArgs& a, int64_t item, i
 
 // The kernels multiply the values of unseen keys by an exact zero, which is not enough where a value is infinite or NaN.  So a tile with
 // a result that is not finite is computed a second time, with such values taken as zero: then what a row does not see has no
-// influence on its bits.  Rows that DO see something not finite are then computed by the definition:
+// influence on its bits.  Rows that DO see something not finite, and those whose sums are beyond the range although their result is not
+// (values near the largest, in the first sum by the weights of up to 2^10 of the tensor-core path), are then computed by the definition:
 //
 // One row, by one warp: keys k0 .. k1 - 1 of the list, what the row does not see skipped altogether.  Returns whether a score or a
-// value that it sees is not finite.  m in units of log2; o[i]: dims lane + 32 i.  (m stays -inf, l and o zero, where every score
-// seen is -inf.)
+// value that it sees is not finite.  m in units of log2; o[i]: dims lane + 32 i, with weights that add up to one, which no sum of finite
+// values leaves the range by; l: the sum of weights at the maximum m, NEGATIVE as a mark that o is divided by it.  (m stays -inf, l and o
+// zero, where every score seen is -inf.)
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
 template <typename T>
 __device__ __noinline__ bool exact_row(const AttnArgs& a, const TileList& t, const int* depth, const T* q, int p, uint32_t anc, int k0, int k1,
@@ -111,7 +113,8 @@ __device__ __noinline__ bool exact_row(const AttnArgs& a, const TileList& t, con
   bool nan = false, saw = false;
 #pragma unroll
   for (int i = 0; i < 16; ++i) o[i] = 0.f;
-  for (int pass = 0; pass < 2; ++pass)
+  float inv = 0.f;
+  for (int pass = 0; pass < 2; ++pass) {
     for (int kk = k0; kk < k1; ++kk) {
       if (!list_sees(a, t, depth, p, anc, kk)) continue;
       const int64_t code = list_row(a, t, kk);
@@ -120,9 +123,14 @@ __device__ __noinline__ bool exact_row(const AttnArgs& a, const TileList& t, con
       float x = 0.f;
       for (int e = lane; e < d; e += 32) x = fmaf(to_f(q[e]), to_f(k[e]), x);
       x = warp_sum(x) * a.scale2;
-      if (pass == 0) { nan |= isnan(x); saw |= !is_finite(x); m = fmaxf(m, x); continue; }
-      const float w = exp2f(x - m);
-      l += w;
+      if (pass == 0) {
+        nan |= isnan(x); saw |= !is_finite(x);
+        const float to = fmaxf(m, x);
+        if (to != -INFINITY) l = l * exp2f(m - to) + exp2f(x - to);
+        m = to;
+        continue;
+      }
+      const float w = exp2f(x - m) * inv;
       const T* v = row_ptr<T>(a, t.hk, code, true);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
@@ -132,12 +140,13 @@ __device__ __noinline__ bool exact_row(const AttnArgs& a, const TileList& t, con
           o[i] = fmaf(w, y, o[i]);
         }
     }
+    inv = 1.f / l;
+  }
   if (m == -INFINITY && !nan) {
-    l = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[i] = 0.f;
   }
-  if (nan) l = NAN;
+  l = nan ? NAN : -l;
   return __any_sync(0xffffffffu, saw);
 }
 // 16 bytes in shared memory, infinities and NaN taken as zero.

@@ -286,21 +286,21 @@ __device__ __noinline__ void rescale(uint32_t p_col, int words, uint32_t o_col, 
   }
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-// Columns c0 .. c1 - 1 of row r of an item (r0: in its sequence and key head) by definition, if the row sees something not finite; part:
-// the row's place among partial outputs.  By a warp.
+// Columns c0 .. c1 - 1 of row r of an item (r0: in its sequence and key head) by definition, if the row sees something not finite or is
+// `still` not finite without what it does not see; part: the row's place among partial outputs.  By a warp.
 __device__ __noinline__ void exact_output(const AttnArgs& a, const TileList& t, const int* depth, int gr, int p, uint32_t an, int k0, int k1, int c0, int c1,
-                                          size_t part) {
+                                          size_t part, bool still) {
   const int lane = threadIdx.x & 31;
   const int64_t tok = t.row0 + gr / a.G;
   const size_t head = (size_t)t.hk * a.G + gr % a.G;
   float m, l, o[16];
-  if (!exact_row<bf16>(a, t, depth, reinterpret_cast<const bf16*>(a.in.q) + tok * a.in.q_ld + head * a.s.d, p, an, k0, k1, m, l, o)) return;
+  if (!exact_row<bf16>(a, t, depth, reinterpret_cast<const bf16*>(a.in.q) + tok * a.in.q_ld + head * a.s.d, p, an, k0, k1, m, l, o) && !still) return;
   bf16* out = reinterpret_cast<bf16*>(a.out) + (tok * a.s.H + head) * a.s.d;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int col = lane + 32 * i;
     if (col < c0 || col >= c1) continue;
-    if (a.nsplit > 1) a.po[part * a.s.d + col] = o[i]; else out[col] = from_f<bf16>(o[i] / l);
+    if (a.nsplit > 1) a.po[part * a.s.d + col] = o[i]; else out[col] = from_f<bf16>(l < 0.f ? o[i] : o[i] / l);
   }
   if (a.nsplit > 1 && c0 == 0 && lane == 0) a.pml[part] = make_float2(m, l);
 }
@@ -732,10 +732,11 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
       if (mode == 2) {
         uint32_t an;
         const int p = position(w, rt + row, an);
+        const uint32_t still = __ballot_sync(FULL, C::PAIR == 2 ? bad_in_pair(odd) : odd);
         for (uint32_t todo = __ballot_sync(FULL, bad); todo; todo &= todo - 1) {
           const int x = __ffs(todo) - 1;
           exact_output(a, t, w.depth, t.r0 + r0 + x, __shfl_sync(FULL, p, x), __shfl_sync(FULL, an, x), w.k0, w.k1, col0,
-                       min(a.s.d, col0 + C::OC), part_at(w, r0 + x));
+                       min(a.s.d, col0 + C::OC), part_at(w, r0 + x), still >> x & 1u);
         }
       }
     };

@@ -1,0 +1,63 @@
+"""Token-level operators at the ends of their ranges: values near the largest of the type, lengths and rows that no sequence can have, sequences
+without tokens, other lengths under one captured call."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tok_oracle as T
+from tests.test_gpu_tokens import Layer, api, f64  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def set_history(lay, b, k, v):
+    """Other committed keys and values of sequence b, in the rows where they are visible."""
+    lay.hist_k[b], lay.hist_v[b] = k, v
+    pos = torch.tensor([p for p in range(lay.L[b]) if p < lay.shape.n_sink or p > lay.L[b] - lay.shape.window])
+    if not len(pos):
+        return
+    if lay.page:
+        at = torch.from_numpy(lay.table)[b][pos // lay.page].long() * lay.page + pos % lay.page
+    else:
+        at = torch.tensor([T.ring_row(b, int(p), lay.shape.n_sink, lay.shape.window) for p in pos])
+    lay.cache.k[at.cuda()] = k[pos].cuda()
+    if lay.cache.v is not None:
+        lay.cache.v[at.cuda()] = v[pos].cuda()
+
+
+def fill(lay, big, rise):
+    """Scores that rise with the position, by `rise` powers of two over a sequence (the first dim's product; the others' is zero), and values of
+    magnitudes from big / 2 to big, of one sign in a column."""
+    rng = np.random.default_rng(3)
+    H, Hk, d, dt = lay.shape.H, lay.shape.Hk, lay.shape.d, lay.shape.torch_dtype
+    lay.q.zero_()
+    lay.q[:, :, 0] = 1.0
+    for b in range(lay.B):
+        total = lay.L[b] + lay.n[b]
+        v = rng.uniform(0.5, 1.0, (total, Hk, d)) * big * np.where(np.arange(d) % 2, -1.0, 1.0)
+        k = v.copy() if lay.v is None else rng.standard_normal((total, Hk, d))
+        k[:, :, 0] = (np.arange(total) * (rise * np.log(2.0) / max(1, total - 1)))[:, None]
+        k = torch.from_numpy(k).float().to(dt)
+        v = k if lay.v is None else torch.from_numpy(v).float().to(dt)
+        r = slice(lay.row0[b], lay.row0[b] + lay.n[b])
+        lay.k[r] = k[lay.L[b]:].cuda()
+        if lay.v is not None:
+            lay.v[r] = v[lay.L[b]:].cuda()
+        set_history(lay, b, k[:lay.L[b]], v[:lay.L[b]])
+
+
+# every kernel: tiles of 128 rows of each width, with shares joined afterwards and without; tiles of 16 rows, shares joined in a cluster and afterwards;
+# fp32.  Sums over the keys go beyond what fp32 holds: 700 keys, weights of up to 2^9 beside the first block's, of 1e36; or equal weights of 3e38
+@pytest.mark.parametrize("big,rise", [(1e36, 9.5), (3e38, 0.0), (3e38, 3.0)])
+@pytest.mark.parametrize("heads,L,n", [
+    (("bf16", 2, 1, 64, False), [0, 40], [250, 20]), (("bf16", 4, 2, 128, True), [300], [40]), (("bf16", 2, 1, 256, False), [500], [20]),
+    (("bf16", 2, 1, 200, True), [0], [140]), (("bf16", 2, 1, 512, True), [430], [70]), (("bf16", 2, 1, 512, False), [300], [20]),
+    (("bf16", 20, 1, 128, False), [9000], [1]), (("bf16", 2, 1, 512, True), [17000], [1]), (("bf16", 2, 1, 256, False), [17000], [1]),
+    (("bf16", 2, 1, 64, False), [700], [1]), (("bf16", 2, 1, 128, True), [90, 3], [1, 2]), (("bf16", 2, 1, 128, False), [9000], [1]),
+    (("bf16", 2, 1, 256, False), [700], [1]), (("bf16", 2, 1, 512, True), [1200], [3]), (("bf16", 2, 1, 512, False), [9000], [1]),
+    (("fp32", 2, 1, 64, False), [700], [30]), (("fp32", 2, 1, 264, True), [700], [1]), (("fp32", 2, 1, 512, False), [9000], [1])], ids=str)
+def test_sums_beyond_the_range(api, heads, L, n, big, rise):
+    _, tk, _ = api
+    lay = Layer(tk, *heads, window=20000, sinks=4, L=L, n=n, page=64, seed=len(L), scale=1.0)
+    fill(lay, big, rise)
+    lay.check(lay.run(tk))
