@@ -9,6 +9,8 @@
 // owns a head, and a lane the SAME dims of every head its warp walks over, both members of each pair among them: weights and
 // angles stay in registers (their products), the rotation needs no exchange, and the only reduction is the sum of squares over the group.
 // Arithmetic goes two values at a time (fma.rn.f32x2): with one the instructions took as long as the bytes.
+#include <type_traits>
+
 #include "tok_common.cuh"
 
 namespace tsv {
@@ -63,6 +65,17 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
+}
+
+// Means of squares beyond these (squares that fp32 does not hold, or as zero) are taken again of the vector times a power of two that brings
+// its largest value, or the square root of eps, to 1 .. 4: the norm does not depend on it.  (0, an infinity and NaN stay as they are.)
+__device__ __forceinline__ bool in_range(float mean) {      // 2^-100 .. 2^120, in one comparison
+  return (uint32_t)(__float_as_int(mean) - (27 << 23)) < 220u << 23;
+}
+__device__ __forceinline__ float scale_of(float x) {
+  if (!(x > 0.f && x < INFINITY)) return 1.f;
+  const int e = (__float_as_int(x) >> 23) - 127;
+  return __int_as_float((127 - min(max(e, -126), 126)) << 23);
 }
 
 // A unit: two 16-byte vectors of a head, their members as pairs (a, b) two at a time.  PAIRS: neighbours; else member i of one vector and of
@@ -222,45 +235,77 @@ __global__ void __launch_bounds__(kRopeThreads, UPL == 1 ? 2 : 1) rope_kernel(co
           bc[p][i] = pair2(wb[0] * c[0].x, wb[1] * c[1].x); bs[p][i] = pair2(-wb[0] * c[0].y, -wb[1] * c[1].y);
         }
       }
+      bool later = false;
+      auto walk = [&](auto slow) {
+        constexpr bool SLOW = decltype(slow)::value;
 #pragma unroll 1
-      for (int h0 = first; h0 < heads; h0 += AHEAD * step) {
-        if (!(early && which == 0 && h0 == first)) fetch(in, h0, heads);
+        for (int h0 = first; h0 < heads; h0 += AHEAD * step) {
+          if (SLOW || !(early && which == 0 && h0 == first)) fetch(in, h0, heads);
 #pragma unroll
-        for (int e = 0; e < AHEAD; ++e) {
-          const int head = h0 + e * step + gi;
-          uint64_t xa[UPL][NP], xb[UPL][NP], s2 = 0, s3 = 0;
+          for (int e = 0; e < AHEAD; ++e) {
+            const int head = h0 + e * step + gi;
+            uint64_t xa[UPL][NP], xb[UPL][NP], s2 = 0, s3 = 0;
 #pragma unroll
-          for (int p = 0; p < UPL; ++p) {
-            Unit<T, PAIRS>::split(raw[e][p], xa[p], xb[p]);
+            for (int p = 0; p < UPL; ++p) {
+              Unit<T, PAIRS>::split(raw[e][p], xa[p], xb[p]);
 #pragma unroll
-            for (int i = 0; i < NP; ++i) { s2 = fma2(xa[p][i], xa[p][i], s2); s3 = fma2(xb[p][i], xb[p][i], s3); }
-          }
-          const float2 sa = unpair(s2), sb = unpair(s3);
-          float ss = (sa.x + sa.y) + (sb.x + sb.y);
-          for (int o = a.group >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const float r = ok == 1 ? rsqrtf(fmaf(ss, inv_d, a.eps)) : 0.f;      // (2 units in the last place)
-          const uint64_t r2 = pair2(r, r);
-#pragma unroll
-          for (int p = 0; p < UPL; ++p) {
-            uint64_t ya[NP], yb[NP];
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-              if (turn[p][PAIRS ? i / (NP / 2) : 0]) {
-                ya[i] = mul2(fma2(xa[p][i], ac[p][i], mul2(xb[p][i], bs[p][i])), r2);
-                yb[i] = mul2(fma2(xa[p][i], as[p][i], mul2(xb[p][i], bc[p][i])), r2);
-              } else {
-                ya[i] = mul2(mul2(xa[p][i], ac[p][i]), r2);
-                yb[i] = mul2(mul2(xb[p][i], bc[p][i]), r2);
-              }
+              for (int i = 0; i < NP; ++i) { s2 = fma2(xa[p][i], xa[p][i], s2); s3 = fma2(xb[p][i], xb[p][i], s3); }
             }
-            uint4 v[2];
-            Unit<T, PAIRS>::join(ya, yb, v);
+            const float2 sa = unpair(s2), sb = unpair(s3);
+            float ss = (sa.x + sa.y) + (sb.x + sb.y);
+            for (int o = a.group >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            float mean = fmaf(ss, inv_d, a.eps);
+            const bool far = !in_range(mean);
+            later |= far;
+            if (SLOW) {
+              float mx = 0.f, s1 = 0.f;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (head < heads && vec[p][h] >= 0) *reinterpret_cast<uint4*>(out + (size_t)head * s.d + vec[p][h] * VE) = v[h];
+              for (int p = 0; p < UPL; ++p)
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                  const float2 u = unpair(xa[p][i]), v = unpair(xb[p][i]);
+                  mx = fmaxf(fmaxf(mx, fmaxf(fabsf(u.x), fabsf(u.y))), fmaxf(fabsf(v.x), fabsf(v.y)));
+                }
+              for (int o = a.group >> 1; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+              const float by = scale_of(fmaxf(mx, sqrtf(a.eps)));
+              const uint64_t by2 = pair2(by, by);
+#pragma unroll
+              for (int p = 0; p < UPL; ++p)
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                  xa[p][i] = mul2(xa[p][i], by2); xb[p][i] = mul2(xb[p][i], by2);
+                  const float2 u = unpair(xa[p][i]), v = unpair(xb[p][i]);
+                  s1 = fmaf(u.x, u.x, fmaf(u.y, u.y, fmaf(v.x, v.x, fmaf(v.y, v.y, s1))));
+                }
+              for (int o = a.group >> 1; o; o >>= 1) s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+              mean = fmaf(s1, inv_d, a.eps * by * by);
+            }
+            const float r = ok == 1 ? rsqrtf(mean) : 0.f;    // (2 units in the last place)
+            const uint64_t r2 = pair2(r, r);
+#pragma unroll
+            for (int p = 0; p < UPL; ++p) {
+              uint64_t ya[NP], yb[NP];
+#pragma unroll
+              for (int i = 0; i < NP; ++i) {
+                if (turn[p][PAIRS ? i / (NP / 2) : 0]) {
+                  ya[i] = mul2(fma2(xa[p][i], ac[p][i], mul2(xb[p][i], bs[p][i])), r2);
+                  yb[i] = mul2(fma2(xa[p][i], as[p][i], mul2(xb[p][i], bc[p][i])), r2);
+                } else {
+                  ya[i] = mul2(mul2(xa[p][i], ac[p][i]), r2);
+                  yb[i] = mul2(mul2(xb[p][i], bc[p][i]), r2);
+                }
+              }
+              uint4 v[2];
+              Unit<T, PAIRS>::join(ya, yb, v);
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                if (head < heads && vec[p][h] >= 0 && far == SLOW) *reinterpret_cast<uint4*>(out + (size_t)head * s.d + vec[p][h] * VE) = v[h];
+            }
           }
         }
-      }
+      };
+      walk(std::false_type());
+      if (__any_sync(0xffffffffu, later)) walk(std::true_type());      // (nearly never; the others' places may be their inputs')
     }
   }
 }

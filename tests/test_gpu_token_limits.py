@@ -61,3 +61,26 @@ def test_sums_beyond_the_range(api, heads, L, n, big, rise):
     lay = Layer(tk, *heads, window=20000, sinks=4, L=L, n=n, page=64, seed=len(L), scale=1.0)
     fill(lay, big, rise)
     lay.check(lay.run(tk))
+
+
+@pytest.mark.parametrize("dtype,d,rot,pairs", [("bf16", 128, 64, True), ("bf16", 72, 32, False), ("fp32", 64, 64, False), ("fp32", 512, 16, True)])
+def test_norms_of_vectors_at_the_ends_of_the_range(api, dtype, d, rot, pairs):
+    """Vectors whose squares fp32 does not hold, or holds as zero, beside ordinary ones, in one call; eps zero, so that it does not count."""
+    _, tk, _ = api
+    lay = Layer(tk, dtype, 3, 1, d, True, window=1, sinks=0, L=[0, 0], n=[9, 40], seed=d)
+    scales = [1.0, 1e30, 3e37, 1e-30, 1e18, 1e-24, 1e-37, 1.0, 1e20]
+    for b in range(2):
+        for i in range(lay.n[b]):
+            lay.q[lay.row0[b] + i] *= scales[i % 9]
+            lay.k[lay.row0[b] + i] *= scales[(i + 4) % 9]
+    w = torch.from_numpy(np.random.default_rng(d).uniform(0.5, 1.5, d).astype(np.float32)).cuda()
+    inv = torch.from_numpy((10000.0 ** (-np.arange(rot // 2) * 2 / rot)).astype(np.float32)).cuda()
+    qo, ko = torch.zeros_like(lay.q), torch.zeros_like(lay.k)
+    first = 8 if d > rot else 0
+    tk.qk_norm_rope(lay.shape, lay.cache.L, lay.batch, lay.q, lay.k, qo, ko, w, w, 0.0, inv, first, pairs, lay.status)
+    for b in range(2):
+        r = slice(lay.row0[b], lay.row0[b] + lay.n[b])
+        for got, x in ((qo, lay.q), (ko, lay.k)):
+            ref, mag = T.norm_rope(f64(x[r]), f64(w), 0.0, range(lay.n[b]), f64(inv), first, pairs)
+            tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref) + mag * (d * 2.0 ** -24 + 2.0 ** -20) + 1e-30
+            assert (np.abs(f64(got[r]) - ref) <= tol).all()
