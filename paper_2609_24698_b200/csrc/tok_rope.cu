@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kRopeThreads, UPL == 1 ? 2 : 1) rope_kernel(co
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < VE; ++e) wt[h][e] = w && vec[p][h] >= 0 ? __ldg(w + vec[p][h] * VE + e) : 1.f;
+          for (int e = 0; e < VE; ++e) wt[h][e] = w && ok == 1 && vec[p][h] >= 0 ? __ldg(w + vec[p][h] * VE + e) : 1.f;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
           float wa[2], wb[2];

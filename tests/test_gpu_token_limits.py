@@ -84,3 +84,16 @@ def test_norms_of_vectors_at_the_ends_of_the_range(api, dtype, d, rot, pairs):
             ref, mag = T.norm_rope(f64(x[r]), f64(w), 0.0, range(lay.n[b]), f64(inv), first, pairs)
             tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref) + mag * (d * 2.0 ** -24 + 2.0 ** -20) + 1e-30
             assert (np.abs(f64(got[r]) - ref) <= tol).all()
+
+
+def test_a_flagged_sequence_has_zeros_whatever_the_weights(api):
+    _, tk, _ = api
+    for bad in (float("nan"), float("inf")):
+        lay = Layer(tk, "bf16", 4, 2, 64, True, window=1, sinks=0, L=[0, 0], n=[5, 3], seed=1)
+        lay.cache.L[0] = -1
+        w = torch.full((64,), bad, device="cuda")
+        inv = (10000.0 ** -torch.arange(0, 1, 2 / 32, device="cuda")).float()
+        qo, ko = torch.full_like(lay.q, 3.0), torch.full_like(lay.k, 3.0)
+        tk.qk_norm_rope(lay.shape, lay.cache.L, lay.batch, lay.q, lay.k, qo, ko, w, w, 1e-6, inv, 16, False, lay.status)
+        r = slice(lay.row0[0], lay.row0[0] + 5)
+        assert lay.status.tolist() == [api[0].ST_LENGTH, 0] and (qo[r] == 0).all() and (ko[r] == 0).all()
