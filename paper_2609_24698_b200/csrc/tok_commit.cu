@@ -180,9 +180,11 @@ __global__ void __launch_bounds__(kCommitThreads) commit_wide_kernel(const Commi
 __global__ void commit_lengths_kernel(const CommitArgs a) {
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b >= a.s.B || a.status[b]) return;
-  const int n = __ldg(a.bt.n + b), cnt = a.count ? __ldg(a.count + b) : n;
-  if (n == 0 && cnt != 0) atomicOr(a.status + b, TSV_ST_NODES);       // (no CTA has looked at a sequence without tokens)
-  else a.c.L[b] += cnt;
+  const int n = __ldg(a.bt.n + b), cnt = a.count ? __ldg(a.count + b) : n, L = a.c.L[b];
+  int st = 0;
+  if (n == 0) st = (cnt != 0 ? TSV_ST_NODES : 0) | (L < 0 || L > a.s.max_L ? TSV_ST_LENGTH : 0);      // (no CTA has looked at a sequence without tokens)
+  if (st) atomicOr(a.status + b, st);
+  else a.c.L[b] = L + cnt;
 }
 
 }  // namespace

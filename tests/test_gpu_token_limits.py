@@ -97,3 +97,16 @@ def test_a_flagged_sequence_has_zeros_whatever_the_weights(api):
         tk.qk_norm_rope(lay.shape, lay.cache.L, lay.batch, lay.q, lay.k, qo, ko, w, w, 1e-6, inv, 16, False, lay.status)
         r = slice(lay.row0[0], lay.row0[0] + 5)
         assert lay.status.tolist() == [api[0].ST_LENGTH, 0] and (qo[r] == 0).all() and (ko[r] == 0).all()
+
+
+@pytest.mark.parametrize("max_n", [8, 64, 65, 300])
+@pytest.mark.parametrize("page", [0, 16])
+def test_commit_flags_lengths_of_sequences_without_tokens(api, max_n, page):
+    """A length that no sequence can have is flagged whether or not there are tokens to commit, and whatever the shape's bounds."""
+    tsv, tk, _ = api
+    lay = Layer(tk, "bf16", 2, 2, 64, False, window=10, sinks=1, L=[4, 9, 2, 5, 0], n=[3, 0, 0, 0, 2], page=page, seed=2, extra_n=max_n - 3)
+    assert lay.shape.max_n == max_n
+    lay.cache.L[1], lay.cache.L[2] = -1, lay.shape.max_L + 1
+    tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, lay.status)
+    assert lay.status.tolist() == [0, tsv.ST_LENGTH, tsv.ST_LENGTH, 0, 0]
+    assert lay.cache.L.tolist() == [7, -1, lay.shape.max_L + 1, 5, 2]
