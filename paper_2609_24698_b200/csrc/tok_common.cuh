@@ -15,7 +15,7 @@ struct TokUnit {
 __device__ __forceinline__ int tok_count(const tsv_tok_shape& s, const tsv_tok_batch& bt, int b, int32_t* status, int64_t& row0) {
   const int n = __ldg(bt.n + b);
   row0 = __ldg(bt.row0 + b);
-  if (n < 0 || n > s.max_n || row0 < 0 || row0 + n > bt.rows) {
+  if (n < 0 || n > s.max_n || row0 < 0 || row0 > bt.rows - n) {     // (row0 + n may pass 64 bits)
     if (status) atomicOr(status + b, TSV_ST_NODES);
     return -1;
   }

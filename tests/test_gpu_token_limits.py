@@ -110,3 +110,24 @@ def test_commit_flags_lengths_of_sequences_without_tokens(api, max_n, page):
     tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, lay.status)
     assert lay.status.tolist() == [0, tsv.ST_LENGTH, tsv.ST_LENGTH, 0, 0]
     assert lay.cache.L.tolist() == [7, -1, lay.shape.max_L + 1, 5, 2]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [[3, 4], [40, 90]])
+def test_first_rows_at_the_ends_of_64_bits(api, dtype, n):
+    """row0[b] + n[b] passes 64 bits: outside the packed arrays like any other such row, in every call."""
+    tsv, tk, _ = api
+    for row0 in (2 ** 63 - 1, 2 ** 63 - n[0], 2 ** 63 - n[0] - 1, -2 ** 63):
+        lay = Layer(tk, dtype, 4, 2, 64, False, window=20, sinks=2, L=[30, 8], n=n, page=4, seed=3, extra_n=5)
+        was = lay.row0[0]
+        good, q = lay.run(tk).clone(), torch.full_like(lay.q, 3.0)
+        lay.batch.row0[0] = row0
+        mine = slice(lay.row0[1], lay.row0[1] + n[1])
+        out = lay.run(tk)
+        assert lay.status.tolist() == [tsv.ST_NODES, 0] and torch.equal(out[mine], good[mine]) and (out[was:was + n[0]] == 3.0).all()
+        st = torch.zeros_like(lay.status)
+        tk.qk_norm_rope(lay.shape, lay.cache.L, lay.batch, lay.q, None, q, None, None, None, 1e-6, None, 0, False, st)
+        assert st.tolist() == [tsv.ST_NODES, 0] and (q[was:was + n[0]] == 3.0).all() and not (q[mine] == 3.0).any()
+        st.zero_()
+        tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, st)
+        assert st.tolist() == [tsv.ST_NODES, 0] and lay.cache.L.tolist() == [30, 8 + n[1]]
