@@ -12,6 +12,12 @@ namespace tsv {
 static std::atomic<uint64_t> g_launches{0};
 void count_launch(int n) { g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
 
+static std::atomic<int64_t> g_tries{-1};
+uint32_t wait_tries(uint32_t usual) {
+  const int64_t t = g_tries.load(std::memory_order_relaxed);
+  return t < 0 ? usual : (uint32_t)t;
+}
+
 bool ensure_smem(const void* kernel, int bytes) {
   struct Entry { std::atomic<const void*> kernel{nullptr}; std::atomic<int> dev{-1}, bytes{0}; };
   static Entry table[256];                              // (kernel, device) pairs, filled from the front
@@ -195,6 +201,10 @@ using namespace tsv;
 extern "C" {
 
 int tsv_version(void) { return 1000; }
+
+// For tests (not in the header): the waits of the token-level and page kernels give up after this many tries in launches from now on, negative: after
+// their usual number.
+void tsv_test_wait_tries(int64_t tries) { g_tries.store(tries < 0 ? -1 : tries > 0xffffffffll ? 0xffffffffll : tries, std::memory_order_relaxed); }
 
 uint64_t tsv_kernel_launches(void) { return g_launches.load(std::memory_order_relaxed); }
 

@@ -276,6 +276,7 @@ struct CopyArgs {
   int32_t renumber;                 // the table's words become the new numbers (compact)
   int32_t* failed;                  // where a copy that never came is told of
   int32_t n_failed;
+  uint32_t tries;                   // of a wait for a copy
 };
 
 // Thread 0 moves the planes' chunks: a load into the next stage once the store out of it has been read, a store three chunks behind the
@@ -298,10 +299,10 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
     int loaded = 0, stored = 0;                            // chunks so far
     bool fail = false;
     // one round of the stages, unrolled: what a stage is for stays in registers
-    while (item < items || stored < loaded) {
+    while (!fail && (item < items || stored < loaded)) {
 #pragma unroll
       for (int st = 0; st < kStages; ++st) {
-        if (item < items && loaded - stored <= kStoreLag && loaded % kStages == st) {
+        if (!fail && item < items && loaded - stored <= kStoreLag && loaded % kStages == st) {
           const int i = (int)(item / per_plane), c = (int)(item - (int64_t)i * per_plane);
           int lo = 0, hi = planes;                         // the plane of this chunk
           while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (a.chunk0[mid] <= c) lo = mid; else hi = mid; }
@@ -316,17 +317,22 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
           ++loaded;
         }
         const int sst = (st + kStages - kStoreLag) % kStages;      // (the store that is due behind this load)
-        if (stored < loaded && stored % kStages == sst && (loaded - stored > kStoreLag || item >= items)) {
-          if (!fail && !bulk_bar_wait(bar + 8 * sst, (stored / kStages) & 1)) fail = true;
-          if (size[sst] && !fail) bulk_store(to[sst], at + sst * kChunk, size[sst]);
-          bulk_commit();
-          ++stored;
+        if (!fail && stored < loaded && stored % kStages == sst && (loaded - stored > kStoreLag || item >= items)) {
+          fail = !bulk_bar_wait(bar + 8 * sst, (stored / kStages) & 1, a.tries);
+          if (!fail) {
+            if (size[sst]) bulk_store(to[sst], at + sst * kChunk, size[sst]);
+            bulk_commit();
+            ++stored;
+          }
         }
       }
     }
     bulk_wait();
-    if (fail)                                              // (an internal error)
+    if (fail) {                                            // (an internal error)
       for (int i = 0; i < a.n_failed; ++i) { if (a.compact) a.failed[i] = -1; else atomicOr(a.failed + i, TSV_ST_INTERNAL); }
+      // (no load is under way into shared memory when this CTA gives it up)
+      for (; stored < loaded; ++stored) bulk_bar_wait(bar + 8 * (stored % kStages), (stored / kStages) & 1, kBulkTries);
+    }
   } else if (tid >= 32) {
     const int t = tid - 32, n = kCopyThreads - 32;
     const int64_t items = (int64_t)pairs * per_row;
@@ -370,6 +376,7 @@ int launch_copies(const tsv_page_pool& p, const Work& w, bool rows, int64_t most
     a.compact = renumber;
     a.renumber = renumber && at == 0;
     a.failed = failed; a.n_failed = n_failed;
+    a.tries = wait_tries(kBulkTries);
     int64_t chunks = 0;
     for (int i = 0; i < a.n; ++i) {
       const tsv_page_array& x = at + i < p.n_planes ? p.planes[at + i] : p.rows[at + i - p.n_planes];

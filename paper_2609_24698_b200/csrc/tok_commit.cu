@@ -20,6 +20,7 @@ struct CommitArgs {
   const int32_t *path, *count;
   int32_t path_ld, row_vecs;             // 16-byte vectors of a row
   int32_t unit_rows;                     // rows of a CTA where several share a sequence
+  uint32_t tries;                        // of a wait for copies
   int32_t* status;
 };
 
@@ -154,8 +155,12 @@ __global__ void __launch_bounds__(kCommitThreads) commit_rows_kernel(const Commi
   __syncthreads();
   if (src) bulk_load(at + tid * bytes, src, bytes, bar_at);
   if (src) {
-    if (bulk_bar_wait(bar_at, 0)) bulk_store(dst, at + tid * bytes, bytes);
-    else atomicOr(a.status + u.b, TSV_ST_INTERNAL);
+    if (bulk_bar_wait(bar_at, 0, a.tries)) {
+      bulk_store(dst, at + tid * bytes, bytes);
+    } else {
+      atomicOr(a.status + u.b, TSV_ST_INTERNAL);
+      bulk_bar_wait(bar_at, 0, kBulkTries);               // (no copy is under way into shared memory when this CTA gives it up)
+    }
     bulk_commit();
     bulk_wait();
   }
@@ -192,7 +197,7 @@ __global__ void commit_lengths_kernel(const CommitArgs a) {
 int launch_token_commit(const tsv_tok_shape& s, const tsv_tok_cache& c, const tsv_tok_batch& bt, const tsv_tok_rows& in, const int32_t* path, int path_ld,
                         const int32_t* count, int32_t* status, cudaStream_t st) {
   const int es = s.dtype == TSV_BF16 ? 2 : 4;
-  CommitArgs a = {s, c, bt, in.k, in.v, in.k_ld * es, in.v_ld * es, path, count, path_ld, s.Hk * s.d * es / 16, 0, status};
+  CommitArgs a = {s, c, bt, in.k, in.v, in.k_ld * es, in.v_ld * es, path, count, path_ld, s.Hk * s.d * es / 16, 0, wait_tries(kBulkTries), status};
   if (s.max_n <= 64) {
     TSV_PREP(commit_seq_kernel);
     commit_seq_kernel<<<s.B, kCommitThreads, 0, st>>>(a);

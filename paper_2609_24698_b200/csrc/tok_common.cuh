@@ -119,9 +119,10 @@ __device__ __forceinline__ void bulk_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void bulk_bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-__device__ __forceinline__ bool bulk_bar_wait(uint32_t bar, uint32_t parity) {     // gives up after 2^14 tries of up to 4 us
+constexpr uint32_t kBulkTries = 1u << 14;      // of up to 4 us
+__device__ __forceinline__ bool bulk_bar_wait(uint32_t bar, uint32_t parity, uint32_t tries) {
 #pragma unroll 1
-  for (uint32_t it = 0; it < 1u << 14; ++it) {
+  for (uint32_t it = 0; it < tries; ++it) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(bar), "r"(parity), "r"(4000u) : "memory");

@@ -131,3 +131,60 @@ def test_first_rows_at_the_ends_of_64_bits(api, dtype, n):
         st.zero_()
         tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, st)
         assert st.tolist() == [tsv.ST_NODES, 0] and lay.cache.L.tolist() == [30, 8 + n[1]]
+
+
+@pytest.fixture
+def tries(api):
+    """Sets how often the waits inside the kernels try before they give up, for the launches of one test."""
+    import ctypes as C
+    f = api[0]._lib.tsv_test_wait_tries
+    f.argtypes, f.restype = [C.c_int64], None
+    yield f
+    torch.cuda.synchronize()
+    f(-1)
+
+
+@pytest.mark.parametrize("n", [[70, 0, 300], [4000, 3, 65]])
+def test_commit_whose_copies_do_not_come(api, tries, n):
+    """Waits that give up at once: the sequences are flagged and keep their lengths, the next call does everything."""
+    tsv, tk, _ = api
+    lay = Layer(tk, "bf16", 2, 2, 128, False, window=20, sinks=1, L=[3, 9, 5], n=n, page=16, seed=1)
+    tries(0)
+    tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, lay.status)
+    assert lay.status.tolist() == [tsv.ST_INTERNAL if k else 0 for k in n] and lay.cache.L.tolist() == [3, 9, 5]
+    tries(-1)
+    lay.status.zero_()
+    tk.token_commit(lay.shape, lay.cache, lay.batch, lay.k, lay.v, lay.status)
+    assert not lay.status.any() and lay.cache.L.tolist() == [3 + n[0], 9 + n[1], 5 + n[2]]
+    for b in range(3):
+        pos = np.arange(lay.L[b], lay.L[b] + n[b])
+        at = torch.from_numpy(lay.table[b][pos // 16].astype(np.int64) * 16 + pos % 16).cuda()
+        assert torch.equal(lay.cache.k[at], lay.k[lay.row0[b]:lay.row0[b] + n[b]]) and torch.equal(lay.cache.v[at], lay.v[lay.row0[b]:lay.row0[b] + n[b]])
+
+
+@pytest.mark.parametrize("words", [8, 5000, 300000])
+def test_page_copies_that_do_not_come(api, tries, words):
+    """A fork and a compaction whose waits give up at once tell so, and the next call on the same pool works."""
+    tsv, _, pg = api
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    plane = torch.arange(40, dtype=torch.int32, device="cuda")[:, None].expand(40, words).contiguous()
+    L = i32(10, 0, 0, 9, 0)
+    pool = pg.PagePool(torch.full((5, 4), -1, dtype=torch.int32, device="cuda"), torch.zeros(40, dtype=torch.int32, device="cuda"), 4, [plane], [L])
+    ws, st, used = pg.alloc_workspace(pool), i32(0, 0), i32(7)
+    pool.page_table[0, :3], pool.page_table[3, :3] = i32(30, 31, 32), i32(33, 34, 35)
+    pool.ref[30:36] = 1
+    tries(0)
+    pg.pages_fork(pool, i32(0, 3), i32(1, 2), L, ws, st)
+    assert st.tolist() == [tsv.ST_INTERNAL] * 2
+    tries(-1)
+    st.zero_()
+    pg.pages_free(pool, i32(1, 2), i32(0, 0), i32(4, 4), st)
+    pg.pages_fork(pool, i32(0, 3), i32(1, 2), L, ws, st)
+    assert not st.any() and pool.page_table[1].tolist() == [30, 31, 0, -1] and pool.page_table[2].tolist() == [33, 34, 1, -1]
+    assert (plane[0] == 32).all() and (plane[1] == 35).all()
+    tries(0)
+    pg.pages_compact(pool, used, ws)
+    assert used.tolist() == [-1]
+    tries(-1)
+    pg.pages_compact(pool, used, ws)                      # (nothing left to move)
+    assert used.tolist() == [8]
