@@ -55,7 +55,10 @@ constexpr int kItems = 3;             // items found ahead
 constexpr float kGap = 10.f;          // log2 units by which a maximum may exceed the row's reference
 constexpr int kCtl = 3 * 1024;            // bytes in front of the panels (a multiple of 1024)
 // Polls of up to 4 us before a wait gives up: a role may wait for a whole item, and that may be millions of keys, or rows computed one by one.
+// A warp whose wait has given up starts nothing more that runs by itself (copies, products, words for the other CTA), takes no item and gives
+// none out, and goes to the end, where what is under way is waited for before the memory is given up.
 constexpr uint32_t kWaitLimit = WAIT_LIMIT << 8;
+constexpr uint32_t kDrain = WAIT_LIMIT;     // those at the end
 
 template <int N> struct Int { static constexpr int value = N; };
 
@@ -97,9 +100,11 @@ struct TcCtl {
   uint64_t stat_full, stat_free;              // one tile: reference and sum of its rows, for the epilogue
   uint64_t x_full[4], x_free[4];              // a warp's rows of the other CTA's part of S: there; taken there, of this one's
   uint64_t bad_full[2][4];                    // the other CTA's word of `bad`, by turns
+  uint64_t drained[2];                        // at the end: all products are done
   uint32_t bad[2][4];                         // rows with a result that is not finite there, a bit each
   uint64_t item_full[kItems], item_free[kItems];
   uint32_t tmem_base;
+  uint32_t failed;                            // a pair: a wait has given up in one of the CTAs
   uint32_t redo[32];                  // items with a result that is not finite, a bit each
   float2 stat[kTile];
   Item item[kItems];
@@ -115,9 +120,9 @@ __device__ __forceinline__ void bar_arrive(uint64_t* b) {
 // A first look in line, then tries to the limit in a function: a wait is in the code of some thirty places.  A test is back sooner than a try
 // that may suspend, a try leaves the other warps more; pairs of CTAs, whose softmax hardly ever finds a phase incomplete, take the test
 // (prompts of 64 heads x 512: 672 against 691 us; 32 heads x 128 the other way about, 565 and 540).
-__device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
+__device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity, uint32_t tries) {
 #pragma unroll 1
-  for (uint32_t it = 0; it < kWaitLimit; ++it) {
+  for (uint32_t it = 0; it < tries; ++it) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
@@ -126,7 +131,7 @@ __device__ __noinline__ bool bar_wait_on(uint32_t addr, uint32_t parity) {
   return false;
 }
 template <bool TEST>
-__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, uint32_t tries) {
   const uint32_t addr = smem_u32(bar);
   uint32_t ok;
   if (TEST)
@@ -134,13 +139,13 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
   else
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
-  return ok || bar_wait_on(addr, parity);
+  return ok || bar_wait_on(addr, parity, tries);
 }
 // The same for what the other CTA of a pair sends.
-__device__ __noinline__ bool bar_wait_pair(uint64_t* bar, uint32_t parity) {
+__device__ __noinline__ bool bar_wait_pair(uint64_t* bar, uint32_t parity, uint32_t tries) {
   const uint32_t addr = smem_u32(bar);
 #pragma unroll 1
-  for (uint32_t it = 0; it < kWaitLimit; ++it) {
+  for (uint32_t it = 0; it < tries; ++it) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(addr), "r"(parity), "r"(SUSPEND_NS) : "memory");
@@ -245,6 +250,7 @@ struct TcArgs {
   AttnArgs a;
   int32_t items;
   int32_t q_box;                // the queries come by it
+  uint32_t tries;               // of a wait
 };
 __device__ __forceinline__ void tma_box3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -316,15 +322,17 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
   const uint32_t q_at = base, k_at = q_at + C::QB * C::NP * kPanel, v_at = k_at + C::NKB * C::NP * C::PB, x_at = v_at + C::NVB * C::NP * C::PB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = C::PAIR == 2 ? (int)(blockIdx.x & 1) : 0, col0 = rank * C::OC;      // its columns: from col0 on
+  constexpr uint32_t FULL = 0xffffffffu;
   int fail = (smem_u32(smem_raw) & 1023u) ? 1 : 0;             // (swizzled panels need a 1024-byte aligned base)
   if (tid == 0) {
     for (int i = 0; i < kItems; ++i) { bar_init(&sm.item_full[i], 1); bar_init(&sm.item_free[i], kWarps - 1); }
     for (int i = 0; i < 4; ++i) { bar_init(&sm.fullV[i], 32 * C::TEAM); bar_init(&sm.fullK[i], 32 * C::TEAM); bar_init(&sm.emptyK[i], 1); bar_init(&sm.emptyV[i], 1); bar_init(&sm.s_full[i], 1); bar_init(&sm.p_ready[i], kTile); bar_init(&sm.s_free[i], 1); bar_init(&sm.x_full[i], 1); bar_init(&sm.x_free[i], 1); bar_init(&sm.bad_full[0][i], 1); bar_init(&sm.bad_full[1][i], 1); }
-    for (int i = 0; i < 2; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.emptyQ[i], 1); bar_init(&sm.o_full[i], 1); bar_init(&sm.o_free[i], kTile); }
+    for (int i = 0; i < 2; ++i) { bar_init(&sm.fullQ[i], g.q_box ? 1 : 32); bar_init(&sm.emptyQ[i], 1); bar_init(&sm.o_full[i], 1); bar_init(&sm.o_free[i], kTile); bar_init(&sm.drained[i], 1); }
     bar_init(&sm.stat_full, kTile); bar_init(&sm.stat_free, kTile);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid < 32) sm.redo[tid] = 0;
+  if (tid == 32) sm.failed = 0;
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem_base)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -335,7 +343,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
   fence_after();
   const uint32_t tm = sm.tmem_base, s_col = tm, o_col = tm + 2 * kTile;
 
-  auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait<C::PAIR == 2>(b, parity)) fail = 1; };
+  auto wait = [&](uint64_t* b, uint32_t parity) { if (!fail && !bar_wait<C::PAIR == 2>(b, parity, g.tries)) fail = 1; };
   // After the first round: whether there is a second (alike in all threads of a CTA or a pair).
   auto marks = [&](int i) {
     uint32_t m = sm.redo[i & 31];
@@ -388,10 +396,11 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
         for (int mode = round; more && mode <= 2 * round; ++mode, ++c) {
           wait(&sm.item_free[c % kItems], (c / kItems & 1) ^ 1);
           fail = __any_sync(0xffffffffu, fail);
+          if (fail) { more = false; break; }               // (the others may still be at the item in that place)
           Item& w = sm.item[c % kItems];
           TileList t;
           t.ok = 0;
-          if (idx < g.items && !fail) t = make_list(a, unit, hk, NT * kTile, w.depth, w.anc);
+          if (idx < g.items) t = make_list(a, unit, hk, NT * kTile, w.depth, w.anc);
           more = t.ok != 0;
           int k0 = 0, k1 = 0, nb = 0;
           bool missing = false;
@@ -446,7 +455,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
       }
     };
     if (me == kCopyWarps - 1) {
-      uint32_t par = 3, qb = 0;                            // a bit per buffer
+      uint32_t par = 3, qb = 0, used = 0, last = 3;        // a bit per buffer; used: it has been filled, last: that phase's parity
       walk([&](const Item& w) {
         if (w.nb == 0) return;
         if (C::PAIR == 1) { wait(&sm.emptyQ[0], par & 1); par ^= 1u; }
@@ -454,6 +463,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
         for (int tile = 0; tile < w.nt; ++tile) {
           const int r0 = w.t.r0 + tile * kTile, hk = w.t.hk;
           if (C::PAIR == 1) qb = tile; else { wait(&sm.emptyQ[qb], par >> qb & 1); par ^= 1u << qb; }
+          fail = __any_sync(FULL, fail);
+          if (fail) return;
+          used |= 1u << qb; last ^= 1u << qb;
           const uint32_t to = q_at + qb * C::NP * kPanel;
           if (g.q_box) {
             if (lane == 0) {
@@ -475,6 +487,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
           if (C::PAIR == 2) qb ^= 1;
         }
       });
+      // (whoever has failed, no copy is under way at the end, and no product: nearly always they are done long before)
+      for (int i = 0; i < 2; ++i) if (used >> i & 1u) bar_wait_on(smem_u32(&sm.fullQ[i]), last >> i & 1u, kDrain);
     } else {
       const bool is_v = !C::KP || me >= C::TEAM;
       const int r0 = C::RW * (me % C::TEAM);               // of a block's rows, and every RW TEAM rows on
@@ -536,25 +550,25 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
     // the next S buffer of each tile, in a byte of its own (an item of one tile does not use the other's)
     auto next = [&](uint32_t x, int t) { return (x >> 8 * t & 255u) + 1 == C::SB ? x & ~(255u << 8 * t) : x + (1u << 8 * t); };
     // S buffer xs = Q (buffer qb) K^T (buffer kb, of K or V), `keys` of them
-    auto scores = [&](int xs, int qb, int kb, int keys) {
+    auto scores = [&](int xs, int qb, int kb, int keys, bool go) {
       fence_proxy();
       fence_after();
       // (values that the compiler knows to be the warp's: they go through uniform registers, one instruction each for a product)
       const uint32_t qd = uniform(desc_lo(q_at + qb * C::NP * kPanel, 1)), kd = uniform(desc_lo((C::KP ? k_at : v_at) + kb * C::NP * C::PB, 1));
       const uint32_t to = uniform(s_col + xs * C::SW), id = uniform(make_idesc((min(C::BN, keys) + 15) & ~15, 0));
-      if (one) {
+      if (go) {
 #pragma unroll
         for (int i = 0; i < 4 * C::NP; ++i)
           mma_ss2(to, qd + (i >> 2) * (kPanel >> 4) + 2 * (i & 3), kDescHi, kd + (i >> 2) * (C::PB >> 4) + 2 * (i & 3), kDescHi, id, i != 0);
       }
     };
     // O of tile t (+)= P (S buffer xo) V (buffer vo)
-    auto output = [&](int t, int xo, int vo, int keys, int acc) {
+    auto output = [&](int t, int xo, int vo, int keys, int acc, bool go) {
       fence_proxy();
       fence_after();
       const uint32_t vd = uniform(desc_lo(v_at + vo * C::NP * C::PB, C::PB >> 4)), pc = uniform(s_col + xo * C::SW), oc = uniform(o_col + t * C::OC);
       const uint32_t left = uniform(keys), more = uniform(acc);
-      if (one) {
+      if (go) {
 #pragma unroll
         for (int k = 0; k < C::BN / 16; ++k) {
           if (16 * k >= (int)left) break;
@@ -583,8 +597,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
             wait(&sm.s_free[xs], par_s >> xs & 1);
             par_s ^= 1u << xs;
             fail = __any_sync(0xffffffffu, fail);
-            scores(xs, qb, kb, k_all - j * C::BN);
-            if (one) {
+            const bool go = one && !fail;
+            scores(xs, qb, kb, k_all - j * C::BN, go);
+            if (go) {
               if (C::KP && t == nt - 1) mma_commit(&sm.emptyK[kb]);
               mma_commit(&sm.s_full[xs]);
               if (j == nb - 1 && t == nt - 1) mma_commit(&sm.emptyQ[C::PAIR == 2 ? qb : 0]);
@@ -613,8 +628,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
             wait(&sm.p_ready[xo], par_p >> xo & 1);
             par_p ^= 1u << xo;
             fail = __any_sync(0xffffffffu, fail);
-            output(t, xo, vb, k_all - j * C::BN, j);
-            if (one) {
+            const bool go = one && !fail;
+            output(t, xo, vb, k_all - j * C::BN, j, go);
+            if (go) {
               if (t == nt - 1) mma_commit(&sm.emptyV[vb]);
               mma_commit(&sm.s_free[xo]);
               if (j == nb - 1) mma_commit(&sm.o_full[t]);
@@ -626,12 +642,15 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
         }
       });
     }
+    uint64_t* done = &sm.drained[warp == kOutWarp];
+    if (one) mma_commit(done);
+    __syncwarp();
+    bar_wait_on(smem_u32(done), 0, kDrain);
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
     const int grp = warp >> 2, q4 = warp & 3;              // (a warp reaches the 32 lanes of tensor memory of its number modulo 4)
     const uint32_t lane_at = (uint32_t)(q4 * 32) << 16;
     const int tile = NT == 2 ? grp : 0, row = q4 * 32 + lane;
-    constexpr uint32_t FULL = 0xffffffffu;
     auto out_at = [&](const TileList& t, int r) {          // (r: within the item)
       const int gr = t.r0 + r;
       return reinterpret_cast<bf16*>(a.out) + ((t.row0 + gr / a.G) * a.s.H + (size_t)t.hk * a.G + gr % a.G) * a.s.d;
@@ -664,7 +683,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other_cta(&sm.bad[k][q4], rank ^ 1)), "r"(mine) : "memory");
         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(other_cta(&sm.bad_full[k][q4], rank ^ 1)) : "memory");
       }
-      if (!fail && !bar_wait_pair(&sm.bad_full[k][q4], turn >> 1 & 1)) fail = 1;
+      if (!fail && !bar_wait_pair(&sm.bad_full[k][q4], turn >> 1 & 1, g.tries)) fail = 1;
       ++turn;
       return ((mine | *(volatile uint32_t*)&sm.bad[k][q4]) >> lane & 1u) != 0;
     };
@@ -780,8 +799,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
         fence_after();
         load(s_col + x * C::SW + lane_at);
         wait(&sm.x_free[q4], par_x ^ 1);
-        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(&sm.x_full[q4])), "r"(32 * C::SL * 4) : "memory");
+        if (lane == 0 && !fail) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(&sm.x_full[q4])), "r"(32 * C::SL * 4) : "memory");
         loaded();
+        if (fail) return;
 #pragma unroll
         for (int e = 0; e < C::SL; e += 4)
           asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
@@ -924,9 +944,18 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
       });
     }
   }
-  if (__any_sync(0xffffffffu, fail)) for (int b = lane; b < a.s.B; b += 32) atomicOr(a.status + b, TSV_ST_INTERNAL);   // (an internal error: every sequence is flagged)
+  if (__any_sync(FULL, fail)) {                                  // an internal error: every sequence is flagged
+    for (int b = lane; b < a.s.B; b += 32) atomicOr(a.status + b, TSV_ST_INTERNAL);
+    if (C::PAIR == 2 && lane == 0) {
+      *(volatile uint32_t*)&sm.failed = 1;
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other_cta(&sm.failed, rank ^ 1)), "r"(1) : "memory");
+    }
+  }
   fence_before();
   all_sync();                                                   // (a pair: nobody reaches for the other's memory any more)
+  // Scores that the other CTA has sent, which nobody may have waited for, land within microseconds.
+  if (C::PAIR == 2 && *(volatile uint32_t*)&sm.failed)
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
 }
 
@@ -951,6 +980,7 @@ int tc_launch(const AttnArgs& a, int64_t units, cudaStream_t st) {
   typedef Cfg<DP, SHARED> C;
   TcArgs g;
   g.a = a;
+  g.tries = wait_tries(kWaitLimit);
   // (heads that do not fill a box of 128 rows evenly, or rows beyond a tensor map's: by the copying warps' own loads)
   g.q_box = (128 % a.G == 0 || a.G % 128 == 0) && a.bt.rows < (int64_t)1 << 31 && a.in.q_ld < (int64_t)1 << 38 && query_map(&g.q, a);
   const int64_t items = units * a.s.Hk * a.nsplit;

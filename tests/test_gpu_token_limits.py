@@ -188,3 +188,51 @@ def test_page_copies_that_do_not_come(api, tries, words):
     tries(-1)
     pg.pages_compact(pool, used, ws)                      # (nothing left to move)
     assert used.tolist() == [8]
+
+
+@pytest.mark.parametrize("heads,L,n", [
+    (("bf16", 8, 2, 64, False), [700, 20], [30, 140]), (("bf16", 32, 1, 128, True), [900], [300]), (("bf16", 6, 1, 256, False), [300, 4], [20, 300]),
+    (("bf16", 64, 1, 512, True), [700, 20, 3], [3, 140, 50]), (("bf16", 64, 1, 512, True), [17000], [1])], ids=str)
+def test_attention_whose_waits_give_up(api, tries, heads, L, n):
+    """After any number of tries: the sequences are flagged, or the result is whole (no wait was longer than its first try, of 4 us); other rows stay
+    as they were, and the next call is right."""
+    tsv, tk, _ = api
+    lay = Layer(tk, *heads, window=20000, sinks=3, L=L, n=n, page=64, seed=1)
+    good = lay.run(tk).clone()
+    assert not lay.status.any()
+    mine = torch.zeros(lay.rows, dtype=torch.bool)
+    for r, k in zip(lay.row0, n):
+        mine[r:r + k] = True
+    seen = set()
+    for k in [0, 0, 0, 1, 1, 2, 3, 5, 8, 13, 40, 1 << 20]:
+        tries(k)
+        lay.status.zero_()
+        out = lay.run(tk)
+        st = set(lay.status.tolist())
+        assert st <= {0, tsv.ST_INTERNAL} and len(st) == 1 and (out[~mine.cuda()] == 3.0).all()
+        seen |= st
+        if st == {0}:
+            assert torch.equal(out.nan_to_num(9), good.nan_to_num(9))
+        tries(-1)
+        lay.status.zero_()
+        assert torch.equal(lay.run(tk).nan_to_num(9), good.nan_to_num(9)) and not lay.status.any()
+    assert 0 in seen
+
+
+# (more than two tiles for every CTA, and a first position that all rows see)
+@pytest.mark.parametrize("heads,n", [(("bf16", 16, 1, 64, False), 9000), (("bf16", 16, 1, 128, True), 9000), (("bf16", 32, 1, 256, False), 2400),
+                                     (("bf16", 64, 1, 512, True), 500), (("bf16", 64, 1, 512, False), 500)], ids=str)
+def test_rows_one_by_one_that_outlast_the_waits(api, tries, heads, n):
+    """Rows that see a NaN take longer than the others wait for them: the call is flagged, and the items that are being worked on stay as they are."""
+    tsv, tk, _ = api
+    lay = Layer(tk, *heads, window=200, sinks=1, L=[0], n=[n], seed=1)
+    (lay.k if lay.v is None else lay.v)[lay.row0[0], 0, 3] = float("nan")
+    want = lay.run(tk).clone()
+    assert not lay.status.any()
+    for k in (0, 1, 3, 10, 30, 100):
+        tries(k)
+        lay.run(tk)
+        assert lay.status.tolist() == [tsv.ST_INTERNAL]
+        tries(-1)
+        lay.status.zero_()
+        assert torch.equal(lay.run(tk).nan_to_num(9), want.nan_to_num(9)) and not lay.status.any()
