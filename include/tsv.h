@@ -341,8 +341,10 @@ typedef struct tsv_tok_shape {
 /* Token-level keys and values of ONE layer.  Rows of Hk * d elements, one per token; the row of position pos of sequence b is
  *   ring (page_table NULL):  b * (n_sink + window) + (pos < n_sink ? pos : n_sink + (pos - n_sink) % window)
  *   pages:                   page_table[b][pos / page_tokens] * page_tokens + pos % page_tokens
- * With n_sink = 0 these are win_kv of tsv_cache, ring or token pool (v = NULL).  Pages that hold no visible position may be
- * missing (-1): a window layer can give back what lies between its sinks and its window.  Rows that are not visible may
+ * With n_sink = 0 and the layer's window these are win_kv of tsv_cache, ring or token pool (v = NULL), for window_sink_attn
+ * only: token_commit would move L without the layer's compressed entries and open blocks, which accept_and_refresh moves
+ * with it.  Pages that hold no visible position may be missing (-1): a window layer can give back what lies between its
+ * sinks and its window.  Rows that are not visible may
  * hold anything, also infinities and NaN. */
 typedef struct tsv_tok_cache {
   int32_t *L;                 /* [B] committed tokens                                       */

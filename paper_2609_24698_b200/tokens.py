@@ -130,14 +130,20 @@ class TokenCache:
     v: Optional[torch.Tensor] = None          # None: the keys are the values
     page_table: Optional[torch.Tensor] = None  # [B, max_pages] int32
     page_tokens: int = 0
+    ring: Optional[tuple] = None              # (n_sink, window) that the rows of a ring are laid out for, if known
+    commits: bool = True                      # False: the sequences advance by another call, and token_commit refuses
 
     @staticmethod
     def of_layer(cache: tsv.LayerCache) -> "TokenCache":
-        """The token-level KV of a verify layer: its window ring, or its pool's third physical layer (n_sink = 0 for a ring)."""
-        return TokenCache(cache.L, cache.win_kv, None, cache.page_table, cache.page_tokens)
+        """The token-level KV of a verify layer, to be read: its window ring (n_sink = 0 and the layer's window then), or its pool's third
+        physical layer.  L, compressed entries and open blocks of the layer advance together, by accept_and_refresh, so token_commit refuses."""
+        ring = None if cache.page_table is not None else (0, cache.win_kv.shape[1])
+        return TokenCache(cache.L, cache.win_kv, None, cache.page_table, cache.page_tokens, ring, False)
 
     def pack(self, shape: TokenShape, dev: int) -> bytes:
         dt, width, k, table = shape.torch_dtype, shape.Hk * shape.d, self.k, self.page_table
+        if self.ring is not None and self.ring != (shape.n_sink, shape.window):
+            raise TsvError(tsv.ERR_SHAPE, f"cache: rings of (n_sink, window) = {self.ring}, the shape has {(shape.n_sink, shape.window)}")
         rows = k.numel() // width
         return _pack_cache(_flat("L", self.L, _i32, shape.B, dev), _flat("cache.k", k, dt, width, dev), _maybe("cache.v", self.v, dt, rows * width, dev), rows,
                            0 if table is None else _flat("page_table", table, _i32, shape.B * table.shape[1], dev), self.page_tokens,
@@ -147,7 +153,7 @@ class TokenCache:
 def alloc_token_cache(shape: TokenShape, values: bool = True, device="cuda") -> TokenCache:
     """Empty rings (L = 0) for the shape's sequences."""
     z = lambda: torch.zeros(shape.B, shape.n_sink + shape.window, shape.Hk, shape.d, dtype=shape.torch_dtype, device=device)
-    return TokenCache(torch.zeros(shape.B, dtype=torch.int32, device=device), z(), z() if values else None)
+    return TokenCache(torch.zeros(shape.B, dtype=torch.int32, device=device), z(), z() if values else None, ring=(shape.n_sink, shape.window))
 
 
 def alloc_token_pool(shape: TokenShape, n_pages: int, page_tokens: int, max_pages: int, values: bool = True, device="cuda") -> TokenCache:
@@ -218,6 +224,8 @@ def window_sink_attn(shape: TokenShape, cache: TokenCache, batch: TokenBatch, q:
 def token_commit(shape: TokenShape, cache: TokenCache, batch: TokenBatch, k: torch.Tensor, v: Optional[torch.Tensor], status: torch.Tensor,
                  path: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, stream=None) -> None:
     """Rows of new tokens (all n[b] of a sequence, or the first count[b] nodes of path[b]) into the cache; L[b] grows by them."""
+    if not cache.commits:
+        raise TsvError(tsv.ERR_SHAPE, "token_commit: a verify layer's cache advances by accept_and_refresh, which keeps its compressed entries and open blocks with L")
     dev = _device()
     ld = 0 if path is None else path.shape[1]
     r = _lib.token_commit(_at(shape.c), cache.pack(shape, dev), batch.pack(shape.B, k.shape[0], dev), _kv(shape, None, k, v, dev),

@@ -236,3 +236,50 @@ def test_rows_one_by_one_that_outlast_the_waits(api, tries, heads, n):
         tries(-1)
         lay.status.zero_()
         assert torch.equal(lay.run(tk).nan_to_num(9), want.nan_to_num(9)) and not lay.status.any()
+
+
+@pytest.mark.parametrize("page_tokens", [0, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_over_a_verify_layers_window(api, dtype, page_tokens):
+    """New tokens attend to the token-level KV that a verify layer holds, after cycles of it, and the layer goes on as without that."""
+    tsv, tk, _ = api
+    from paper_2609_24698_b200 import harness as hz, synth
+    from tests.helpers import oracle_states, state_arrays
+    from tests.test_gpu_tokens import STEP
+    sh = synth.Shape("bf16", 3, 8, 64, 512, 4, 512, 4, 128, 128, 128) if dtype == "bf16" else synth.Shape("fp32", 3, 8, 16, 128, 4, 64, 1, 64, 128, 128)
+    cfg = synth.Config("tokens", 230, sh, layers=1, L_min=0, L_max=1000, seed=4)
+    lengths = np.asarray([1000, 3, 300])
+    states = oracle_states(cfg, lengths)
+    ccap, hcap = hz.capacities(sh, [1000, 1000, 300], 64)
+    eng = hz.VerifyEngine(sh, 1, ccap, hcap, 1200, page_tokens=page_tokens)
+    for b in range(3):
+        hz.fill_cache(eng.caches[0], sh, b, int(lengths[b]), state_arrays(states[0][b]))
+    for cyc in range(2):
+        parent, n_nodes = synth.trees(cfg, cyc)
+        draft, target = synth.tokens(cfg, cyc, parent, n_nodes)
+        eng.launch_cycle(hz.InputSet.from_numpy(sh, [synth.node_inputs(cfg, 0, cyc)], parent, n_nodes, draft, target))
+    layer = eng.caches[0]
+    L = layer.L.tolist()
+    cache = tk.TokenCache.of_layer(layer)
+    n, d, H = [2, 40, 1], sh.d, 8
+    row0, rows = [0, 2, 42], 43
+    shape = tk.TokenShape(dtype, 3, H, 1, d, sh.window, max_L=2000, max_n=40)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q, k = (torch.randn(rows, h, d, device="cuda", generator=gen).to(shape.torch_dtype) for h in (H, 1))
+    batch = tk.TokenBatch(torch.tensor(row0, dtype=torch.int64).cuda(), torch.tensor(n, dtype=torch.int32).cuda())
+    out, st = torch.zeros_like(q), torch.zeros(3, dtype=torch.int32, device="cuda")
+    before = layer.win_kv.clone()
+    tk.window_sink_attn(shape, cache, batch, q, k, None, out, tk.alloc_workspace(shape, rows), st)
+    assert not st.any() and layer.L.tolist() == L and torch.equal(layer.win_kv, before)
+    flat = layer.win_kv.view(-1, d)
+    for b in range(3):
+        first = max(0, L[b] - sh.window)
+        hist = np.zeros((L[b], 1, d))
+        hist[first:, 0] = f64(flat[layer.tok_row_index(sh, b, torch.arange(first, L[b], device="cuda"))])
+        r = slice(row0[b], row0[b] + n[b])
+        ref, mag, reach = T.attend(f64(q[r]), f64(k[r]), f64(k[r]), hist, hist, sh.window, 0, d ** -0.5)
+        tol = STEP[dtype] * np.abs(ref) + mag * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -20) + mag * 2 * ((d + 4) * 2.0 ** -24 * reach)[..., None]
+        assert (np.abs(f64(out[r]) - ref) <= tol).all()
+    with pytest.raises(tsv.TsvError):
+        tk.token_commit(shape, cache, batch, k, None, st)
+    assert layer.L.tolist() == L

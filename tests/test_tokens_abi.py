@@ -242,3 +242,23 @@ def test_pool_operations_keep_counts():
     for s in range(6):
         for p in pool.table[s]:
             assert p < 0 or pool.ref[p] > 0
+
+
+def test_a_verify_layers_cache_is_read_only(api):
+    """Its lengths belong to the verify path; a ring is refused under another window than its own."""
+    import torch
+    tsv, tk, _ = api
+    from types import SimpleNamespace
+    layer = SimpleNamespace(L=torch.zeros(2, dtype=torch.int32), win_kv=torch.zeros(2, 8, 16, dtype=torch.bfloat16), page_table=None, page_tokens=0)
+    cache = tk.TokenCache.of_layer(layer)
+    batch = tk.TokenBatch(torch.zeros(2, dtype=torch.int64), torch.ones(2, dtype=torch.int32))
+    shape = lambda window, sinks=0: tk.TokenShape("bf16", 2, 4, 1, 16, window=window, n_sink=sinks, max_L=64, max_n=4)
+    with pytest.raises(tsv.TsvError, match="accept_and_refresh"):
+        tk.token_commit(shape(8), cache, batch, torch.zeros(2, 1, 16, dtype=torch.bfloat16), None, torch.zeros(2, dtype=torch.int32))
+    assert len(cache.pack(shape(8), -1)) == C.sizeof(tk.CTokCache)
+    for bad in (shape(4), shape(7, 1)):
+        with pytest.raises(tsv.TsvError) as e:
+            cache.pack(bad, -1)
+        assert e.value.code == tsv.ERR_SHAPE
+        with pytest.raises(tsv.TsvError):
+            tk.alloc_token_cache(shape(8), device="cpu").pack(bad, -1)
