@@ -41,6 +41,12 @@ _lib.pages_compact.argtypes = [_p, _p, _p, C.c_size_t, _p]
 _at = C.addressof
 
 
+def counts_of(page_table: torch.Tensor, n_pages: int) -> torch.Tensor:
+    """How many words of the table name each page (int32); words that name none of the pool's count for nothing."""
+    held = page_table.flatten().long()
+    return torch.zeros(n_pages, dtype=torch.int32, device=held.device).index_add_(0, held.clamp(0, n_pages - 1), ((held >= 0) & (held < n_pages)).int())
+
+
 class PagePool:
     """Description of a pool over the caller's tensors, which it keeps: page_table [slots, max_pages] and ref [n_pages] (int32), planes
     (contiguous, the same share of each belongs to a page) and rows (contiguous, [slots, ...])."""
@@ -61,15 +67,16 @@ class PagePool:
 
     @staticmethod
     def of_layers(caches: Sequence[tsv.LayerCache], ref: Optional[torch.Tensor] = None) -> "PagePool":
-        """The pool behind the paged caches of layers that share one page table tensor; ref: the counts, by default those that the table
-        shows."""
-        c0 = caches[0]
-        if c0.page_table is None or any(c.page_table is None or c.page_table.data_ptr() != c0.page_table.data_ptr() for c in caches):
+        """The pool behind the paged caches of layers that share one page table tensor and the size and number of its pages; ref: the counts, by
+        default those that the table shows."""
+        c0 = caches[0] if len(caches) else None
+        if c0 is None or c0.page_table is None or any(c.page_table is None or c.page_table.data_ptr() != c0.page_table.data_ptr() for c in caches):
             raise TsvError(tsv.ERR_SHAPE, "PagePool.of_layers: the layers must share one page table")
+        if any(c.page_tokens != c0.page_tokens or c.win_kv.shape[0] != c0.win_kv.shape[0] for c in caches):
+            raise TsvError(tsv.ERR_SHAPE, f"PagePool.of_layers: page sizes {[c.page_tokens for c in caches]} and token rows {[c.win_kv.shape[0] for c in caches]} differ")
         n = c0.win_kv.shape[0] // c0.page_tokens
         if ref is None:
-            held = c0.page_table.flatten().long()
-            ref = torch.zeros(n, dtype=torch.int32, device=held.device).index_add_(0, held.clamp(min=0), (held >= 0).int())
+            ref = counts_of(c0.page_table, n)
         planes = [t for c in caches for t in (c.csa_kv, c.csa_ik, c.hca_kv, c.win_kv)]
         rows = [t for c in caches for t in (c.L, c.csa_cap, c.hca_cap, c.csa_mx, c.csa_s, c.csa_acc_kv, c.csa_acc_ik, c.hca_mx, c.hca_s, c.hca_acc_kv)]
         return PagePool(c0.page_table, ref, c0.page_tokens, planes, rows)

@@ -283,3 +283,26 @@ def test_attention_over_a_verify_layers_window(api, dtype, page_tokens):
     with pytest.raises(tsv.TsvError):
         tk.token_commit(shape, cache, batch, k, None, st)
     assert layer.L.tolist() == L
+
+
+def test_a_pool_of_layers_whose_table_names_pages_that_are_none(api):
+    """Counts are made without such words, and the sequences that hold them are flagged where they are forked."""
+    tsv, _, pg = api
+    from paper_2609_24698_b200 import harness as hz, synth
+    sh = synth.Shape("fp32", 3, 8, 16, 128, 4, 64, 1, 64, 128, 128)
+    ccap, hcap = hz.capacities(sh, [1000, 1000, 300], 64)
+    eng = hz.VerifyEngine(sh, 2, ccap, hcap, 1200, page_tokens=128)
+    eng.caches[1].page_table = eng.caches[0].page_table
+    table = eng.caches[0].page_table
+    n = eng.caches[0].win_kv.shape[0] // 128
+    table.fill_(-1)
+    table[0, :3] = torch.tensor([4, n, 5], dtype=torch.int32)
+    table[2, :2] = torch.tensor([4, -9], dtype=torch.int32)
+    pool = pg.PagePool.of_layers(eng.caches)
+    want = [0] * n
+    want[4], want[5] = 2, 1
+    assert pool.ref.tolist() == want
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    pg.pages_fork(pool, i32(0), i32(1), eng.caches[0].L, pg.alloc_workspace(pool), st)
+    assert st.tolist() == [pg.ST_PAGE] and (table[1] == -1).all()

@@ -262,3 +262,37 @@ def test_a_verify_layers_cache_is_read_only(api):
         assert e.value.code == tsv.ERR_SHAPE
         with pytest.raises(tsv.TsvError):
             tk.alloc_token_cache(shape(8), device="cpu").pack(bad, -1)
+
+
+def _paged_layer(pages=6, page_tokens=4, table=None):
+    import torch
+    from types import SimpleNamespace
+    z = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt)
+    rows = {n: z(2, 3) for n in ("csa_mx", "csa_s", "csa_acc_kv", "csa_acc_ik", "hca_mx", "hca_s", "hca_acc_kv")}
+    return SimpleNamespace(L=z(2, dt=torch.int32), csa_cap=z(2, dt=torch.int32), hca_cap=z(2, dt=torch.int32), page_tokens=page_tokens,
+                           csa_kv=z(pages, 8), csa_ik=z(pages, 8), hca_kv=z(pages, 8), win_kv=z(pages * page_tokens, 8),
+                           page_table=torch.tensor([[0, 1, -1], [2, -1, -1]], dtype=torch.int32) if table is None else table, **rows)
+
+
+@pytest.mark.parametrize("word", [6, 1 << 30, -2, -(1 << 31)])
+def test_counts_of_a_table_with_words_that_name_no_page(api, word):
+    """Such words count for nothing.  (Everything is on the CPU here, which the pool itself refuses, last.)"""
+    import torch
+    tsv, _, pg = api
+    table = torch.tensor([[0, word, -1], [2, 0, -1]], dtype=torch.int32)
+    assert pg.counts_of(table, 6).tolist() == [2, 0, 1, 0, 0, 0]
+    with pytest.raises(tsv.TsvError):
+        pg.PagePool.of_layers([_paged_layer(table=table)])
+
+
+def test_layers_whose_pools_differ_are_refused(api):
+    """Pages of other sizes or another number of them behind the one table: the bytes of a page would be wrong in every plane of that layer."""
+    tsv, _, pg = api
+    a = _paged_layer()
+    for b in (_paged_layer(pages=12, table=a.page_table), _paged_layer(page_tokens=8, table=a.page_table)):
+        with pytest.raises(tsv.TsvError, match="page sizes"):
+            pg.PagePool.of_layers([a, b])
+    with pytest.raises(tsv.TsvError, match="one page table"):
+        pg.PagePool.of_layers([a, _paged_layer(table=a.page_table.clone())])
+    with pytest.raises(tsv.TsvError):
+        pg.PagePool.of_layers([])
