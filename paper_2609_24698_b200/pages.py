@@ -12,8 +12,8 @@ from typing import Optional, Sequence
 import torch
 
 from . import binding as tsv
-from .binding import TsvError, _aligned, _lib, _p
-from .tokens import ST_PAGE, ST_POOL, _bad, _device, _flat, _i32, _on  # noqa: F401
+from .binding import TsvError, _lib, _p
+from .tokens import ST_PAGE, ST_POOL, _bad, _device, _flat, _i32, _on, _workspace  # noqa: F401
 
 MAX_LIST = 1024
 
@@ -52,6 +52,8 @@ class PagePool:
     (contiguous, the same share of each belongs to a page) and rows (contiguous, [slots, ...])."""
 
     def __init__(self, page_table: torch.Tensor, ref: torch.Tensor, page_tokens: int, planes: Sequence[torch.Tensor], rows: Sequence[torch.Tensor] = ()):
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or not isinstance(ref, torch.Tensor):
+            raise TsvError(tsv.ERR_SHAPE, "PagePool: expected page_table [slots, max_pages] and ref [n_pages]")
         slots, max_pages = page_table.shape
         n = ref.numel()
         self.page_table, self.ref, self.planes, self.rows = page_table, ref, list(planes), list(rows)
@@ -89,20 +91,22 @@ def alloc_workspace(pool: PagePool) -> torch.Tensor:
     return torch.empty(n + 256, dtype=torch.uint8, device=pool.page_table.device)
 
 
-def _here(pool: PagePool, workspace: Optional[torch.Tensor] = None) -> int:
+def _here(pool: PagePool) -> int:
     dev = _device()
     if pool.device != dev:
         _bad("pool", "a pool", pool.page_table)
-    if workspace is not None and workspace.get_device() != dev:
-        _bad("workspace", "a workspace", workspace)
     return dev
+
+
+def _count(where: str, t: torch.Tensor) -> int:
+    return t.numel() if isinstance(t, torch.Tensor) else _bad(where, "an int32 tensor", t)
 
 
 def pages_assign(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor,
                  stream=None) -> None:
     """Logical pages first[i] .. last[i] - 1 of slots[i] that have no page get the free ones with the lowest numbers."""
-    n, dev = slots.numel(), _here(pool, workspace)
-    wp, wn = _aligned(workspace)
+    n, dev = _count("slots", slots), _here(pool)
+    wp, wn = _workspace(workspace, dev)
     r = _lib.pages_assign(_at(pool.c), n, _flat("slots", slots, _i32, n, dev), _flat("first", first, _i32, n, dev), _flat("last", last, _i32, n, dev), wp, wn,
                           _flat("status", status, _i32, n, dev), _on(stream, dev))
     if r:
@@ -111,7 +115,7 @@ def pages_assign(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last:
 
 def pages_free(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """slots[i] gives up its logical pages first[i] .. last[i] - 1."""
-    n, dev = slots.numel(), _here(pool)
+    n, dev = _count("slots", slots), _here(pool)
     r = _lib.pages_free(_at(pool.c), n, _flat("slots", slots, _i32, n, dev), _flat("first", first, _i32, n, dev), _flat("last", last, _i32, n, dev),
                         _flat("status", status, _i32, n, dev), _on(stream, dev))
     if r:
@@ -120,8 +124,8 @@ def pages_free(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: t
 
 def pages_fork(pool: PagePool, src: torch.Tensor, dst: torch.Tensor, L: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """dst[i], a slot without pages, becomes a copy of src[i] with L[src[i]] tokens: full pages shared, the last one and the rows copied."""
-    n, dev = src.numel(), _here(pool, workspace)
-    wp, wn = _aligned(workspace)
+    n, dev = _count("src", src), _here(pool)
+    wp, wn = _workspace(workspace, dev)
     r = _lib.pages_fork(_at(pool.c), n, _flat("src", src, _i32, n, dev), _flat("dst", dst, _i32, n, dev), _flat("L", L, _i32, pool.c.slots, dev), wp, wn,
                         _flat("status", status, _i32, n, dev), _on(stream, dev))
     if r:
@@ -130,8 +134,8 @@ def pages_fork(pool: PagePool, src: torch.Tensor, dst: torch.Tensor, L: torch.Te
 
 def pages_compact(pool: PagePool, n_used: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """The used pages move to the lowest numbers, contents, table and counts; n_used (int32, 1 value) becomes their number."""
-    dev = _here(pool, workspace)
-    wp, wn = _aligned(workspace)
+    dev = _here(pool)
+    wp, wn = _workspace(workspace, dev)
     r = _lib.pages_compact(_at(pool.c), _flat("n_used", n_used, _i32, 1, dev), wp, wn, _on(stream, dev))
     if r:
         raise TsvError(r, "pages_compact")

@@ -91,7 +91,7 @@ def _bad(where: str, expected: str, t) -> None:
 
 def _flat(where: str, t: torch.Tensor, dtype: torch.dtype, numel: int, dev: int) -> int:
     """Pointer of a contiguous tensor of at least `numel` elements on device dev."""
-    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or t.get_device() != dev:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or t.get_device() != dev:
         _bad(where, f"a contiguous {dtype} tensor of {numel} elements", t)
     return t.data_ptr()
 
@@ -100,14 +100,35 @@ def _maybe(where: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int
     return 0 if t is None else _flat(where, t, dtype, numel, dev)
 
 
+def _table(where: str, t: Optional[torch.Tensor], rows: int, dev: int):
+    """Pointer and row length of an int32 table of at least `rows` rows; (0, 0) for None."""
+    if t is None:
+        return 0, 0
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        _bad(where, f"an int32 tensor of {rows} rows", t)
+    return _flat(where, t, _i32, rows * t.shape[1], dev), t.shape[1]
+
+
+def _workspace(workspace: torch.Tensor, dev: int):
+    if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev:
+        _bad("workspace", "a workspace", workspace)
+    return _aligned(workspace)
+
+
 def _vectors(where: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, d: int, dev: int):
     """Pointer and row stride of a [>= rows, heads, d] tensor whose heads follow each other in a row."""
-    s = t.shape
-    if t.dtype is dtype and len(s) == 3 and s[0] >= rows and s[1] == heads and s[2] == d and t.get_device() == dev:
+    s = t.shape if isinstance(t, torch.Tensor) else ()
+    if s and t.dtype is dtype and len(s) == 3 and s[0] >= rows and s[1] == heads and s[2] == d and t.get_device() == dev:
         ld, hs, es = t.stride()
         if es == 1 and (hs == d or heads == 1):
             return t.data_ptr(), (ld if s[0] > 1 else heads * d)
     _bad(where, f"a {dtype} tensor [{rows}, {heads}, {d}] whose rows are contiguous", t)
+
+
+def _rows(where: str, t: torch.Tensor) -> int:
+    if not isinstance(t, torch.Tensor) or not t.dim():
+        _bad(where, "a tensor of rows", t)
+    return t.shape[0]
 
 
 @dataclass
@@ -144,10 +165,9 @@ class TokenCache:
         dt, width, k, table = shape.torch_dtype, shape.Hk * shape.d, self.k, self.page_table
         if self.ring is not None and self.ring != (shape.n_sink, shape.window):
             raise TsvError(tsv.ERR_SHAPE, f"cache: rings of (n_sink, window) = {self.ring}, the shape has {(shape.n_sink, shape.window)}")
-        rows = k.numel() // width
-        return _pack_cache(_flat("L", self.L, _i32, shape.B, dev), _flat("cache.k", k, dt, width, dev), _maybe("cache.v", self.v, dt, rows * width, dev), rows,
-                           0 if table is None else _flat("page_table", table, _i32, shape.B * table.shape[1], dev), self.page_tokens,
-                           0 if table is None else table.shape[1])
+        kp, rows = _flat("cache.k", k, dt, width, dev), k.numel() // width
+        tp, max_pages = _table("page_table", table, shape.B, dev)
+        return _pack_cache(_flat("L", self.L, _i32, shape.B, dev), kp, _maybe("cache.v", self.v, dt, rows * width, dev), rows, tp, self.page_tokens, max_pages)
 
 
 def alloc_token_cache(shape: TokenShape, values: bool = True, device="cuda") -> TokenCache:
@@ -185,7 +205,7 @@ def qk_norm_rope(shape: TokenShape, L: torch.Tensor, batch: TokenBatch, q: Optio
     some = q if q is not None else k
     if some is None:
         raise TsvError(tsv.ERR_NULL, "qk_norm_rope")
-    rows, H, Hk, d = some.shape[0], shape.H, shape.Hk, shape.d
+    rows, H, Hk, d = _rows("q" if q is not None else "k", some), shape.H, shape.Hk, shape.d
     qp = qo = kp = ko = ql = qol = kl = kol = 0
     if q is not None:
         (qp, ql), (qo, qol) = _vectors("q", q, dt, rows, H, d, dev), _vectors("q_out", q_out, dt, rows, H, d, dev)
@@ -200,7 +220,7 @@ def qk_norm_rope(shape: TokenShape, L: torch.Tensor, batch: TokenBatch, q: Optio
 
 
 def _kv(shape: TokenShape, q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], dev: int) -> bytes:
-    dt, rows, Hk, d = shape.torch_dtype, k.shape[0], shape.Hk, shape.d
+    dt, rows, Hk, d = shape.torch_dtype, _rows("k", k), shape.Hk, shape.d
     qp, qs = _vectors("q", q, dt, rows, shape.H, d, dev) if q is not None else (0, 0)
     kp, ks = _vectors("k", k, dt, rows, Hk, d, dev)
     vp, vs = _vectors("v", v, dt, rows, Hk, d, dev) if v is not None else (0, 0)
@@ -210,10 +230,8 @@ def _kv(shape: TokenShape, q: Optional[torch.Tensor], k: torch.Tensor, v: Option
 def window_sink_attn(shape: TokenShape, cache: TokenCache, batch: TokenBatch, q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor],
                      out: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """out [rows, H, d]: every new token's attention to the sinks and its window, committed (cache) and new (k, v) tokens."""
-    rows, dev = k.shape[0], _device()
-    if workspace.get_device() != dev:
-        _bad("workspace", "a workspace", workspace)
-    wp, wn = _aligned(workspace)
+    dev = _device()
+    (wp, wn), rows = _workspace(workspace, dev), _rows("k", k)
     r = _lib.window_sink_attn(_at(shape.c), cache.pack(shape, dev), batch.pack(shape.B, rows, dev), _kv(shape, q, k, v, dev),
                               _flat("out", out, shape.torch_dtype, rows * shape.H * shape.d, dev), wp, wn, _flat("status", status, _i32, shape.B, dev),
                               _on(stream, dev))
@@ -227,9 +245,8 @@ def token_commit(shape: TokenShape, cache: TokenCache, batch: TokenBatch, k: tor
     if not cache.commits:
         raise TsvError(tsv.ERR_SHAPE, "token_commit: a verify layer's cache advances by accept_and_refresh, which keeps its compressed entries and open blocks with L")
     dev = _device()
-    ld = 0 if path is None else path.shape[1]
-    r = _lib.token_commit(_at(shape.c), cache.pack(shape, dev), batch.pack(shape.B, k.shape[0], dev), _kv(shape, None, k, v, dev),
-                          _maybe("path", path, _i32, shape.B * ld, dev), ld, _maybe("count", count, _i32, shape.B, dev),
+    pp, ld = _table("path", path, shape.B, dev)
+    r = _lib.token_commit(_at(shape.c), cache.pack(shape, dev), batch.pack(shape.B, _rows("k", k), dev), _kv(shape, None, k, v, dev), pp, ld, _maybe("count", count, _i32, shape.B, dev),
                           _flat("status", status, _i32, shape.B, dev), _on(stream, dev))
     if r:
         raise TsvError(r, "token_commit")

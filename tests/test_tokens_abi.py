@@ -296,3 +296,41 @@ def test_layers_whose_pools_differ_are_refused(api):
         pg.PagePool.of_layers([a, _paged_layer(table=a.page_table.clone())])
     with pytest.raises(tsv.TsvError):
         pg.PagePool.of_layers([])
+
+
+def test_missing_arguments_and_other_ranks_are_refused(api, monkeypatch):
+    """None, numbers and tensors of another rank where a tensor is needed: the library's own error, before it is called.  (On the CPU, taken for the
+    current device; a call that gets through would end in the library's refusal of a NULL pointer or of the workspace.)"""
+    import torch
+    tsv, tk, pg = api
+    for m in (tk, pg):
+        monkeypatch.setattr(m, "_device", lambda: -1)
+        monkeypatch.setattr(m, "_on", lambda stream, dev: 0)
+    s = tk.TokenShape("bf16", 2, 4, 2, 16, window=8, max_L=64, max_n=4)
+    i32 = lambda *sh: torch.zeros(*sh, dtype=torch.int32)
+    z = lambda h: torch.zeros(5, h, 16, dtype=torch.bfloat16)
+    batch, st = tk.TokenBatch(torch.zeros(2, dtype=torch.int64), i32(2)), i32(2)
+    cache = tk.alloc_token_cache(s, device="cpu")
+    table = lambda t: tk.TokenCache(cache.L, cache.k, cache.v, t, 4)
+    ws = torch.zeros(64, dtype=torch.uint8)
+    rope = lambda L=st, q=z(4), k=z(2), qo=z(4), ko=z(2), w=None, inv=torch.zeros(8), status=st, b=batch: tk.qk_norm_rope(s, L, b, q, k, qo, ko, w, w, 1e-6, inv, 0, False, status)
+    attn = lambda c=cache, b=batch, q=z(4), k=z(2), v=z(2), out=z(4), ws=ws, status=st: tk.window_sink_attn(s, c, b, q, k, v, out, ws, status)
+    commit = lambda c=cache, b=batch, k=z(2), v=z(2), status=st, path=None, count=None: tk.token_commit(s, c, b, k, v, status, path=path, count=count)
+    calls = [lambda x=x: rope(**{x: bad}) for x in ("L", "qo", "ko", "status") for bad in (None, 3)]
+    calls += [lambda: rope(q=None, k=None), lambda: rope(q=3), lambda: rope(w=3), lambda: rope(inv=torch.zeros(8, dtype=torch.float64))]
+    calls += [lambda x=x, bad=bad: attn(**{x: bad}) for x in ("q", "k", "out", "ws", "status") for bad in ((3,) if x == "ws" else (3, torch.zeros(())))]
+    calls += [lambda: attn(k=None), lambda: attn(out=None), lambda: attn(ws=None), lambda: attn(status=None), lambda: attn(q=None)]
+    calls += [lambda t=t: attn(c=table(t)) for t in (i32(6), i32(2, 3, 1), 3)] + [lambda: attn(c=tk.TokenCache(None, cache.k)), lambda: attn(c=tk.TokenCache(cache.L, None))]
+    calls += [lambda b=b: attn(b=b) for b in (tk.TokenBatch(None, i32(2)), tk.TokenBatch(batch.row0, None), tk.TokenBatch(batch.row0, batch.n, 3))]
+    calls += [lambda: commit(k=None), lambda: commit(status=None), lambda: commit(path=i32(8)), lambda: commit(path=3), lambda: commit(path=i32(1, 4)), lambda: commit(count=3)]
+    pool = pg.PagePool.__new__(pg.PagePool)
+    pool.device, pool.page_table, pool.c = -1, i32(2, 3), pg.CPagePool()
+    one = i32(1)
+    calls += [lambda: pg.pages_assign(pool, None, one, one, ws, one), lambda: pg.pages_assign(pool, one, None, one, ws, one), lambda: pg.pages_assign(pool, one, one, one, None, one),
+              lambda: pg.pages_free(pool, None, one, one, one), lambda: pg.pages_free(pool, one, one, one, None), lambda: pg.pages_fork(pool, None, one, one, ws, one),
+              lambda: pg.pages_fork(pool, one, one, None, ws, one), lambda: pg.pages_fork(pool, one, one, one, None, one), lambda: pg.pages_compact(pool, None, ws),
+              lambda: pg.pages_compact(pool, one, None), lambda: pg.PagePool(i32(6), one, 4, []), lambda: pg.PagePool(None, one, 4, []), lambda: pg.PagePool(i32(2, 3), None, 4, [])]
+    for i, call in enumerate(calls):
+        with pytest.raises(tsv.TsvError):
+            call()
+            raise AssertionError(f"call {i} went through")
