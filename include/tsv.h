@@ -376,7 +376,9 @@ typedef struct tsv_tok_rows {
  *   pairs = 0:  a = x[first + i],     b = x[first + rot / 2 + i]
  *   pairs = 1:  a = x[first + 2 i],   b = x[first + 2 i + 1].
  * rot is 0 or a multiple of 16, first a multiple of 8, first + rot <= d.  in->q or in->k may be NULL (that part is left
- * out; not both).  q_out, k_out: rows of ldq, ldk elements; each may be its input.  L [B] is read only.  in->v is not used.
+ * out; not both).  q_out, k_out: rows of ldq, ldk elements; each may be its input (same address and stride), and shares no
+ * other element with the inputs or the other output (TSV_ERR_SHAPE; rows of one stride may lie between each other's).
+ * L [B] is read only.  in->v is not used.
  */
 int qk_norm_rope(const tsv_tok_shape *shape, const int32_t *L, const tsv_tok_batch *batch, const tsv_tok_rows *in,
                  const float *wq, const float *wk, float eps, const float *inv_freq, int32_t rot, int32_t first, int32_t pairs,

@@ -41,6 +41,19 @@ static bool meets(const tsv_tok_shape* s, const void* out, int64_t bytes, const 
   return p && a < b + span && b < a + bytes;
 }
 
+// Do two arrays of `rows` rows share an element?  Of `heads` vectors each, ld elements from row to row; rows of one and the same stride may lie
+// between each other's (column ranges of one array), others not.
+static bool rows_meet(const tsv_tok_shape* s, const void* p, int64_t ld, int heads, const void* q, int64_t qld, int qheads, int64_t rows) {
+  if (!p || !q || rows < 1) return false;
+  const int64_t es = s->dtype == TSV_BF16 ? 2 : 4, w = (int64_t)heads * s->d * es, qw = (int64_t)qheads * s->d * es;
+  if (!meets(s, p, (rows - 1) * ld * es + w, q, qld, qheads, rows)) return false;
+  if (ld != qld || rows == 1) return true;
+  const int64_t stride = ld * es;
+  int64_t m = ((int64_t)(uintptr_t)q - (int64_t)(uintptr_t)p) % stride;
+  if (m < 0) m += stride;
+  return m < w || m + qw > stride;                       // (q's rows begin m bytes behind p's)
+}
+
 static int check_tok_cache(const tsv_tok_cache* c, const tsv_tok_shape* s) {
   if (!c || !c->L || !c->k) return TSV_ERR_NULL;
   if (!al(c->k, 16) || !al(c->v, 16)) return TSV_ERR_ALIGN;
@@ -108,6 +121,13 @@ int qk_norm_rope(const tsv_tok_shape* shape, const int32_t* L, const tsv_tok_bat
   if (rot < 0 || rot % 16 || first < 0 || first % 8 || first > shape->d - rot) return TSV_ERR_SHAPE;
   if (in->q && ((r = check_rows(shape, in->q, in->q_ld, shape->H)) || (r = check_rows(shape, q_out, ldq, shape->H)))) return r;
   if (in->k && ((r = check_rows(shape, in->k, in->k_ld, shape->Hk)) || (r = check_rows(shape, k_out, ldk, shape->Hk)))) return r;
+  const int64_t n = batch->rows;
+  const bool q = in->q && n, k = in->k && n;
+  // (an output may be its input, row by row; anything else of the call that it shares a row with would be read after it is written)
+  if (q && !(q_out == in->q && ldq == in->q_ld) && rows_meet(shape, q_out, ldq, shape->H, in->q, in->q_ld, shape->H, n)) return TSV_ERR_SHAPE;
+  if (k && !(k_out == in->k && ldk == in->k_ld) && rows_meet(shape, k_out, ldk, shape->Hk, in->k, in->k_ld, shape->Hk, n)) return TSV_ERR_SHAPE;
+  if (q && k && (rows_meet(shape, q_out, ldq, shape->H, in->k, in->k_ld, shape->Hk, n) || rows_meet(shape, k_out, ldk, shape->Hk, in->q, in->q_ld, shape->H, n) ||
+                 rows_meet(shape, q_out, ldq, shape->H, k_out, ldk, shape->Hk, n))) return TSV_ERR_SHAPE;
   return launch_rope(*shape, L, *batch, *in, wq, wk, eps, inv_freq, rot, first, pairs != 0, q_out, ldq, k_out, ldk, status, (cudaStream_t)stream);
 }
 

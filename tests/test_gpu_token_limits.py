@@ -306,3 +306,32 @@ def test_a_pool_of_layers_whose_table_names_pages_that_are_none(api):
     i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
     pg.pages_fork(pool, i32(0), i32(1), eng.caches[0].L, pg.alloc_workspace(pool), st)
     assert st.tolist() == [pg.ST_PAGE] and (table[1] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rope_among_column_ranges(api, dtype):
+    """Outputs in column ranges of the array that holds the inputs, in place and beside them, with the bits of outputs of their own; one row; and what
+    would share rows is refused."""
+    tsv, tk, _ = api
+    H, Hk, d, rows = 4, 2, 64, 70
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    shape = tk.TokenShape(dtype, 1, H, Hk, d, 1, max_L=1000, max_n=rows)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    L, st = torch.tensor([7], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    inv = (10000.0 ** -torch.arange(0, 1, 2 / 64, device="cuda")).float()
+    for n in (rows, 1):
+        batch = tk.TokenBatch(torch.zeros(1, dtype=torch.int64, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda"))
+        big = torch.randn(n, 2 * (H + Hk) * d, device="cuda", generator=gen).to(dt)
+        part = lambda a, heads: big[:, a * d:(a + heads) * d].unflatten(1, (heads, d))
+        q, k, q2, k2 = part(0, H), part(H, Hk), part(H + Hk, H), part(2 * H + Hk, Hk)
+        call = lambda *x: tk.qk_norm_rope(shape, L, batch, *x, None, None, 1e-6, inv, 0, False, st)
+        qo, ko = torch.empty(n, H, d, dtype=dt, device="cuda"), torch.empty(n, Hk, d, dtype=dt, device="cuda")
+        call(q, k, qo, ko)
+        call(q, k, q2, k2)
+        assert torch.equal(q2, qo) and torch.equal(k2, ko)
+        call(q, k, q, k)
+        assert torch.equal(q, qo) and torch.equal(k, ko) and not st.any()
+        for bad in ((q, k, part(1, H), k2), (q, k, part(H - 1, H), k2), (q, k, q2, part(H - 1, Hk)), (q, k, q2, part(H + Hk + 1, Hk))):
+            with pytest.raises(tsv.TsvError) as e:
+                call(*bad)
+            assert e.value.code == tsv.ERR_SHAPE

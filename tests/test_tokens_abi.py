@@ -334,3 +334,34 @@ def test_missing_arguments_and_other_ranks_are_refused(api, monkeypatch):
         with pytest.raises(tsv.TsvError):
             call()
             raise AssertionError(f"call {i} went through")
+
+
+def test_rope_outputs_over_other_rows_are_refused(api):
+    """Against marks of every element: any sharing but that of an output with its input at the same address and stride."""
+    tsv, tk, _ = api
+    a, s = C.addressof, _shape(tk, H=2, Hk=1, d=8)
+    n, es = 3, 2
+    batch = tk.CTokBatch(FAKE, FAKE, None, n)
+
+    def marks(base, ld, heads):
+        return {base + (r * ld + i) * es for r in range(n) for i in range(heads * 8)}
+    rng = np.random.default_rng(0)
+    refused = 0
+    for _ in range(1500):
+        ld = [int(x) * 8 for x in rng.integers(3, 6, 4)]
+        if rng.random() < 0.6:
+            ld = [ld[0]] * 4
+        base = [FAKE + 16 * int(x) for x in rng.integers(0, 24, 4)]
+        if rng.random() < 0.3:
+            base[2] = base[0]
+        if rng.random() < 0.3:
+            base[3] = base[1]
+        q, k, qo, ko = (marks(b, l, h) for b, l, h in zip(base, ld, (2, 1, 2, 1)))
+        own = lambda out, i: base[out] == base[i] and ld[out] == ld[i]
+        bad = (q & qo and not own(2, 0)) or (k & ko and not own(3, 1)) or (qo & k) or (ko & q) or (qo & ko)
+        if not bad:
+            continue
+        io = tk.CTokRows(base[0], base[1], None, ld[0], ld[1], 0)
+        assert tsv._lib.qk_norm_rope(a(s), FAKE, a(batch), a(io), None, None, 1e-6, None, 0, 0, 0, base[2], ld[2], base[3], ld[3], FAKE, None) == tsv.ERR_SHAPE, (base, ld)
+        refused += 1
+    assert refused > 500
