@@ -99,7 +99,10 @@ def _here(pool: PagePool) -> int:
 
 
 def _count(where: str, t: torch.Tensor) -> int:
-    return t.numel() if isinstance(t, torch.Tensor) else _bad(where, "an int32 tensor", t)
+    try:
+        return t.numel()
+    except AttributeError:
+        _bad(where, "an int32 tensor", t)
 
 
 def pages_assign(pool: PagePool, slots: torch.Tensor, first: torch.Tensor, last: torch.Tensor, workspace: torch.Tensor, status: torch.Tensor,

@@ -91,9 +91,12 @@ def _bad(where: str, expected: str, t) -> None:
 
 def _flat(where: str, t: torch.Tensor, dtype: torch.dtype, numel: int, dev: int) -> int:
     """Pointer of a contiguous tensor of at least `numel` elements on device dev."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or t.get_device() != dev:
-        _bad(where, f"a contiguous {dtype} tensor of {numel} elements", t)
-    return t.data_ptr()
+    try:                                      # (what is no tensor has no dtype: asking it first takes a microsecond a call)
+        if t.dtype is dtype and t.numel() >= numel and t.is_contiguous() and t.get_device() == dev:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _bad(where, f"a contiguous {dtype} tensor of {numel} elements", t)
 
 
 def _maybe(where: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, dev: int) -> int:
@@ -104,31 +107,40 @@ def _table(where: str, t: Optional[torch.Tensor], rows: int, dev: int):
     """Pointer and row length of an int32 table of at least `rows` rows; (0, 0) for None."""
     if t is None:
         return 0, 0
-    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+    try:
+        _, ld = t.shape
+    except (AttributeError, ValueError):
         _bad(where, f"an int32 tensor of {rows} rows", t)
-    return _flat(where, t, _i32, rows * t.shape[1], dev), t.shape[1]
+    return _flat(where, t, _i32, rows * ld, dev), ld
 
 
 def _workspace(workspace: torch.Tensor, dev: int):
-    if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev:
-        _bad("workspace", "a workspace", workspace)
-    return _aligned(workspace)
+    try:
+        if workspace.get_device() == dev:
+            return _aligned(workspace)
+    except AttributeError:
+        pass
+    _bad("workspace", "a workspace", workspace)
 
 
 def _vectors(where: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, d: int, dev: int):
     """Pointer and row stride of a [>= rows, heads, d] tensor whose heads follow each other in a row."""
-    s = t.shape if isinstance(t, torch.Tensor) else ()
-    if s and t.dtype is dtype and len(s) == 3 and s[0] >= rows and s[1] == heads and s[2] == d and t.get_device() == dev:
-        ld, hs, es = t.stride()
-        if es == 1 and (hs == d or heads == 1):
-            return t.data_ptr(), (ld if s[0] > 1 else heads * d)
+    try:
+        s = t.shape
+        if t.dtype is dtype and len(s) == 3 and s[0] >= rows and s[1] == heads and s[2] == d and t.get_device() == dev:
+            ld, hs, es = t.stride()
+            if es == 1 and (hs == d or heads == 1):
+                return t.data_ptr(), (ld if s[0] > 1 else heads * d)
+    except AttributeError:
+        pass
     _bad(where, f"a {dtype} tensor [{rows}, {heads}, {d}] whose rows are contiguous", t)
 
 
 def _rows(where: str, t: torch.Tensor) -> int:
-    if not isinstance(t, torch.Tensor) or not t.dim():
+    try:
+        return t.shape[0]
+    except (AttributeError, IndexError):
         _bad(where, "a tensor of rows", t)
-    return t.shape[0]
 
 
 @dataclass
