@@ -319,10 +319,16 @@ int tree_verify_attn_static(const tsv_shape *shape, const tsv_cache *cache, cons
  * New tokens are PACKED: those of sequence b are rows row0[b] .. row0[b] + n[b] - 1 of every [rows][...] array, in order
  * of their positions (a chain: token i is at position L[b] + i) or, with `parent`, as the nodes of a draft tree (node i is
  * at L[b] + its depth; parent before child).  n[b] may be 0; the ranges of two sequences must not overlap.  Rows of no
- * sequence are not written and have no influence; with rows = 0 the arrays may be NULL.  A sequence with a problem that
- * the device sees (n[b] outside 0..max_n or rows outside 0..rows: TSV_ST_NODES; a bad parent array, or a tree of more
- * than TSV_MAX_D nodes: TSV_ST_PARENT; L[b] < 0 or L[b] + n[b] > max_L: TSV_ST_LENGTH) gets zeros in its output rows,
- * where those are inside 0..rows, and commits nothing.
+ * sequence are not written and have no influence; with rows = 0 the arrays may be NULL.  What the device finds wrong
+ * with a sequence:
+ *   TSV_ST_NODES     n[b] outside 0..max_n, or rows outside 0..rows: it counts as a sequence without rows, so what it names
+ *                    as its output rows is left as it was
+ *   TSV_ST_LENGTH    L[b] < 0 or L[b] + n[b] > max_L: zeros in its output rows (without rows only token_commit flags it)
+ *   TSV_ST_PARENT    a bad parent array, or a tree of more than TSV_MAX_D nodes: zeros in its output rows.  token_commit
+ *                    does not look at parents: `path` says what it takes, and status[b] of the calls before stops it
+ *   TSV_ST_INTERNAL  a wait gave up (window_sink_attn sets it for all sequences of the call): output rows hold anything
+ * A sequence with one of them commits nothing (TSV_ST_INTERNAL of a commit: L stays, cache rows behind it may be written).
+ * Sums are fp32: a score q.k that is beyond its range counts as infinite.
  * ====================================================================================================================== */
 
 /* HOST memory.  Supported: B <= 2^20, H a multiple of Hk, H <= 256, d a multiple of 8, 8 <= d <= 512, window >= 1, n_sink >= 0. */

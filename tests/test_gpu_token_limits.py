@@ -335,3 +335,25 @@ def test_rope_among_column_ranges(api, dtype):
             with pytest.raises(tsv.TsvError) as e:
                 call(*bad)
             assert e.value.code == tsv.ERR_SHAPE
+
+
+@pytest.mark.parametrize("n", [[5, 4], [5, 70]])
+def test_commit_does_not_look_at_parents(api, n):
+    """As the header says: the path decides; a flag of an earlier call of the same tokens stops the sequence."""
+    tsv, tk, _ = api
+    for flagged in (False, True):
+        lay = Layer(tk, "bf16", 2, 2, 64, False, window=10, sinks=1, L=[4, 9], n=n, page=4, seed=2)
+        par = torch.full((lay.rows,), 7, dtype=torch.int32, device="cuda")
+        batch = tk.TokenBatch(lay.batch.row0, lay.batch.n, par)
+        path, count = torch.tensor([[0, 2, 4, -1], [0, 1, 3, 2]], dtype=torch.int32, device="cuda"), torch.tensor([3, 4], dtype=torch.int32, device="cuda")
+        if flagged:
+            tk.qk_norm_rope(lay.shape, lay.cache.L, batch, lay.q, None, lay.q.clone(), None, None, None, 1e-6, None, 0, False, lay.status)
+            assert lay.status.tolist() == [tsv.ST_PARENT] * 2
+        before = lay.cache.k.clone()
+        tk.token_commit(lay.shape, lay.cache, batch, lay.k, lay.v, lay.status, path=path, count=count)
+        assert lay.status.tolist() == [tsv.ST_PARENT * flagged] * 2 and lay.cache.L.tolist() == ([4, 9] if flagged else [7, 13])
+        for b, nodes in enumerate([[0, 2, 4], [0, 1, 3, 2]]):
+            pos = np.arange(lay.L[b], lay.L[b] + len(nodes))
+            at = torch.from_numpy(lay.table[b][pos // 4].astype(np.int64) * 4 + pos % 4).cuda()
+            want = before[at] if flagged else lay.k[[lay.row0[b] + i for i in nodes]]
+            assert torch.equal(lay.cache.k[at].nan_to_num(9), want.nan_to_num(9))
