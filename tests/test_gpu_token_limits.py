@@ -357,3 +357,55 @@ def test_commit_does_not_look_at_parents(api, n):
             at = torch.from_numpy(lay.table[b][pos // 4].astype(np.int64) * 4 + pos % 4).cuda()
             want = before[at] if flagged else lay.k[[lay.row0[b] + i for i in nodes]]
             assert torch.equal(lay.cache.k[at].nan_to_num(9), want.nan_to_num(9))
+
+
+
+@pytest.mark.parametrize("heads", [("bf16", 64, 1, 512, True), ("bf16", 8, 2, 128, False), ("fp32", 16, 1, 128, True)], ids=lambda h: "_".join(map(str, h)))
+@pytest.mark.parametrize("n", [[3, 140], [1, 2]])
+def test_a_replay_at_other_lengths(api, heads, n):
+    """A captured call replayed at other lengths, shorter and longer ones, has the bits of a call made at them."""
+    _, tk, _ = api
+    lay = Layer(tk, *heads, window=600, sinks=3, L=[700, 20], n=n, page=64, seed=1)
+    lay.cache.k.nan_to_num_(0.5)                          # (rows of the pages that the captured lengths do not reach)
+    if lay.cache.v is not None:
+        lay.cache.v.nan_to_num_(0.5)
+    ws, out = tk.alloc_workspace(lay.shape, lay.rows), torch.zeros(lay.rows, *lay.q.shape[1:], dtype=lay.q.dtype, device="cuda")
+    call = lambda o, st: tk.window_sink_attn(lay.shape, lay.cache, lay.batch, lay.q, lay.k, lay.v, o, ws, st)
+    call(out, lay.status)
+    g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        call(out, lay.status)
+    for L in ([25, 20], [0, 1], [640, 22], [700, 20]):
+        lay.cache.L.copy_(torch.tensor(L, dtype=torch.int32))
+        out.zero_()
+        g.replay()
+        want = torch.zeros_like(out)
+        call(want, lay.status)
+        torch.cuda.synchronize()
+        assert torch.equal(out.nan_to_num(9), want.nan_to_num(9)) and not lay.status.any()
+
+
+@pytest.mark.parametrize("heads", [("bf16", 8, 2, 64, False), ("bf16", 8, 1, 512, True), ("fp32", 4, 1, 64, True), ("bf16", 16, 1, 128, False), ("bf16", 8, 1, 256, False)],
+                         ids=lambda h: "_".join(map(str, h)))
+@pytest.mark.parametrize("n", [6, 150])
+def test_rows_that_see_an_infinite_value(api, heads, n):
+    """An infinity in a value, and a score with it (without values of their own): what stays finite is within the bounds of any other result."""
+    _, tk, _ = api
+    for bad in (float("inf"), -float("inf")):
+        lay = Layer(tk, *heads, window=40, sinks=1, L=[20, 0], n=[n, 3], seed=n)
+        if lay.v is None:
+            lay.k[lay.row0[0] + n // 2, -1, 1] = bad
+        else:
+            lay.v[lay.row0[0] + n // 2, :, 3] = bad
+        got = f64(lay.run(tk))[lay.row0[0]:lay.row0[0] + n]
+        ref, mag, reach = lay.ref(0)
+        ok = np.isfinite(ref)
+        assert (ok == np.isfinite(got)).all() and ok.any() and not ok.all()
+        es, d = 2.0 ** -8 if heads[0] == "bf16" else 2.0 ** -24, heads[3]
+        with np.errstate(all="ignore"):
+            # (a row whose score of the key is -infinity gives it no weight, and its bound comes from the others: at most the largest of them)
+            top = np.where(np.isfinite(mag), mag, 0) if lay.v is not None else np.full_like(ref, np.abs(f64(lay.k)[np.isfinite(f64(lay.k))]).max())
+            far = np.where(np.isfinite(reach), reach, np.nanmax(np.where(np.isfinite(reach), reach, 0)))
+            tol = es * np.abs(ref) + top * (2.0 ** -8 if heads[0] == "bf16" else 2.0 ** -20) + top * 2 * ((d + 4) * 2.0 ** -24 * far)[..., None] + 1e-30
+            assert (np.abs(got - ref) <= tol)[ok].all()
