@@ -383,8 +383,7 @@ int launch_copies(const tsv_page_pool& p, const Work& w, bool rows, int64_t most
       a.base[i] = reinterpret_cast<char*>(x.base); a.bytes[i] = x.bytes; a.chunk0[i] = (int32_t)chunks;
       chunks += (x.bytes + kChunk - 1) / kChunk;
     }
-    if (chunks > 0x7fffffff) return TSV_ERR_LIMIT;
-    a.chunk0[a.n] = (int32_t)chunks;
+    a.chunk0[a.n] = (int32_t)chunks;                        // (at most 2^16 of each array: check_pool)
     int64_t grid = most_pairs * chunks;
     if (renumber && grid < 32) grid = 32;
     if (grid > 148 * kCopyCtas) grid = 148 * kCopyCtas;

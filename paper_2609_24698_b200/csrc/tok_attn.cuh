@@ -90,7 +90,6 @@ __device__ __forceinline__ TileList make_list(const AttnArgs& a, int64_t item, i
   t.lo = max(0, (a.bt.parent ? t.L : t.p0) - a.s.window + 1);
   t.ns = min(a.s.n_sink, t.lo);
   t.nc = t.ns + (a.bt.parent ? t.L : t.p1 + 1) - t.lo;
-  if (a.bt.parent && t.lo > t.L) t.nc = t.ns;              // (window 1)
   t.nk = t.nc + (a.bt.parent ? t.n : 0);
   return t;
 }

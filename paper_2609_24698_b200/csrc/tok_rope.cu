@@ -35,8 +35,9 @@ struct RopeArgs {
   int32_t* status;
 };
 
-// The angle is exact as a product of a 30-bit and a 24-bit number in fp64; whole turns are taken off there too (what is left has
-// an error of some 2^-53 of the turns, 2^-25 at positions of 2^30), and only the rest of at most half a turn goes on in fp32.
+// The angle in turns is made in fp64: a rounding of the product of a 30-bit and a 24-bit number, one of 1 / (2 pi) and one of the product with
+// it, at most 3 x 2^-53 of the turns (position 2^30, frequency 1: 2^27.3 turns, 2^-24 of a turn).  Whole turns are taken off there too,
+// and only the rest of at most half a turn goes on in fp32.
 __device__ __forceinline__ float2 cos_sin(int pos, float freq) {
   double turns = (double)pos * (double)freq * 0.15915494309189533576888;
   turns -= rint(turns);
@@ -338,8 +339,7 @@ int launch_rope(const tsv_tok_shape& s, const int32_t* L, const tsv_tok_batch& b
   while (a.parts < most && rows * a.parts * 2 <= warps) a.parts *= 2;
   const int64_t share = (rows * a.parts + warps - 1) / warps;
   a.tokens = (int32_t)(share < 1 ? 1 : share);
-  const int64_t chunks = rows / a.tokens + 1;               // (one behind the last token: it looks at every sequence)
-  if (chunks * a.parts > (int64_t)0x7fffffff * kRopeWarps) return TSV_ERR_LIMIT;
+  const int64_t chunks = rows / a.tokens + 1;               // (one behind the last token: it looks at every sequence; no more than about `warps`)
   const dim3 grid((unsigned)((chunks * a.parts + kRopeWarps - 1) / kRopeWarps));
   const int smem = kRopeWarps * (rot / 2) * (int)sizeof(float2);
   if (s.dtype == TSV_BF16) return rope_launch<bf16, 1>(a, grid, smem, st);
