@@ -328,7 +328,7 @@ int tree_verify_attn_static(const tsv_shape *shape, const tsv_cache *cache, cons
  *                    does not look at parents: `path` says what it takes, and status[b] of the calls before stops it
  *   TSV_ST_INTERNAL  a wait gave up (window_sink_attn sets it for all sequences of the call): output rows hold anything
  * A sequence with one of them commits nothing (TSV_ST_INTERNAL of a commit: L stays, cache rows behind it may be written).
- * Sums are fp32: a score q.k that is beyond its range counts as infinite.
+ * Sums are fp32: a score q.k that is beyond its range counts as infinite, a weight below 2^-125 of the row's largest as zero.
  * ====================================================================================================================== */
 
 /* HOST memory.  Supported: B <= 2^20, H a multiple of Hk, H <= 256, d a multiple of 8, 8 <= d <= 512, window >= 1, n_sink >= 0. */

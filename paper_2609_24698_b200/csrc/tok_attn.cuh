@@ -101,15 +101,16 @@ __device__ __forceinline__ TileList make_list(const AttnArgs& a, int64_t item, i
 //
 // One row, by one warp: keys k0 .. k1 - 1 of the list, what the row does not see skipped altogether.  Returns whether a score or a
 // value that it sees is not finite.  m in units of log2; o[i]: dims lane + 32 i, with weights that add up to one, which no sum of finite
-// values leaves the range by; l: the sum of weights at the maximum m, NEGATIVE as a mark that o is divided by it.  (m stays -inf, l and o
-// zero, where every score seen is -inf.)
+// values leaves the range by; l: the sum of weights at the maximum m, NEGATIVE as a mark that o is divided by it.  Where nothing is seen m is
+// -inf, l and o zero.  Where every score seen is -inf, the weights are 0 / 0 if these are all keys of the row (l NaN); in a share of them the
+// others decide the weights of these, zero, which leave what is not finite NaN (m -inf, l -1, o the values times zero).
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
 template <typename T>
 __device__ __noinline__ bool exact_row(const AttnArgs& a, const TileList& t, const int* depth, const T* q, int p, uint32_t anc, int k0, int k1,
                                        float& m, float& l, float* o) {
   const int lane = threadIdx.x & 31, d = a.s.d;
   m = -INFINITY; l = 0.f;
-  bool nan = false, saw = false;
+  bool nan = false, saw = false, any = false;
 #pragma unroll
   for (int i = 0; i < 16; ++i) o[i] = 0.f;
   float inv = 0.f;
@@ -123,13 +124,13 @@ __device__ __noinline__ bool exact_row(const AttnArgs& a, const TileList& t, con
       for (int e = lane; e < d; e += 32) x = fmaf(to_f(q[e]), to_f(k[e]), x);
       x = warp_sum(x) * a.scale2;
       if (pass == 0) {
-        nan |= isnan(x); saw |= !is_finite(x);
+        any = true; nan |= isnan(x); saw |= !is_finite(x);
         const float to = fmaxf(m, x);
         if (to != -INFINITY) l = l * exp2f(m - to) + exp2f(x - to);
         m = to;
         continue;
       }
-      const float w = exp2f(x - m) * inv;
+      const float w = m == -INFINITY ? 0.f : exp2f(x - m) * inv;
       const T* v = row_ptr<T>(a, t.hk, code, true);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
@@ -141,10 +142,7 @@ __device__ __noinline__ bool exact_row(const AttnArgs& a, const TileList& t, con
     }
     inv = 1.f / l;
   }
-  if (m == -INFINITY && !nan) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[i] = 0.f;
-  }
+  if (m == -INFINITY && any) l = a.nsplit == 1 ? NAN : 1.f;
   l = nan ? NAN : -l;
   return __any_sync(0xffffffffu, saw);
 }

@@ -409,3 +409,27 @@ def test_rows_that_see_an_infinite_value(api, heads, n):
             far = np.where(np.isfinite(reach), reach, np.nanmax(np.where(np.isfinite(reach), reach, 0)))
             tol = es * np.abs(ref) + top * (2.0 ** -8 if heads[0] == "bf16" else 2.0 ** -20) + top * 2 * ((d + 4) * 2.0 ** -24 * far)[..., None] + 1e-30
             assert (np.abs(got - ref) <= tol)[ok].all()
+
+
+# a share of split keys, joined in a cluster or afterwards, that holds nothing but keys with an infinite value, which no other share has
+@pytest.mark.parametrize("heads,L,first,last", [
+    (("bf16", 16, 1, 64, True), 500, 128, 192), (("bf16", 16, 1, 512, True), 1200, 320, 480), (("bf16", 16, 1, 128, True), 9000, 2048, 2560),
+    (("bf16", 8, 1, 512, True), 17000, 2640, 3168), (("bf16", 24, 1, 128, True), 6000, 1024, 1536), (("fp32", 16, 1, 72, True), 500, 128, 192),
+    (("fp32", 4, 1, 512, True), 9000, 2048, 2560), (("fp32", 16, 1, 128, True), 64, 63, 64)], ids=str)
+def test_shares_of_infinite_keys(api, heads, L, first, last):
+    """Rows whose score of those keys is -infinity give them no weight, and 0 times infinity is NaN in that column alone; where it is +infinity, all is."""
+    _, tk, _ = api
+    lay = Layer(tk, *heads, window=20000, sinks=0, L=[L], n=[1], page=64, seed=4)
+    k = lay.hist_k[0].clone()
+    k[first:last, :, 3] = float("inf")
+    set_history(lay, 0, k, k)
+    lay.q[:, ::2, 3] = -lay.q[:, ::2, 3].abs() - 0.1
+    lay.q[:, 1::2, 3] = lay.q[:, 1::2, 3].abs() + 0.1
+    got = f64(lay.run(tk))[lay.row0[0]]
+    ref, mag, _ = lay.ref(0)
+    ref, mag = ref[0], mag[0]
+    assert np.isnan(ref[::2, 3]).all() and np.isfinite(np.delete(ref[::2], 3, 1)).all() and np.isnan(ref[1::2]).all()
+    assert (np.isnan(got) == np.isnan(ref)).all() and not np.isinf(got).any() and not lay.status.any()
+    ok = np.isfinite(ref)
+    # (a rounding of each weight, of the result, and of fp32 sums)
+    assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 1e-3) * mag)[ok].all()
