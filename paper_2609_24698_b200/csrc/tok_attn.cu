@@ -83,7 +83,7 @@ struct TileCtl {
   int pos[kRows];
   uint32_t row_anc[kRows];
   TileList t;
-  uint32_t bad, still;                // rows with a result that is not finite, after the first pass and after the second
+  uint32_t bad[2];                    // rows with a result that is not finite, after the first pass and after the second
 };
 
 // The tile of this CTA; false (alike in all CTAs of a cluster) where there is nothing to attend to.
@@ -91,7 +91,7 @@ template <typename T>
 __device__ __forceinline__ bool begin_tile(const AttnArgs& a, TileCtl& sm) {
   if (threadIdx.x < 32) {
     const TileList t = make_list(a, blockIdx.x, blockIdx.y, kRows, sm.depth, sm.anc);
-    if (threadIdx.x == 0) { sm.t = t; sm.bad = 0; sm.still = 0; }
+    if (threadIdx.x == 0) { sm.t = t; sm.bad[0] = sm.bad[1] = 0; }
   }
   __syncthreads();
   const TileList& t = sm.t;
@@ -109,31 +109,53 @@ __device__ __forceinline__ bool begin_tile(const AttnArgs& a, TileCtl& sm) {
 }
 
 // From o [16][ld] and sm.ml in shared memory, written by this CTA before, to the output: through the partial outputs, or at once, the
-// shares of a cluster's CTAs joined in order.  Rows of sm.bad that see something not finite, and those of sm.still, are computed by
+// shares of a cluster's CTAs joined in order.  Rows of sm.bad[0] that see something not finite, and those of sm.bad[1], are computed by
 // definition first.
 __device__ __forceinline__ bool all_finite(const float4& x) { return is_finite(x.x) && is_finite(x.y) && is_finite(x.z) && is_finite(x.w); }
-// Four values joined from a cluster's shares whose sum is not finite: with weights that add up to one what is finite stays so.  l becomes 1.
-__device__ __noinline__ void join_again(float4& x, float& l, float m, int shares, uint32_t ml_at, uint32_t o_at) {
+// Four values joined from a cluster's shares with weights that add up to one: what is finite stays so.  Out of line, for shares of which one is
+// divided by its sum (l < 0), or whose plain sum is not finite.
+__device__ __noinline__ float4 join_again(float m, int shares, uint32_t ml_at, uint32_t o_at) {
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < shares; ++s) {
-    const float2 ml = ld_rank2(at_rank(ml_at, s));
-    const float4 v = ld_rank4(at_rank(o_at, s));
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;
-    const float w = exp2f(ml.x - m) / l * (ml.y < 0.f ? -ml.y : 1.f);
-    y.x = fmaf(v.x, w, y.x); y.y = fmaf(v.y, w, y.y); y.z = fmaf(v.z, w, y.z); y.w = fmaf(v.w, w, y.w);
-  }
-  if (all_finite(y)) { x = y; l = 1.f; }
+  float l = 0.f;
+  for (int pass = 0; pass < 2; ++pass)
+    for (int s = 0; s < shares; ++s) {
+      const float2 ml = ld_rank2(at_rank(ml_at, s));
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;
+      float w = exp2f(ml.x - m);
+      if (pass == 0) { l = fmaf(fabsf(ml.y), w, l); continue; }
+      const float4 v = ld_rank4(at_rank(o_at, s));
+      w = w / l * (ml.y < 0.f ? -ml.y : 1.f);
+      y.x = fmaf(v.x, w, y.x); y.y = fmaf(v.y, w, y.y); y.z = fmaf(v.z, w, y.z); y.w = fmaf(v.w, w, y.w);
+    }
+  return y;
+}
+// The same of partial outputs in memory: the shares' o at po, `stride` floats apart, their {m, l} in the lanes (h: share lane + 32 h).
+__device__ __noinline__ float4 join_parts_again(const float* po, size_t stride, bool live, int shares, float w0, float w1, float l0, float l1) {
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+  for (int pass = 0; pass < 2; ++pass)
+    for (int s = 0; s < shares; ++s) {
+      float w = __shfl_sync(0xffffffffu, s < 32 ? w0 : w1, s & 31);
+      const float ls = __shfl_sync(0xffffffffu, s < 32 ? l0 : l1, s & 31);
+      if (w == -1.f) continue;
+      if (pass == 0) { l = fmaf(fabsf(ls), w, l); continue; }
+      if (!live) continue;
+      const float4 v = *reinterpret_cast<const float4*>(po + s * stride);
+      w = w / l * (ls < 0.f ? -ls : 1.f);
+      y.x = fmaf(v.x, w, y.x); y.y = fmaf(v.y, w, y.y); y.z = fmaf(v.z, w, y.z); y.w = fmaf(v.w, w, y.w);
+    }
+  return y;
 }
 template <typename T>
 __device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* o, int ld, int k0, int k1) {
   const TileList& t = sm.t;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, d = a.s.d;
   __syncthreads();
-  if (sm.bad) {
+  if (sm.bad[0]) {
     for (int r = warp; r < t.nr; r += kThreads / 32) {
-      if (!(sm.bad >> r & 1u)) continue;
+      if (!(sm.bad[0] >> r & 1u)) continue;
       float m, l, x[16];
-      if (!exact_row<T>(a, t, sm.depth, query_row<T>(a, t, r), sm.pos[r], sm.row_anc[r], k0, k1, m, l, x) && !(sm.still >> r & 1u)) continue;
+      if (!exact_row<T>(a, t, sm.depth, query_row<T>(a, t, r), sm.pos[r], sm.row_anc[r], k0, k1, m, l, x) && !(sm.bad[1] >> r & 1u)) continue;
 #pragma unroll
       for (int i = 0; i < 16; ++i) if (lane + 32 * i < d) o[r * ld + lane + 32 * i] = x[i];
       if (lane == 0) sm.ml[r] = make_float2(m, l);
@@ -163,7 +185,7 @@ __device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* 
     } else {
       float2 ml[8];
       float4 v[8];
-      float m = -INFINITY;
+      float m = -INFINITY, least = 0.f;
 #pragma unroll
       for (int s = 0; s < 8; ++s)
         if (s < shares) {
@@ -174,12 +196,15 @@ __device__ __forceinline__ void end_tile(const AttnArgs& a, TileCtl& sm, float* 
 #pragma unroll
       for (int s = 0; s < 8; ++s)
         if (s < shares && !(ml[s].x == -INFINITY && ml[s].y == 0.f)) {           // (else nothing seen)
-          float w = exp2f(ml[s].x - m);
-          l = fmaf(fabsf(ml[s].y), w, l);
-          if (ml[s].y < 0.f) w *= -ml[s].y;
+          const float w = exp2f(ml[s].x - m);
+          l = fmaf(ml[s].y, w, l);
+          least = fminf(least, ml[s].y);
           x.x = fmaf(v[s].x, w, x.x); x.y = fmaf(v[s].y, w, x.y); x.z = fmaf(v[s].z, w, x.z); x.w = fmaf(v[s].w, w, x.w);
         }
-      if (!all_finite(x) && l > 0.f && is_finite(l)) join_again(x, l, m, shares, ml_at + r * 8, o_at + (r * ld + c) * 4);
+      if (least < 0.f || (!all_finite(x) && l > 0.f && is_finite(l))) {
+        const float4 y = join_again(m, shares, ml_at + r * 8, o_at + (r * ld + c) * 4);
+        if (least < 0.f || all_finite(y)) { x = y; l = 1.f; }
+      }
     }
     const float inv = 1.f / l;
     T* out = out_row<T>(a, t, r) + c;
@@ -239,8 +264,10 @@ struct MmaSmem {
   int missing[ST + 1][2];             // a key of the block has no page (32 keys each)
 };
 
+// (Shared memory leaves one to three CTAs an SM, so a thread may have more than the 128 registers at which the compiler stops by itself, and
+// spills: single tokens of 8 sequences, 32 heads on 8 x 128, 32 k keys, warm 236 us; 218 with as many as it wants.)
 template <int DP, bool SHARED>
-__global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) attn_mma_kernel(const AttnArgs a) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   typedef MmaSmem<DP, SHARED> Sm;
   Sm& sm = *reinterpret_cast<Sm*>(smem_raw);
@@ -487,7 +514,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
       m[h] = mn;
       if (warp == 0 && tc == 0) sm.c.ml[r] = make_float2(m[h], l[h]);
       const bool bad = !is_finite(l[h]) || (m[h] == -INFINITY && a.nsplit == 1);
-      if (bad && r < t.nr) atomicOr(pass ? &sm.c.still : &sm.c.bad, 1u << r);
+      if (bad && r < t.nr) atomicOr(sm.c.bad + pass, 1u << r);
 #pragma unroll
       for (int i = 0; i < CT; ++i) *reinterpret_cast<float2*>(os + (warp * kRows + r) * DP + i * 8 + 2 * tc) = make_float2(o[i][2 * h] * part[h], o[i][2 * h + 1] * part[h]);
     }
@@ -500,7 +527,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
         x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
       }
       const int r = 4 * i / DP;
-      if (r < t.nr && !all_finite(x)) atomicOr(pass ? &sm.c.still : &sm.c.bad, 1u << r);
+      if (r < t.nr && !all_finite(x)) atomicOr(sm.c.bad + pass, 1u << r);
       *reinterpret_cast<float4*>(os + 4 * i) = x;
     }
   } else
@@ -515,11 +542,11 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const AttnArgs a) {
       bad |= !is_finite(o[i][2 * h]) || !is_finite(o[i][2 * h + 1]);
       *reinterpret_cast<float2*>(os + r * DP + warp * CW + i * 8 + 2 * tc) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
     }
-    if (bad && r < t.nr) atomicOr(pass ? &sm.c.still : &sm.c.bad, 1u << r);
+    if (bad && r < t.nr) atomicOr(sm.c.bad + pass, 1u << r);
     if (warp == 0 && tc == 0) sm.c.ml[r] = make_float2(m[h], l[h]);
   }
   __syncthreads();
-  if (!sm.c.bad) break;
+  if (!sm.c.bad[0]) break;
   }
   end_tile<bf16>(a, sm.c, reinterpret_cast<float*>(sm.k), DP, k0, k1);
 }
@@ -656,10 +683,10 @@ __global__ void __launch_bounds__(kThreads) attn_fp32_kernel(const AttnArgs a, c
 #pragma unroll
     for (int c = 0; c < NC; ++c) bad |= !is_finite(o[c][r]);
     if (tid == 0) sm.c.ml[r] = make_float2(sm.m[r], l);
-    if (bad) atomicOr(again ? &sm.c.bad : &sm.c.still, 1u << r);
+    if (bad) atomicOr(sm.c.bad + pass, 1u << r);
   }
   __syncthreads();
-  if (!sm.c.bad || !again) {                              // (Q's place: it is not read any more)
+  if (!sm.c.bad[0] || !again) {                              // (Q's place: it is not read any more)
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -705,43 +732,30 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a, c
     for (int h = 0; h < 2; ++h) w[h] = ml[h].x == -INFINITY && ml[h].y == 0.f ? -1.f : exp2f(ml[h].x - m);      // (-1: nothing seen)
     float l = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    // (a second time where a sum is not finite, with weights that add up to one: what is finite stays so)
-    float by = 1.f, div = 1.f;
-    float4 first = x;
-#pragma unroll 1
-    for (bool again = false;; again = true) {
-      l = 0.f;
-      x = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
-        float4 v[8];
+    for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
+      float4 v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (s0 + k < a.nsplit && col < d) v[k] = *reinterpret_cast<const float4*>(a.po + (base + (size_t)(s0 + k) * per) * d + col);
-        }
+      for (int k = 0; k < 8; ++k) {
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s0 + k < a.nsplit && col < d) v[k] = *reinterpret_cast<const float4*>(a.po + (base + (size_t)(s0 + k) * per) * d + col);
+      }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float ws = __shfl_sync(0xffffffffu, s0 + k < 32 ? w[0] : w[1], (s0 + k) & 31);
-          const float ls = __shfl_sync(0xffffffffu, s0 + k < 32 ? ml[0].y : ml[1].y, (s0 + k) & 31);
-          if (s0 + k >= a.nsplit || ws == -1.f) continue;
-          ws *= by;
-          l = fmaf(fabsf(ls), ws, l);
-          if (ls < 0.f) ws *= -ls;
-          x.x = fmaf(v[k].x, ws, x.x); x.y = fmaf(v[k].y, ws, x.y); x.z = fmaf(v[k].z, ws, x.z); x.w = fmaf(v[k].w, ws, x.w);
-        }
+      for (int k = 0; k < 8; ++k) {
+        const float ws = __shfl_sync(0xffffffffu, s0 + k < 32 ? w[0] : w[1], (s0 + k) & 31), ls = __shfl_sync(0xffffffffu, s0 + k < 32 ? ml[0].y : ml[1].y, (s0 + k) & 31);
+        if (s0 + k >= a.nsplit || ws == -1.f) continue;
+        l = fmaf(ls, ws, l);
+        x.x = fmaf(v[k].x, ws, x.x); x.y = fmaf(v[k].y, ws, x.y); x.z = fmaf(v[k].z, ws, x.z); x.w = fmaf(v[k].w, ws, x.w);
       }
-      if (again) {
-        if (all_finite(first) || !all_finite(x)) x = first; else div = 1.f;
-        break;
-      }
-      div = l;                                            // (the same in all lanes)
-      if (!(l > 0.f && is_finite(l) && __any_sync(0xffffffffu, !all_finite(x)))) break;
-      first = x;
-      by = 1.f / l;
+    }
+    const bool divided = ml[0].y < 0.f || ml[1].y < 0.f;
+    if (__any_sync(0xffffffffu, divided || !all_finite(x))) {      // (nearly never; then by all lanes alike)
+      const bool must = __any_sync(0xffffffffu, divided);
+      const float4 y = join_parts_again(a.po + base * d + col, (size_t)per * d, col < d, a.nsplit, w[0], w[1], ml[0].y, ml[1].y);
+      if (must || (!all_finite(x) && l > 0.f && is_finite(l) && all_finite(y))) { x = y; l = 1.f; }
     }
     if (col < d) {
       T* out = out_row<T>(a, t, r) + col;
-      out[0] = from_f<T>(x.x / div); out[1] = from_f<T>(x.y / div); out[2] = from_f<T>(x.z / div); out[3] = from_f<T>(x.w / div);
+      out[0] = from_f<T>(x.x / l); out[1] = from_f<T>(x.y / l); out[2] = from_f<T>(x.z / l); out[3] = from_f<T>(x.w / l);
     }
   }
 }
