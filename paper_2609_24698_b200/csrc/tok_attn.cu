@@ -239,9 +239,9 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 // ---------------------------------------------------------------- bf16, 16 rows
 // Four warps, blocks of KB keys.  d <= 128: a quarter of a block's keys is a warp's own from the scores to the output (16 rows x 128 columns
 // are 64 registers), with its own maxima and sums; the warps are joined at the end, and a block has one barrier.  (Through shared memory, as
-// below: 8 sequences of 32 heads on 8 x 128, 32 k keys, 366 us instead of 277.)  Beyond, where one warp's registers do not hold all of d:
+// below: 8 sequences of 32 heads on 8 x 128, 32 k keys, 366 us instead of 277, at that step.)  Beyond, where one warp's registers do not hold all of d:
 // each computes the scores of a quarter of the keys, the row maxima go through shared memory, then each adds the whole block's P V to
-// its quarter of the output columns.  P is rounded to bf16 for the product (half a step, 2^-9, of a weight; the sum of the weights is of
+// its quarter of the output columns.  P is rounded to bf16 for the product (half a step, at most 2^-8 of a weight; the sum of the weights is of
 // the unrounded ones); scores, maxima, sums and the output are fp32.  Rows of K and V come by 16-byte asynchronous copies, ST - 1 blocks
 // ahead of the arithmetic (a window of 32 k tokens streams from HBM: that much has to be under way), through the page table or from the
 // new rows, whose addresses are worked out a block before their copies: 16-byte chunks of a row are stored at chunk ^ (row & 7), which
@@ -805,7 +805,8 @@ struct AttnPlan {
 // 32 k): d = 64 and 128 shared 17 / 15 to 97 / 72, the larger ones of 32 on 8 x 128 and of d above 128 the other way about, 135 / 160.
 // Above d = 128 also where there are 64 tiles and more, or lists of 16 k keys: 16 heads x 512, 256 sequences, window 128 42 / 55, 64 of 2048
 // 81 / 91, one of 32 k 56 / 60, but eight of 2048 38 / 34; 8 heads on 8 x 256, 64 of 2048 201 / 296, eight of 32 k 364 / 932; the worst found
-// was 2 heads x 512 with values of their own, eight of 32 k 216 / 185.
+// was 2 heads x 512 with values of their own, eight of 32 k 216 / 185.  (Cold, and before the kernel of tiles of 16
+// had all its registers, which took up to a seventh off its times.)
 int64_t keys_of(const tsv_tok_shape& s) {                 // of a list, at most
   const int64_t reach = std::min<int64_t>((int64_t)s.window + s.max_n, s.max_L);
   return reach + std::min<int64_t>(s.n_sink, s.max_L);
@@ -820,7 +821,7 @@ int slots_of(const tsv_tok_shape& s) { return takes_tc(s) ? 148 / tc_halves(s.d)
 
 // Keys are split where the tiles alone would leave SMs without work.  Tiles of 16 rows: into shares of 32 keys and more, up to eight as a
 // cluster's CTAs, which join them; into more, of 512 keys and more, through partial outputs.  (8 sequences of 8 key heads x 128, 32 k keys:
-// 9 shares, nearly two rounds of CTAs, 262 us; 4, not all of one, 278.)
+// 9 shares, nearly two rounds of CTAs, 229 us; 8 at most, 238.)
 AttnPlan plan_of(const tsv_tok_shape& s, int64_t rows) {
   AttnPlan p;
   p.tc = takes_tc(s);

@@ -25,17 +25,19 @@
 // an item belongs to the two CTAs of a cluster, each with half of the columns of Q, K, V and O: it multiplies its halves of Q and K, sends
 // its part of S to the other through distributed shared memory, adds what comes from there, and both do the same softmax.  Nothing is
 // read or multiplied twice, Q fits twice (the next tile's comes under this one's work) and so do three blocks of 48 keys.  Prompts of 64
-// heads x 512: 644 us; with all of Q and K in both CTAs, which was the form before, 755 with blocks of 48 keys and 828 of 64.
+// heads x 512: 654 us (cold; 649 to 667 in a long run); with all of Q and K in both CTAs, which was the form before, 755 with blocks of
+// 48 keys and 828 of 64.
 //
 // Softmax: S is read once, in slabs of 64 keys (48 at d = 512).  The row's reference is its first maximum, rounded up to a whole power of
 // two; it moves where a later slab exceeds it by more than 2^10 (bf16 and fp32 have the range for weights above one), and then what is
 // there of P, the sum and O are multiplied by a power of two, exactly.  Nearly never after the first slab.
-// P is rounded to bf16 for the product (2^-9 of a weight); scores, sums and O are fp32.
+// P is rounded to bf16 for the product (half a step, at most 2^-8 of a weight); scores, sums and O are fp32.
 //
-// What bounds it (prompts of 32 heads on 8 x 128, window 1024, 17 k tokens: 540 us, 35 % of the tensor pipe's cycles, 37 % of the special
-// function units'): a tile's softmax of 64 keys takes 2.2 k cycles, a third of it the exponentials, which two warps of a scheduler share
+// What bounds it (prompts of 32 heads on 8 x 128, window 1024, 17 k tokens: 549 us cold, 585 to 595 at the clocks of a long run; 36 % of the
+// tensor pipe's cycles, 38 % of the special function units'): a tile's softmax of 64 keys takes 2.2 k cycles, a third of it the exponentials, which two warps of a scheduler share
 // the unit for, the rest latencies of dependent instructions; the products of both tiles 1.6 k (K = 16 of P V from tensor memory costs
-// 103 cycles for 128 columns, of S from shared memory 50 up to 64 keys).  At d = 512 a block's softmax and exchange (2.5 k cycles for 48 keys, of which 0.5 wait for the other CTA).
+// 103 cycles for 128 columns, of S from shared memory 50 up to 64 keys).  At d = 512 a block's softmax and exchange (2.5 k cycles for 48 keys,
+// of which 0.5 wait for the other CTA).  Figures of two forms are those of the step that they belong to, cold.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
