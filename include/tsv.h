@@ -17,8 +17,8 @@
  *     work is enqueued on `stream` and the call returns.  Between calls it keeps nothing of the
  *     caller's data; what it does keep per process is set-up it does once (kernel attributes,
  *     the number of CTA pairs a device holds, the driver entry point for tensor maps), the
- *     launch counter behind tsv_kernel_launches(), and for tree_verify_attn_static the
- *     address of its built-in array.
+ *     launch counter behind tsv_kernel_launches(), the number that tsv_set_wait_tries() gave,
+ *     and for tree_verify_attn_static the address of its built-in array.
  *   - Stream order: the calls of a layer run in the order given above on one stream.  The kernels are
  *     launched as programmatic dependents; those of branch_state_build and accept_and_refresh wait for
  *     all earlier work before they do anything (tree_verify_layer begins with branch_state_build's).  Some kernels of
@@ -198,6 +198,11 @@ int tsv_version(void);
 
 /* Kernels this library has launched in this process so far (monotonic counter; reporting only). */
 uint64_t tsv_kernel_launches(void);
+
+/* How often the waits inside the token-level and page kernels (second half of this file) try before they give up, in launches
+ * from now on; negative: their usual numbers, which stand unless this is called.  For tests of what a caller does then
+ * (TSV_ST_INTERNAL).  Always TSV_OK. */
+int tsv_set_wait_tries(int64_t tries);
 
 /* Text for a TSV_ERR_* code; static storage. */
 const char *tsv_error_string(int code);

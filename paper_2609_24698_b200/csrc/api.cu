@@ -202,9 +202,10 @@ extern "C" {
 
 int tsv_version(void) { return 1000; }
 
-// For tests (not in the header): the waits of the token-level and page kernels give up after this many tries in launches from now on, negative: after
-// their usual number.
-void tsv_test_wait_tries(int64_t tries) { g_tries.store(tries < 0 ? -1 : tries > 0xffffffffll ? 0xffffffffll : tries, std::memory_order_relaxed); }
+int tsv_set_wait_tries(int64_t tries) {
+  g_tries.store(tries < 0 ? -1 : tries > 0xffffffffll ? 0xffffffffll : tries, std::memory_order_relaxed);
+  return TSV_OK;
+}
 
 uint64_t tsv_kernel_launches(void) { return g_launches.load(std::memory_order_relaxed); }
 

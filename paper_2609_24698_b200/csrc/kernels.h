@@ -5,7 +5,7 @@
 namespace tsv {
 
 void count_launch(int n = 1);         // bumps the reporting counter behind tsv_kernel_launches()
-uint32_t wait_tries(uint32_t usual);  // tries before a wait gives up: the usual number, unless tsv_test_wait_tries has set another
+uint32_t wait_tries(uint32_t usual);  // tries before a wait gives up: the usual number, unless tsv_set_wait_tries has given another
 
 // Every kernel of the library asks for the same (maximal) shared-memory carve-out: consecutive kernels with different
 // carve-outs make the SMs drain and reconfigure between launches, which costs far more than these kernels run.

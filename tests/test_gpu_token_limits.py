@@ -137,8 +137,8 @@ def test_first_rows_at_the_ends_of_64_bits(api, dtype, n):
 def tries(api):
     """Sets how often the waits inside the kernels try before they give up, for the launches of one test."""
     import ctypes as C
-    f = api[0]._lib.tsv_test_wait_tries
-    f.argtypes, f.restype = [C.c_int64], None
+    f = api[0]._lib.tsv_set_wait_tries
+    f.argtypes, f.restype = [C.c_int64], C.c_int
     yield f
     torch.cuda.synchronize()
     f(-1)
