@@ -236,11 +236,14 @@ __global__ void __launch_bounds__(kRopeThreads, UPL == 1 ? 2 : 1) rope_kernel(co
           bc[p][i] = pair2(wb[0] * c[0].x, wb[1] * c[1].x); bs[p][i] = pair2(-wb[0] * c[0].y, -wb[1] * c[1].y);
         }
       }
-      bool later = false;
-      auto walk = [&](auto slow) {
+      // 32 heads of a lane, a bit each in `later` for those that are to be done once more (the outputs may be the inputs' places: what has been
+      // written cannot be looked at again)
+      uint32_t later = 0;
+      auto walk = [&](auto slow, int from) {
         constexpr bool SLOW = decltype(slow)::value;
+        uint32_t bit = 1;
 #pragma unroll 1
-        for (int h0 = first; h0 < heads; h0 += AHEAD * step) {
+        for (int h0 = from; h0 < heads && bit; h0 += AHEAD * step, bit <<= AHEAD) {
           if (SLOW || !(early && which == 0 && h0 == first)) fetch(in, h0, heads);
 #pragma unroll
           for (int e = 0; e < AHEAD; ++e) {
@@ -256,8 +259,8 @@ __global__ void __launch_bounds__(kRopeThreads, UPL == 1 ? 2 : 1) rope_kernel(co
             float ss = (sa.x + sa.y) + (sb.x + sb.y);
             for (int o = a.group >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
             float mean = fmaf(ss, inv_d, a.eps);
-            const bool far = !in_range(mean);
-            later |= far;
+            const bool far = SLOW ? (later & bit << e) != 0 : !in_range(mean);
+            if (!SLOW && far) later |= bit << e;
             if (SLOW) {
               float mx = 0.f, s1 = 0.f;
 #pragma unroll
@@ -305,8 +308,11 @@ __global__ void __launch_bounds__(kRopeThreads, UPL == 1 ? 2 : 1) rope_kernel(co
           }
         }
       };
-      walk(std::false_type());
-      if (__any_sync(0xffffffffu, later)) walk(std::true_type());      // (nearly never; the others' places may be their inputs')
+#pragma unroll 1
+      for (int from = first; from < heads; from += 32 * step, later = 0) {
+        walk(std::false_type(), from);
+        if (__any_sync(0xffffffffu, later != 0)) walk(std::true_type(), from);      // (nearly never)
+      }
     }
   }
 }

@@ -433,3 +433,25 @@ def test_shares_of_infinite_keys(api, heads, L, first, last):
     ok = np.isfinite(ref)
     # (a rounding of each weight, of the result, and of fp32 sums)
     assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 1e-3) * mag)[ok].all()
+
+
+@pytest.mark.parametrize("dtype,H,Hk,d", [("bf16", 40, 8, 128), ("bf16", 100, 1, 512), ("fp32", 9, 3, 512), ("fp32", 6, 2, 64)])
+@pytest.mark.parametrize("tokens", [3, 300])
+def test_norms_in_place_at_the_ends_of_the_range(api, dtype, H, Hk, d, tokens):
+    """Heads that are done once more beside heads whose results are as far out as those: weights of 1e-25 bring every result there.  In place every head is
+    done once, with the bits of outputs of their own."""
+    _, tk, _ = api
+    lay = Layer(tk, dtype, H, Hk, d, True, window=1, sinks=0, L=[0], n=[tokens], seed=d)
+    rng = np.random.default_rng(H)
+    for x in (lay.q, lay.k):
+        x *= torch.from_numpy(10.0 ** rng.choice([0, 0, 0, 30, -30], size=(*x.shape[:2], 1))).to(x)
+    w = torch.full((d,), 1e-25, device="cuda")
+    inv = (10000.0 ** -torch.arange(0, 1, 2 / 32, device="cuda")).float()
+    qo, ko = torch.empty_like(lay.q), torch.empty_like(lay.k)
+    call = lambda qo, ko: tk.qk_norm_rope(lay.shape, lay.cache.L, lay.batch, lay.q, lay.k, qo, ko, w, w, 0.0, inv, 16, False, lay.status)
+    call(qo, ko)
+    r = slice(lay.row0[0], lay.row0[0] + tokens)
+    ref, mag = T.norm_rope(f64(lay.q[r]), f64(w), 0.0, range(tokens), f64(inv), 16, False)
+    assert (np.abs(f64(qo[r]) - ref) <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref) + mag * (d * 2.0 ** -24 + 2.0 ** -20)).all()
+    call(lay.q, lay.k)
+    assert torch.equal(lay.q[r], qo[r]) and torch.equal(lay.k[r], ko[r]) and not lay.status.any()
