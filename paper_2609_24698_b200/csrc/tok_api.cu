@@ -124,8 +124,8 @@ int qk_norm_rope(const tsv_tok_shape* shape, const int32_t* L, const tsv_tok_bat
   const int64_t n = batch->rows;
   const bool q = in->q && n, k = in->k && n;
   // (an output may be its input, row by row; anything else of the call that it shares a row with would be read after it is written)
-  if (q && !(q_out == in->q && ldq == in->q_ld) && rows_meet(shape, q_out, ldq, shape->H, in->q, in->q_ld, shape->H, n)) return TSV_ERR_SHAPE;
-  if (k && !(k_out == in->k && ldk == in->k_ld) && rows_meet(shape, k_out, ldk, shape->Hk, in->k, in->k_ld, shape->Hk, n)) return TSV_ERR_SHAPE;
+  if (q && !(q_out == in->q && (ldq == in->q_ld || n == 1)) && rows_meet(shape, q_out, ldq, shape->H, in->q, in->q_ld, shape->H, n)) return TSV_ERR_SHAPE;
+  if (k && !(k_out == in->k && (ldk == in->k_ld || n == 1)) && rows_meet(shape, k_out, ldk, shape->Hk, in->k, in->k_ld, shape->Hk, n)) return TSV_ERR_SHAPE;
   if (q && k && (rows_meet(shape, q_out, ldq, shape->H, in->k, in->k_ld, shape->Hk, n) || rows_meet(shape, k_out, ldk, shape->Hk, in->q, in->q_ld, shape->H, n) ||
                  rows_meet(shape, q_out, ldq, shape->H, k_out, ldk, shape->Hk, n))) return TSV_ERR_SHAPE;
   return launch_rope(*shape, L, *batch, *in, wq, wk, eps, inv_freq, rot, first, pairs != 0, q_out, ldq, k_out, ldk, status, (cudaStream_t)stream);

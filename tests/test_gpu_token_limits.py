@@ -455,3 +455,20 @@ def test_norms_in_place_at_the_ends_of_the_range(api, dtype, H, Hk, d, tokens):
     assert (np.abs(f64(qo[r]) - ref) <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref) + mag * (d * 2.0 ** -24 + 2.0 ** -20)).all()
     call(lay.q, lay.k)
     assert torch.equal(lay.q[r], qo[r]) and torch.equal(lay.k[r], ko[r]) and not lay.status.any()
+
+
+def test_one_row_in_place_under_a_larger_output(api):
+    """A call of one row, whose output is its input by address: the strides of neither count."""
+    _, tk, _ = api
+    H, d = 4, 64
+    shape = tk.TokenShape("bf16", 1, H, 1, d, 1, max_L=1000, max_n=1)
+    L, st = torch.tensor([7], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    batch = tk.TokenBatch(torch.zeros(1, dtype=torch.int64, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda"))
+    inv = (10000.0 ** -torch.arange(0, 1, 2 / 64, device="cuda")).float()
+    big = torch.randn(5, 2 * H * d, device="cuda").to(torch.bfloat16)
+    q = big[:, :H * d].unflatten(1, (H, d))
+    out = torch.empty(1, H, d, dtype=torch.bfloat16, device="cuda")
+    rest = big.clone()
+    tk.qk_norm_rope(shape, L, batch, q[:1], None, out, None, None, None, 1e-6, inv, 0, False, st)
+    tk.qk_norm_rope(shape, L, batch, q[:1], None, q, None, None, None, 1e-6, inv, 0, False, st)
+    assert torch.equal(q[:1], out) and torch.equal(big[1:], rest[1:]) and torch.equal(big[0, H * d:], rest[0, H * d:]) and not st.any()
