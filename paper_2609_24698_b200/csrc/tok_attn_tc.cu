@@ -760,6 +760,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tc_kernel(const __grid_co
         uint32_t an;
         const int p = position(w, rt + row, an);
         const uint32_t still = __ballot_sync(FULL, C::PAIR == 2 ? bad_in_pair(odd) : odd);
+        __syncwarp();                                      // (a row's own lane has written it before: the warp's stores come behind those)
         for (uint32_t todo = __ballot_sync(FULL, bad); todo; todo &= todo - 1) {
           const int x = __ffs(todo) - 1;
           exact_output(a, t, w.depth, t.r0 + r0 + x, __shfl_sync(FULL, p, x), __shfl_sync(FULL, an, x), w.k0, w.k1, col0,
